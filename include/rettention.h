@@ -266,6 +266,89 @@ rt_status rt_attn_sparse_reshape(const void* q, const void* k, const void* v, rt
 rt_status rt_reshape_apply(const void* o_sparse, const float* rho, const void* resid,
                            float rho_delta, rt_dims dims, void* o, void* stream);
 
+/* ---- Training: gradients of attention, and the layer norm -------------------------- */
+
+/* Transpose of a block mask: which query blocks keep each key block, the walk of dK and dV.
+ * `t` describes the result, an rt_bsr whose row_ptr and col_idx are written: row kb of mask m
+ * lists the query blocks whose rows of mask m hold kb, ascending; rows may be empty here.  Its
+ * block, n_qblk and n_masks must equal the mask's; t->nnz is the room in col_idx, at least the
+ * entries of all rows (mask->nnz, unless masks share entries; RT_ECAPACITY below mask->nnz).
+ * If the rows hold more than t->nnz entries all of t's row_ptr entries become -1, which the
+ * gradient calls answer with NaN in dk and dv.  T: the token count the mask was made for.
+ * A mask that is kept for many calls is transposed once. */
+rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, void* stream);
+
+/* Gradients of dense attention (Eq.1) for Q, K and V, the probabilities recomputed from the
+ * row statistics of the forward call:
+ *   P_ij = exp(A^pre_ij - m_i) / l_i          delta_i = dO_i . O_i
+ *   dV_j = sum_i P_ij dO_i                    dS_ij = P_ij (dO_i . V_j - delta_i)
+ *   dQ_i = sum_j dS_ij K_j / sqrt(D)          dK_j = sum_i dS_ij Q_i / sqrt(D)
+ * q, k, v, o, d_o: device bf16 [B,H,T,D]; row_max, row_sum: device fp32 [B,H,T], of
+ * rt_attn_full for these q, k, v; dq, dk, dv: device bf16 [B,H,T,D] (written).  P and dS are
+ * rounded to bf16 for the matrix products, whose sums are fp32.  Equal calls give equal
+ * bits.  workspace: device memory, 16-byte aligned, of at least the bytes that
+ * rt_attn_full_backward_workspace reports (RT_ECAPACITY below), overwritten; it, and the
+ * outputs, must not overlap each other or an input. */
+rt_status rt_attn_full_backward_workspace(rt_dims dims, int64_t* bytes);
+rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, const void* o,
+                                const float* row_max, const float* row_sum, const void* d_o, rt_dims dims,
+                                void* dq, void* dk, void* dv, void* workspace, int64_t workspace_bytes,
+                                void* stream);
+
+/* Gradients of sparse attention (Eq.5), or of the reshaped output
+ *   min(1, rho + rho_delta) * SparseAttention(Q,K,V) + R
+ * for Q, K, V and rho (R's gradient is d_o itself).  As rt_attn_full_backward, over the kept
+ * keys: o, row_max, row_sum are those of rt_attn_sparse (O_S, not the reshaped output); with
+ * w_i = min(1, rho_i + rho_delta), or 1 where rho is NULL, P_ij carries the factor w_i, and
+ *   d_rho_i = dO_i . O_i  where rho_i + rho_delta <= 1, else 0.
+ * mask: the call's block mask; t: its transpose by rt_index_transpose.  rho, d_rho: device
+ * fp32 [B,H,T] (d_rho written); both may be NULL, d_rho alone too (d_rho needs rho).
+ * A ratio is not negative: rows with rho + rho_delta < 0 give NaN.  A query row whose block
+ * keeps no key has no probabilities: its dq is 0 and it adds nothing to dk and dv; a key
+ * block that no query keeps gets 0. */
+rt_status rt_attn_sparse_backward_workspace(rt_dims dims, const rt_bsr* mask, int64_t* bytes);
+rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, const void* o,
+                                  const float* row_max, const float* row_sum, const void* d_o, rt_dims dims,
+                                  const rt_bsr* mask, const rt_bsr* t, const float* rho, float rho_delta,
+                                  void* dq, void* dk, void* dv, float* d_rho, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/* Layer norm.  Rows are counted by three indices (n0, n1, n2) and hold `width` consecutive
+ * elements of `type`; a tensor's stride[3] gives the elements from one row to the next in
+ * each index, so that a call can read the heads of a packed projection and write [B,H,T,D].
+ * weight and bias: weight_sets vectors [weight_sets][width], contiguous, fp32 or of the rows'
+ * type: one set for all rows, or (weight_sets == n0) one for each value of the first index.
+ * 1 <= width <= 16384, n0 * n1 * n2 < 2^31, n0 <= 65535 where each has its own set. */
+enum { RT_BF16 = 0, RT_F16 = 1, RT_F32 = 2 };
+typedef struct {
+    int32_t n0, n1, n2, width;
+    int32_t type;        /* of x, y and their gradients                    */
+    int32_t weight_type; /* of weight and bias: `type` or RT_F32          */
+    int32_t weight_sets; /* 1 or n0                                       */
+} rt_norm_dims;
+
+/* mean and variance of each row (over its elements, no correction), y = (x - mean) rstd * w + b
+ * with rstd = 1 / sqrt(var + eps), in 32 bits.  x: device; y: device (written); weight, bias:
+ * device or NULL (1 and 0); mean, rstd: device fp32 [n0][n1][n2] (written) or NULL.  eps is
+ * finite and not negative.  Elements of y may not share memory; the span of an output's
+ * elements must not overlap another output's or an input's. */
+rt_status rt_layer_norm(const void* x, const int64_t x_stride[3], const void* weight, const void* bias,
+                        rt_norm_dims dims, float eps, void* y, const int64_t y_stride[3], float* mean,
+                        float* rstd, void* stream);
+
+/* Gradients of rt_layer_norm.  With xh = (x - mean) rstd and g = dy w:
+ *   dx = rstd (g - mean(g) - xh mean(g xh));  d_weight = sum of dy xh, d_bias = sum of dy over
+ * the rows of each weight set.  mean, rstd: of the forward call; dx has x's type; d_weight,
+ * d_bias: device fp32 [weight_sets][width] (written), each may be NULL; without rows they are 0.
+ * Sums are fp32 in a fixed order: equal calls give equal bits.  workspace: as above, of the
+ * bytes rt_layer_norm_backward_workspace reports. */
+rt_status rt_layer_norm_backward_workspace(rt_norm_dims dims, int64_t* bytes);
+rt_status rt_layer_norm_backward(const void* dy, const int64_t dy_stride[3], const void* x,
+                                 const int64_t x_stride[3], const float* mean, const float* rstd,
+                                 const void* weight, rt_norm_dims dims, void* dx, const int64_t dx_stride[3],
+                                 float* d_weight, float* d_bias, void* workspace, int64_t workspace_bytes,
+                                 void* stream);
+
 /* Static description of a status code. */
 const char* rt_status_str(rt_status status);
 

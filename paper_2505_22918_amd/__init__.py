@@ -14,6 +14,10 @@ library (the binding only marshals pointers and sizes).
   reshape_apply         the reshape on a precomputed sparse output (Eq.9, 10)
   attn_cache            one-pass caching step: O_full, rho and R (App. A.3, Eq.8, 10)
   attn_postmask         post-softmax masking (A o M) V (Eq.7)
+  attn_full_backward    gradients of dense attention for Q, K, V
+  attn_sparse_backward  gradients of sparse attention, or of its reshaped output, for Q, K, V (and rho)
+  layer_norm            layer norm of rows, of any row strides, with row statistics
+  layer_norm_backward   its gradients, the weight's and bias's among them
   StatCache             per-layer cache of rho and R with the step schedule of Sec.5
 """
 
@@ -39,6 +43,10 @@ __all__ = [
     "cache_build",
     "attn_sparse_reshape",
     "reshape_apply",
+    "attn_full_backward",
+    "attn_sparse_backward",
+    "layer_norm",
+    "layer_norm_backward",
     "StatCache",
     "PAT_EXPLICIT",
     "PAT_LOCAL2D",
@@ -212,6 +220,40 @@ class BlockMask:
             self.__dict__["_c"] = c
         return c
 
+    def transposed(self):
+        """The mask's transpose as the gradient calls take it (rt_index_transpose): row kb lists the query
+        blocks that keep key block kb.  Built on first use on the current stream and kept with the mask, so
+        that a mask of many steps is transposed once; under graph capture, unless it is known to be complete,
+        it is built anew as part of the graph and not kept.  n_masks > 1: masks that share entries of col_idx
+        (from_csr allows for them) do not fit and make the gradients dk and dv NaN."""
+        torch = _torch()
+        with _on(self.row_ptr):
+            raw = _stream(self.row_ptr)
+            capturing = torch.cuda.is_current_stream_capturing()
+            kept = self.__dict__.get("_t")
+            if kept is not None:
+                t, done, built_on = kept
+                if done is None:
+                    return t
+                if not capturing:
+                    if done.query():
+                        self.__dict__["_t"] = (t, None, None)
+                    elif raw != built_on:
+                        torch.cuda.current_stream().wait_event(done)
+                    return t
+            room = self.__dict__.get("_entries", self.nnz)
+            row_ptr = torch.empty_like(self.row_ptr)
+            col_idx = torch.empty(max(room, 1), dtype=torch.int32, device=row_ptr.device)
+            t = BlockMask(row_ptr, col_idx, self.block, self.n_qblk, int(room), self.n_masks)
+            lib = _lib.load()
+            _lib.check("rt_index_transpose", lib.rt_index_transpose(
+                ctypes.byref(self.c_struct()), self.n_qblk * self.block, ctypes.byref(t.c_struct()), raw))
+            if not capturing:
+                done = torch.cuda.Event()
+                done.record()
+                self.__dict__["_t"] = (t, done, raw)
+        return t
+
     @classmethod
     def from_csr(cls, row_ptr, col_idx, block, device="cuda", n_masks=1):
         """Checks a host CSR (numpy / lists) with rt_bsr_check, then copies it to
@@ -233,7 +275,10 @@ class BlockMask:
                                                     hci.ctypes.data if hci.size else None))
         rp = torch.from_numpy(hrp).to(device).contiguous()
         ci = torch.from_numpy(hci).to(device).contiguous()
-        return cls(rp, ci, int(block), n_qblk, int(hci.size), n_masks)
+        mask = cls(rp, ci, int(block), n_qblk, int(hci.size), n_masks)
+        rows = hrp.reshape(n_masks, n_qblk + 1).astype(np.int64)
+        mask.__dict__["_entries"] = max(int((rows[:, -1] - rows[:, 0]).sum()), int(hci.size))  # masks may share entries
+        return mask
 
 
 def _pattern(kind, grid_h=0, grid_w=0, frames=0, n_text=0, keep=0, mask=None, host_mask=None, n_masks=1):
@@ -457,6 +502,166 @@ def reshape_apply(o_sparse, rho, resid, rho_delta=0.0, out=None):
         _lib.check("rt_reshape_apply", lib.rt_reshape_apply(_ptr(o_sparse), _ptr(rho), _ptr(resid), float(rho_delta),
                                                             _lib.RtDims(B, H, T, D), _ptr(o), _stream(o_sparse)))
     return o
+
+
+def _grads(out, q):
+    """The three gradient tensors: the caller's, checked against q, or new ones."""
+    if out is None:
+        return tuple(_torch().empty_like(q) for _ in range(3))
+    if len(out) != 3:
+        raise ValueError("out must hold dq, dk and dv")
+    return tuple(_bf16(t, q.shape, name, q.device) for t, name in zip(out, ("dq", "dk", "dv")))
+
+
+def _grad_inputs(q, o, row_max, row_sum, d_o):
+    torch = _torch()
+    for name, t in (("o", o), ("d_o", d_o)):
+        if not _same(t, torch.bfloat16, q.shape, q):
+            _bf16(t, q.shape, name, q.device)
+    for name, t in (("row_max", row_max), ("row_sum", row_sum)):
+        if not _same(t, torch.float32, q.shape[:3], q):
+            _stat(t, q.shape[:3], name, q.device)
+
+
+def _workspace(nbytes, like):
+    # returns to torch's stream-ordered cache after the call; a later reuse on this stream runs after the launches
+    return _torch().empty(max(int(nbytes) // 4, 4), dtype=_torch().float32, device=like.device)
+
+
+def attn_full_backward(q, k, v, o, row_max, row_sum, d_o, out=None):
+    """Gradients (dq, dk, dv) of dense attention (Eq.1) for the gradient d_o of its output: o, row_max and
+    row_sum are attn_full's for these q, k, v.  out: three tensors to write instead of new ones."""
+    lib = _lib.load()
+    dims = _check_qkv(q, k, v)
+    _grad_inputs(q, o, row_max, row_sum, d_o)
+    dq, dk, dv = _grads(out, q)
+    need = ctypes.c_int64(0)
+    _lib.check("rt_attn_full_backward_workspace", lib.rt_attn_full_backward_workspace(dims, ctypes.byref(need)))
+    work = _workspace(need.value, q)
+    with _on(q):
+        _lib.check("rt_attn_full_backward",
+                   lib.rt_attn_full_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(row_max), _ptr(row_sum),
+                                             _ptr(d_o), dims, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(work), need.value,
+                                             _stream(q)))
+    return dq, dk, dv
+
+
+def attn_sparse_backward(q, k, v, o, row_max, row_sum, d_o, mask: BlockMask, rho=None, rho_delta=0.0, out=None):
+    """Gradients (dq, dk, dv) of sparse attention (Eq.5), or with rho (dq, dk, dv, d_rho) of its reshaped output
+    min(1, rho + rho_delta) * SparseAttn + R, for the output's gradient d_o (which is R's gradient too).  o,
+    row_max and row_sum are attn_sparse's for these q, k, v and mask: the sparse output, not the reshaped one.
+    out: three tensors to write dq, dk, dv into instead of new ones."""
+    torch = _torch()
+    lib = _lib.load()
+    dims = _check_qkv(q, k, v)
+    _mask_on(mask, q)
+    _grad_inputs(q, o, row_max, row_sum, d_o)
+    if rho is not None and not _same(rho, torch.float32, q.shape[:3], q):
+        _stat(rho, q.shape[:3], "rho", q.device)
+    dq, dk, dv = _grads(out, q)
+    bsr, need = mask.c_struct(), ctypes.c_int64(0)
+    _lib.check("rt_attn_sparse_backward_workspace",
+               lib.rt_attn_sparse_backward_workspace(dims, ctypes.byref(bsr), ctypes.byref(need)))
+    if q.numel() == 0:
+        return (dq, dk, dv) if rho is None else (dq, dk, dv, torch.empty_like(rho))
+    t = mask.transposed()
+    d_rho = torch.empty_like(rho) if rho is not None else None
+    work = _workspace(need.value, q)
+    with _on(q):
+        _lib.check("rt_attn_sparse_backward",
+                   lib.rt_attn_sparse_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(row_max), _ptr(row_sum),
+                                               _ptr(d_o), dims, ctypes.byref(bsr), ctypes.byref(t.c_struct()),
+                                               _ptr(rho), float(rho_delta), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_rho),
+                                               _ptr(work), need.value, _stream(q)))
+    return (dq, dk, dv) if rho is None else (dq, dk, dv, d_rho)
+
+
+_NORM_TYPES = None
+
+
+def _norm_rows(x, name, like=None):
+    """x as rows of its last dimension: (sizes, strides) of three leading indices."""
+    global _NORM_TYPES
+    torch = _torch()
+    if _NORM_TYPES is None:
+        _NORM_TYPES = {torch.bfloat16: _lib.RT_BF16, torch.float16: _lib.RT_F16, torch.float32: _lib.RT_F32}
+    _on_device(x, name, like.device if like is not None else None)
+    if x.dtype not in _NORM_TYPES or not 2 <= x.dim() <= 4 or (x.shape[-1] > 1 and x.stride(-1) != 1):
+        raise ValueError(f"{name} must be a bf16, fp16 or fp32 tensor of 2 to 4 dimensions, its last one contiguous")
+    if like is not None and (x.dtype is not like.dtype or x.shape != like.shape):
+        raise ValueError(f"{name} must have the type and shape of x")
+    shape, stride = tuple(x.shape[:-1]), x.stride()[:-1]
+    # leading indices first: the weight sets go by the first dimension of x
+    pad = 3 - len(shape)
+    return shape[:1] + (1,) * pad + shape[1:], _lib.Strides(*(stride[:1] + (0,) * pad + stride[1:]))
+
+
+def _norm_dims(x, sizes, weight, bias):
+    torch = _torch()
+    wt, sets = torch.float32, 1
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is None:
+            continue
+        _on_device(t, name, x.device)
+        if t.dtype not in (torch.float32, x.dtype) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous fp32 tensor, or one of x's type")
+        if tuple(t.shape) not in ((x.shape[-1],), (x.shape[0], x.shape[-1])):
+            raise ValueError(f"{name} must have the shape [{x.shape[-1]}] or [{x.shape[0]}, {x.shape[-1]}]")
+        if t is bias and weight is not None and (t.dtype is not weight.dtype or t.shape != weight.shape):
+            raise ValueError("weight and bias must share type and shape")
+        wt, sets = t.dtype, 1 if t.dim() == 1 else x.shape[0]
+    return _lib.RtNormDims(*sizes, x.shape[-1], _NORM_TYPES[x.dtype], _NORM_TYPES[wt], sets)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None):
+    """Layer norm of x's rows (its last dimension): (x - mean) / sqrt(var + eps) * weight + bias.
+
+    x: bf16, fp16 or fp32, 2 to 4 dimensions with any row strides (a permuted view of a packed projection);
+    weight, bias: [W], or [x.shape[0], W] for one set per sample, fp32 or x's type, or None.  Returns y, a new
+    contiguous tensor or `out` (any row strides); with stats (y, mean, rstd), fp32 of x.shape[:-1]."""
+    torch = _torch()
+    lib = _lib.load()
+    sizes, xs = _norm_rows(x, "x")
+    dims = _norm_dims(x, sizes, weight, bias)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _, ys = _norm_rows(y, "out", x)
+    mean = rstd = None
+    if stats:
+        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        rstd = torch.empty_like(mean)
+    with _on(x):
+        _lib.check("rt_layer_norm", lib.rt_layer_norm(_ptr(x), xs, _ptr(weight), _ptr(bias), dims, float(eps), _ptr(y),
+                                                      ys, _ptr(mean), _ptr(rstd), _stream(x)))
+    return (y, mean, rstd) if stats else y
+
+
+def layer_norm_backward(d_y, x, mean, rstd, weight=None, bias=True, out=None):
+    """Gradients (dx, d_weight, d_bias) of layer_norm for the gradient d_y of its output; mean and rstd are the
+    forward call's.  dx has x's type, in a new contiguous tensor or `out` (any row strides); d_weight and d_bias
+    are fp32 of the weight's shape, summed over the rows of each set.  Without a weight both are None; bias=False
+    leaves d_bias out."""
+    torch = _torch()
+    lib = _lib.load()
+    sizes, xs = _norm_rows(x, "x")
+    _, dys = _norm_rows(d_y, "d_y", x)
+    dims = _norm_dims(x, sizes, weight, None)
+    _stat(mean, x.shape[:-1], "mean", x.device)
+    _stat(rstd, x.shape[:-1], "rstd", x.device)
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    _, dxs = _norm_rows(dx, "out", x)
+    d_weight = d_bias = None
+    if weight is not None:
+        d_weight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
+        d_bias = torch.empty_like(d_weight) if bias else None
+    need = ctypes.c_int64(0)
+    _lib.check("rt_layer_norm_backward_workspace", lib.rt_layer_norm_backward_workspace(dims, ctypes.byref(need)))
+    work = _workspace(need.value, x)
+    with _on(x):
+        _lib.check("rt_layer_norm_backward",
+                   lib.rt_layer_norm_backward(_ptr(d_y), dys, _ptr(x), xs, _ptr(mean), _ptr(rstd), _ptr(weight), dims,
+                                              _ptr(dx), dxs, _ptr(d_weight), _ptr(d_bias), _ptr(work), need.value,
+                                              _stream(x)))
+    return dx, d_weight, d_bias
 
 
 class StatCache:

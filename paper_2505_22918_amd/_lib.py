@@ -53,6 +53,22 @@ class RtPattern(ctypes.Structure):
     ]
 
 
+class RtNormDims(ctypes.Structure):
+    _fields_ = [
+        ("n0", c_int32),
+        ("n1", c_int32),
+        ("n2", c_int32),
+        ("width", c_int32),
+        ("type", c_int32),
+        ("weight_type", c_int32),
+        ("weight_sets", c_int32),
+    ]
+
+
+RT_BF16, RT_F16, RT_F32 = range(3)
+c_int64 = ctypes.c_int64
+Strides = c_int64 * 3
+
 _SIGS = {
     "rt_bsr_check": (c_int32, [ctypes.POINTER(RtBsr), c_void_p, c_void_p]),
     "rt_dynamic_index_workspace": (c_int32, [RtDims, c_int32, c_int32, ctypes.POINTER(ctypes.c_int64)]),
@@ -77,6 +93,18 @@ _SIGS = {
                                          c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p,
                                          c_void_p]),
     "rt_reshape_apply": (c_int32, [c_void_p, c_void_p, c_void_p, c_float, RtDims, c_void_p, c_void_p]),
+    "rt_index_transpose": (c_int32, [ctypes.POINTER(RtBsr), c_int32, ctypes.POINTER(RtBsr), c_void_p]),
+    "rt_attn_full_backward_workspace": (c_int32, [RtDims, ctypes.POINTER(c_int64)]),
+    "rt_attn_full_backward": (c_int32, [c_void_p] * 7 + [RtDims] + [c_void_p] * 4 + [c_int64, c_void_p]),
+    "rt_attn_sparse_backward_workspace": (c_int32, [RtDims, ctypes.POINTER(RtBsr), ctypes.POINTER(c_int64)]),
+    "rt_attn_sparse_backward": (c_int32, [c_void_p] * 7 + [RtDims, ctypes.POINTER(RtBsr), ctypes.POINTER(RtBsr),
+                                                          c_void_p, c_float] + [c_void_p] * 5 + [c_int64, c_void_p]),
+    "rt_layer_norm": (c_int32, [c_void_p, Strides, c_void_p, c_void_p, RtNormDims, c_float, c_void_p, Strides,
+                                c_void_p, c_void_p, c_void_p]),
+    "rt_layer_norm_backward_workspace": (c_int32, [RtNormDims, ctypes.POINTER(c_int64)]),
+    "rt_layer_norm_backward": (c_int32, [c_void_p, Strides, c_void_p, Strides, c_void_p, c_void_p, c_void_p,
+                                         RtNormDims, c_void_p, Strides, c_void_p, c_void_p, c_void_p, c_int64,
+                                         c_void_p]),
     "rt_status_str": (ctypes.c_char_p, [c_int32]),
     "rt_last_error": (ctypes.c_char_p, []),
     "rt_version": (c_int32, []),

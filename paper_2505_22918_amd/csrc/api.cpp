@@ -587,4 +587,364 @@ rt_status rt_reshape_apply(const void* o_sparse, const float* rho, const void* r
                       "reshape launch");
 }
 
+// ---- training ----------------------------------------------------------------------------
+
+namespace {
+
+// A transposed mask against the mask it belongs to.
+rt_status check_transposed(const rt_bsr* t, const rt_bsr* m) {
+    if (!t) return fail(RT_EINVAL, "the transposed mask is NULL");
+    const int32_t nm = m->n_masks > 1 ? m->n_masks : 1, nt = t->n_masks > 1 ? t->n_masks : 1;
+    if (t->block != m->block || t->n_qblk != m->n_qblk || nt != nm)
+        return fail(RT_EINVAL, "the transposed mask (block=%d n_qblk=%d n_masks=%d) is not of this mask (%d, %d, %d)",
+                    t->block, t->n_qblk, nt, m->block, m->n_qblk, nm);
+    if (t->nnz < m->nnz)
+        return fail(RT_ECAPACITY, "the transposed mask has room for %d entries, the mask has %d", t->nnz, m->nnz);
+    RT_TRY(check_stat(t->row_ptr, "the transposed mask's row_ptr"));
+    RT_TRY(check_stat(t->col_idx, "the transposed mask's col_idx"));
+    return RT_OK;
+}
+
+int64_t mask_ptr_bytes(const rt_bsr* m) {
+    return (int64_t)(m->n_masks > 1 ? m->n_masks : 1) * ((int64_t)m->n_qblk + 1) * 4;
+}
+
+typedef std::pair<const void*, int64_t> range;
+
+// No output overlaps an input or another output.
+rt_status check_ranges(std::initializer_list<std::pair<range, const char*>> outs, std::initializer_list<range> ins) {
+    for (auto o = outs.begin(); o != outs.end(); ++o) {
+        if (!o->first.first) continue;
+        RT_TRY(check_no_overlap(o->first.first, o->first.second, o->second, ins, "an input"));
+        for (auto p = outs.begin(); p != o; ++p)
+            if (p->first.first && overlaps(o->first.first, o->first.second, p->first.first, p->first.second))
+                return fail(RT_EINVAL, "%s overlaps %s", o->second, p->second);
+    }
+    return RT_OK;
+}
+
+int64_t backward_workspace(const rt_dims& d) { return (int64_t)d.B * d.H * d.T * 8; }
+
+// What the dense and the sparse gradient call check and set alike (rho and the mask aside).
+rt_status grad_args(const void* q, const void* k, const void* v, const void* o, const float* row_max,
+                    const float* row_sum, const void* d_o, const rt_dims& d, void* dq, void* dk, void* dv,
+                    void* workspace, int64_t workspace_bytes, int64_t need, rt::GradArgs* out) {
+    RT_TRY(check_qkv(q, k, v, const_cast<void*>(o)));
+    RT_TRY(check_tensor(d_o, "d_o"));
+    RT_TRY(check_stat(row_max, "row_max"));
+    RT_TRY(check_stat(row_sum, "row_sum"));
+    RT_TRY(check_tensor(dq, "dq"));
+    RT_TRY(check_tensor(dk, "dk"));
+    RT_TRY(check_tensor(dv, "dv"));
+    RT_TRY(check_tensor(workspace, "workspace"));
+    if (workspace_bytes < need)
+        return fail(RT_ECAPACITY, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+    rt::GradArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.o = static_cast<const uint16_t*>(o);
+    a.d_o = static_cast<const uint16_t*>(d_o);
+    a.row_max = row_max;
+    a.row_sum = row_sum;
+    a.dq = static_cast<uint16_t*>(dq);
+    a.dk = static_cast<uint16_t*>(dk);
+    a.dv = static_cast<uint16_t*>(dv);
+    a.row_log = static_cast<float*>(workspace);
+    a.row_delta = a.row_log + (size_t)d.B * d.H * d.T;
+    a.T = d.T;
+    a.heads = d.H;
+    a.n_bh = d.B * d.H;
+    a.scale_nat = (float)(1.0 / std::sqrt((double)d.D));
+    a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d.D));
+    *out = a;
+    return RT_OK;
+}
+
+int64_t type_bytes(int32_t type) { return type == RT_F32 ? 4 : 2; }
+
+// Shape checks of the norm calls; *rows may come out 0.
+rt_status check_norm(const rt_norm_dims& d, int64_t* rows) {
+    if (d.n0 < 0 || d.n1 < 0 || d.n2 < 0) return fail(RT_EINVAL, "negative dims n0=%d n1=%d n2=%d", d.n0, d.n1, d.n2);
+    if (d.type != RT_BF16 && d.type != RT_F16 && d.type != RT_F32) return fail(RT_EUNSUPPORTED, "type=%d", d.type);
+    if (d.weight_type != d.type && d.weight_type != RT_F32)
+        return fail(RT_EUNSUPPORTED, "weight_type=%d (supported: fp32, or the rows' type)", d.weight_type);
+    if (d.width < 1) return fail(RT_EINVAL, "width=%d (need >= 1)", d.width);
+    if (d.width > 16384) return fail(RT_EUNSUPPORTED, "width=%d (supported: up to 16384)", d.width);
+    if (d.weight_sets != 1 && d.weight_sets != d.n0)
+        return fail(RT_EINVAL, "weight_sets=%d (need 1 or n0=%d)", d.weight_sets, d.n0);
+    if (d.weight_sets > 65535) return fail(RT_EUNSUPPORTED, "weight_sets=%d (supported: up to 65535)", d.weight_sets);
+    const int64_t n01 = (int64_t)d.n0 * d.n1;
+    if (n01 > INT32_MAX || n01 * d.n2 > INT32_MAX) return fail(RT_EINVAL, "n0 * n1 * n2 must be below 2^31");
+    *rows = n01 * d.n2;
+    return RT_OK;
+}
+
+// Checks the rows of one tensor: alignment to its elements, strides that stay within 2^48 elements.  Writes the byte
+// span from its first to its last element; distinct: no two rows may share memory (outputs).
+rt_status check_rows(const void* p, const int64_t stride[3], const rt_norm_dims& d, bool distinct, const char* name,
+                     int64_t* span) {
+    if (!p) return fail(RT_EINVAL, "%s is NULL", name);
+    if (!stride) return fail(RT_EINVAL, "%s's strides are NULL", name);
+    const int64_t size = type_bytes(d.type);
+    if (reinterpret_cast<uintptr_t>(p) % (uintptr_t)size != 0)
+        return fail(RT_EINVAL, "%s is not aligned to its elements", name);
+    const int64_t n[3] = {d.n0, d.n1, d.n2};
+    int64_t last = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (n[i] < 2) continue;
+        if (stride[i] < 0) return fail(RT_EINVAL, "%s has a negative stride", name);
+        if (stride[i] > ((int64_t)1 << 48) / n[i]) return fail(RT_EINVAL, "%s is too large", name);
+        last += stride[i] * (n[i] - 1);
+    }
+    if (distinct) {  // from the closest rows on, each index's step has to pass over what the ones before it cover
+        int order[3] = {0, 1, 2};
+        std::sort(order, order + 3, [&](int x, int y) { return stride[x] < stride[y]; });
+        int64_t covered = d.width;
+        for (int i : order) {
+            if (n[i] < 2) continue;
+            if (stride[i] < covered) return fail(RT_EINVAL, "rows of %s share memory", name);
+            covered += stride[i] * (n[i] - 1);
+        }
+    }
+    *span = (last + d.width) * size;
+    return RT_OK;
+}
+
+// Strides as the kernels take them, and whether rows can be counted flat and read in 16-byte pieces.
+void set_rows(rt::NormArgs& a, const rt_norm_dims& d, std::initializer_list<std::pair<const void*, const int64_t*>> ts) {
+    const int64_t size = type_bytes(d.type);
+    a.flat = 1;
+    a.vec = d.width % 8 == 0;
+    for (const auto& t : ts) {
+        const int64_t* s = t.second;
+        // rows of each index below 2 have no step to fit
+        const int64_t step = d.n2 > 1 ? s[2] : (d.n1 > 1 ? s[1] : (d.n0 > 1 ? s[0] : 0));
+        const bool one = (d.n2 < 2 || s[2] == step) && (d.n1 < 2 || s[1] == step * d.n2) &&
+                         (d.n0 < 2 || s[0] == step * d.n2 * d.n1);
+        if (!one) a.flat = 0;
+        if ((reinterpret_cast<uintptr_t>(t.first) & 15u) != 0) a.vec = 0;
+        const int64_t n[3] = {d.n0, d.n1, d.n2};
+        for (int i = 0; i < 3; ++i)
+            if (n[i] > 1 && s[i] * size % 16 != 0) a.vec = 0;
+    }
+}
+
+void set_strides(int64_t (&to)[3], const int64_t* s, const rt_norm_dims& d, int32_t flat) {
+    to[0] = d.n0 > 1 ? s[0] : 0;
+    to[1] = d.n1 > 1 ? s[1] : 0;
+    to[2] = d.n2 > 1 ? s[2] : 0;
+    if (flat) to[2] = d.n2 > 1 ? s[2] : (d.n1 > 1 ? s[1] : (d.n0 > 1 ? s[0] : 0));
+}
+
+void set_norm(rt::NormArgs& a, const rt_norm_dims& d, int64_t rows, const void* x, const int64_t* xs,
+              const void* weight) {
+    a.x = x;
+    a.weight = weight;
+    a.n1 = d.n1;
+    a.n2 = d.n2;
+    a.sets = (uint32_t)d.weight_sets;
+    a.rows_per_set = (uint32_t)(rows / d.weight_sets);
+    a.width = d.width;
+    a.type = d.type;
+    a.weight_f32 = d.weight_type == RT_F32;
+    set_strides(a.xs, xs, d, a.flat);
+}
+
+rt_status check_weight(const void* p, const rt_norm_dims& d, const char* name) {
+    const uintptr_t size = (uintptr_t)type_bytes(d.weight_type);
+    if (p && reinterpret_cast<uintptr_t>(p) % size != 0) return fail(RT_EINVAL, "%s is not aligned to its elements", name);
+    return RT_OK;
+}
+
+// Workgroups (partial sums of the columns) of a weight set, at most: enough over all sets for several on each CU.
+int32_t norm_parts(const rt_norm_dims& d) {
+    const int64_t all = d.width <= 2048 ? 1024 : 512;
+    return (int32_t)std::max<int64_t>(1, all / std::max(1, d.weight_sets));
+}
+
+int64_t norm_workspace(const rt_norm_dims& d) {
+    return std::max<int64_t>(16, (int64_t)d.weight_sets * norm_parts(d) * 2 * d.width * 4);
+}
+
+}  // namespace
+
+rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, void* stream) {
+    if (!mask) return fail(RT_EINVAL, "mask is NULL");
+    if (T < 0) return fail(RT_EINVAL, "T=%d", T);
+    const int64_t nm = mask->n_masks > 1 ? mask->n_masks : 1;
+    // (any count of masks: the heads are not known here)
+    RT_TRY(check_bsr(mask, rt_dims{1, (int32_t)nm, T, 64}));
+    if (mask->n_qblk == 0) return ok();
+    RT_TRY(check_transposed(t, mask));
+    if (nm * mask->n_qblk > INT32_MAX) return fail(RT_EINVAL, "too many mask rows");
+    const int64_t np = mask_ptr_bytes(mask), nc = (int64_t)mask->nnz * 4, tc = (int64_t)t->nnz * 4;
+    RT_TRY(check_ranges({{{t->row_ptr, np}, "the transposed row_ptr"}, {{t->col_idx, tc}, "the transposed col_idx"}},
+                        {{mask->row_ptr, np}, {mask->col_idx, nc}}));
+    rt::TransposeArgs a{};
+    a.row_ptr = mask->row_ptr;
+    a.col_idx = mask->col_idx;
+    a.nnz = mask->nnz;
+    a.n_blk = mask->n_qblk;
+    a.n_masks = (int32_t)nm;
+    a.t_row_ptr = const_cast<int32_t*>(t->row_ptr);
+    a.t_col_idx = const_cast<int32_t*>(t->col_idx);
+    a.t_nnz = t->nnz;
+    return hip_status(rt::launch_index_transpose(a, static_cast<hipStream_t>(stream)), "index transpose launch");
+}
+
+rt_status rt_attn_full_backward_workspace(rt_dims dims, int64_t* bytes) {
+    if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
+    bool empty = false;
+    RT_TRY(check_dims(dims, &empty));
+    *bytes = backward_workspace(dims);
+    return ok();
+}
+
+rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, const void* o, const float* row_max,
+                                const float* row_sum, const void* d_o, rt_dims dims, void* dq, void* dk, void* dv,
+                                void* workspace, int64_t workspace_bytes, void* stream) {
+    bool empty = false;
+    RT_TRY(check_dims(dims, &empty));
+    if (empty) return ok();
+    RT_TRY(check_items(dims, 32));
+    const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D, need = backward_workspace(dims);
+    rt::GradArgs a{};
+    RT_TRY(grad_args(q, k, v, o, row_max, row_sum, d_o, dims, dq, dk, dv, workspace, workspace_bytes, need, &a));
+    RT_TRY(check_ranges({{{dq, nt}, "dq"}, {{dk, nt}, "dk"}, {{dv, nt}, "dv"}, {{workspace, need}, "workspace"}},
+                        {{q, nt}, {k, nt}, {v, nt}, {o, nt}, {d_o, nt}, {row_max, ns}, {row_sum, ns}}));
+    return hip_status(rt::launch_attention_backward(a, dims.D, static_cast<hipStream_t>(stream)),
+                      "full attention gradient launch");
+}
+
+rt_status rt_attn_sparse_backward_workspace(rt_dims dims, const rt_bsr* mask, int64_t* bytes) {
+    if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
+    bool empty = false;
+    RT_TRY(check_dims(dims, &empty));
+    RT_TRY(check_bsr(mask, dims));
+    *bytes = backward_workspace(dims);
+    return ok();
+}
+
+rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, const void* o, const float* row_max,
+                                  const float* row_sum, const void* d_o, rt_dims dims, const rt_bsr* mask,
+                                  const rt_bsr* t, const float* rho, float rho_delta, void* dq, void* dk, void* dv,
+                                  float* d_rho, void* workspace, int64_t workspace_bytes, void* stream) {
+    bool empty = false;
+    RT_TRY(check_dims(dims, &empty));
+    RT_TRY(check_bsr(mask, dims));
+    if (!std::isfinite(rho_delta)) return fail(RT_EINVAL, "rho_delta is not finite");
+    if (d_rho && !rho) return fail(RT_EINVAL, "d_rho needs rho");
+    if (empty) return ok();
+    RT_TRY(check_transposed(t, mask));
+    RT_TRY(check_items(dims, 32));
+    if (rho) RT_TRY(check_stat(rho, "rho"));
+    if (d_rho) RT_TRY(check_stat(d_rho, "d_rho"));
+    const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D, need = backward_workspace(dims);
+    rt::GradArgs a{};
+    RT_TRY(grad_args(q, k, v, o, row_max, row_sum, d_o, dims, dq, dk, dv, workspace, workspace_bytes, need, &a));
+    const int64_t np = mask_ptr_bytes(mask), nc = (int64_t)mask->nnz * 4;
+    RT_TRY(check_ranges({{{dq, nt}, "dq"}, {{dk, nt}, "dk"}, {{dv, nt}, "dv"}, {{d_rho, ns}, "d_rho"},
+                         {{workspace, need}, "workspace"}},
+                        {{q, nt}, {k, nt}, {v, nt}, {o, nt}, {d_o, nt}, {row_max, ns}, {row_sum, ns}, {rho, ns},
+                         {mask->row_ptr, np}, {mask->col_idx, nc}, {t->row_ptr, np}, {t->col_idx, (int64_t)t->nnz * 4}}));
+    a.rho = rho;
+    a.rho_delta = rho_delta;
+    a.d_rho = d_rho;
+    a.row_ptr = mask->row_ptr;
+    a.col_idx = mask->col_idx;
+    a.nnz = mask->nnz;
+    a.t_row_ptr = t->row_ptr;
+    a.t_col_idx = t->col_idx;
+    a.t_nnz = t->nnz;
+    a.n_masks = mask->n_masks > 1 ? mask->n_masks : 1;
+    a.block = mask->block;
+    return hip_status(rt::launch_attention_backward(a, dims.D, static_cast<hipStream_t>(stream)),
+                      "sparse attention gradient launch");
+}
+
+rt_status rt_layer_norm(const void* x, const int64_t x_stride[3], const void* weight, const void* bias,
+                        rt_norm_dims dims, float eps, void* y, const int64_t y_stride[3], float* mean, float* rstd,
+                        void* stream) {
+    int64_t rows = 0, x_span = 0, y_span = 0;
+    RT_TRY(check_norm(dims, &rows));
+    if (!std::isfinite(eps) || eps < 0) return fail(RT_EINVAL, "eps is negative or not finite");
+    if (rows == 0) return ok();
+    RT_TRY(check_rows(x, x_stride, dims, false, "x", &x_span));
+    RT_TRY(check_rows(y, y_stride, dims, true, "y", &y_span));
+    RT_TRY(check_weight(weight, dims, "weight"));
+    RT_TRY(check_weight(bias, dims, "bias"));
+    if (mean) RT_TRY(check_stat(mean, "mean"));
+    if (rstd) RT_TRY(check_stat(rstd, "rstd"));
+    const int64_t nw = (int64_t)dims.weight_sets * dims.width * type_bytes(dims.weight_type);
+    RT_TRY(check_ranges({{{y, y_span}, "y"}, {{mean, rows * 4}, "mean"}, {{rstd, rows * 4}, "rstd"}},
+                        {{x, x_span}, {weight, nw}, {bias, nw}}));
+    rt::NormArgs a{};
+    set_rows(a, dims, {{x, x_stride}, {y, y_stride}});
+    if (weight && !aligned16(weight)) a.vec = 0;
+    if (bias && !aligned16(bias)) a.vec = 0;
+    set_norm(a, dims, rows, x, x_stride, weight);
+    a.bias = bias;
+    a.eps = eps;
+    a.y = y;
+    set_strides(a.ys, y_stride, dims, a.flat);
+    a.mean_out = mean;
+    a.rstd_out = rstd;
+    return hip_status(rt::launch_norm(a, static_cast<hipStream_t>(stream)), "layer norm launch");
+}
+
+rt_status rt_layer_norm_backward_workspace(rt_norm_dims dims, int64_t* bytes) {
+    if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
+    int64_t rows = 0;
+    RT_TRY(check_norm(dims, &rows));
+    *bytes = norm_workspace(dims);
+    return ok();
+}
+
+rt_status rt_layer_norm_backward(const void* dy, const int64_t dy_stride[3], const void* x, const int64_t x_stride[3],
+                                 const float* mean, const float* rstd, const void* weight, rt_norm_dims dims, void* dx,
+                                 const int64_t dx_stride[3], float* d_weight, float* d_bias, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+    int64_t rows = 0, x_span = 0, y_span = 0, dx_span = 0;
+    RT_TRY(check_norm(dims, &rows));
+    if (d_weight) RT_TRY(check_stat(d_weight, "d_weight"));
+    if (d_bias) RT_TRY(check_stat(d_bias, "d_bias"));
+    const int64_t ns = (int64_t)dims.weight_sets * dims.width * 4, need = norm_workspace(dims);
+    rt::NormArgs a{};
+    a.dweight = d_weight;
+    a.dbias = d_bias;
+    a.sets = (uint32_t)dims.weight_sets;
+    a.width = dims.width;
+    if (rows == 0) {  // sums over no rows
+        RT_TRY(check_ranges({{{d_weight, ns}, "d_weight"}, {{d_bias, ns}, "d_bias"}}, {}));
+        if ((!d_weight && !d_bias) || dims.weight_sets == 0) return ok();
+        return hip_status(rt::launch_norm_backward(a, 0, static_cast<hipStream_t>(stream)), "layer norm gradient launch");
+    }
+    RT_TRY(check_rows(dy, dy_stride, dims, false, "dy", &y_span));
+    RT_TRY(check_rows(x, x_stride, dims, false, "x", &x_span));
+    RT_TRY(check_rows(dx, dx_stride, dims, true, "dx", &dx_span));
+    RT_TRY(check_weight(weight, dims, "weight"));
+    RT_TRY(check_stat(mean, "mean"));
+    RT_TRY(check_stat(rstd, "rstd"));
+    RT_TRY(check_tensor(workspace, "workspace"));
+    if (workspace_bytes < need)
+        return fail(RT_ECAPACITY, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+    const int64_t nw = (int64_t)dims.weight_sets * dims.width * type_bytes(dims.weight_type);
+    RT_TRY(check_ranges({{{dx, dx_span}, "dx"}, {{d_weight, ns}, "d_weight"}, {{d_bias, ns}, "d_bias"},
+                         {{workspace, need}, "workspace"}},
+                        {{dy, y_span}, {x, x_span}, {mean, rows * 4}, {rstd, rows * 4}, {weight, nw}}));
+    set_rows(a, dims, {{dy, dy_stride}, {x, x_stride}, {dx, dx_stride}});
+    if (weight && !aligned16(weight)) a.vec = 0;
+    set_norm(a, dims, rows, x, x_stride, weight);
+    a.dy = dy;
+    a.dx = dx;
+    set_strides(a.ys, dy_stride, dims, a.flat);
+    set_strides(a.dxs, dx_stride, dims, a.flat);
+    a.mean = mean;
+    a.rstd = rstd;
+    a.partial = static_cast<float*>(workspace);
+    return hip_status(rt::launch_norm_backward(a, norm_parts(dims), static_cast<hipStream_t>(stream)),
+                      "layer norm gradient launch");
+}
+
 }  // extern "C"
