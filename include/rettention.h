@@ -271,11 +271,14 @@ rt_status rt_reshape_apply(const void* o_sparse, const float* rho, const void* r
 /* Transpose of a block mask: which query blocks keep each key block, the walk of dK and dV.
  * `t` describes the result, an rt_bsr whose row_ptr and col_idx are written: row kb of mask m
  * lists the query blocks whose rows of mask m hold kb, ascending; rows may be empty here.  Its
- * block, n_qblk and n_masks must equal the mask's; t->nnz is the room in col_idx, at least the
- * entries of all rows (mask->nnz, unless masks share entries; RT_ECAPACITY below mask->nnz).
- * If the rows hold more than t->nnz entries all of t's row_ptr entries become -1, which the
- * gradient calls answer with NaN in dk and dv.  T: the token count the mask was made for.
+ * block, n_qblk and n_masks must equal the mask's; t->nnz is the room for entries, at least
+ * those of all rows (mask->nnz, unless masks share entries; RT_ECAPACITY below mask->nnz).
+ * t->col_idx, 16-byte aligned, holds more than them: rt_index_transpose_size (host only) gives
+ * the int32 values it needs for room for `entries`; a plan of the gradient calls' work follows
+ * the entries.  If the rows hold more than t->nnz entries, all of t's row_ptr entries become -1
+ * and the gradient calls write NaN to dk and dv.  T: the token count the mask was made for.
  * A mask that is kept for many calls is transposed once. */
+rt_status rt_index_transpose_size(const rt_bsr* mask, int32_t entries, int64_t* values);
 rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, void* stream);
 
 /* Gradients of dense attention (Eq.1) for Q, K and V, the probabilities recomputed from the
@@ -305,8 +308,9 @@ rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, con
  * fp32 [B,H,T] (d_rho written); both may be NULL, d_rho alone too (d_rho needs rho).
  * A ratio is not negative: rows with rho + rho_delta < 0 give NaN.  A query row whose block
  * keeps no key has no probabilities: its dq is 0 and it adds nothing to dk and dv; a key
- * block that no query keeps gets 0. */
-rt_status rt_attn_sparse_backward_workspace(rt_dims dims, const rt_bsr* mask, int64_t* bytes);
+ * block that no query keeps gets 0.  The workspace's size goes by the transpose's room for
+ * entries (t->nnz; 0: mask->nnz). */
+rt_status rt_attn_sparse_backward_workspace(rt_dims dims, const rt_bsr* mask, int32_t room, int64_t* bytes);
 rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, const void* o,
                                   const float* row_max, const float* row_sum, const void* d_o, rt_dims dims,
                                   const rt_bsr* mask, const rt_bsr* t, const float* rho, float rho_delta,

@@ -243,9 +243,11 @@ class BlockMask:
                     return t
             room = self.__dict__.get("_entries", self.nnz)
             row_ptr = torch.empty_like(self.row_ptr)
-            col_idx = torch.empty(max(room, 1), dtype=torch.int32, device=row_ptr.device)
+            lib, values = _lib.load(), ctypes.c_int64(0)
+            _lib.check("rt_index_transpose_size",
+                       lib.rt_index_transpose_size(ctypes.byref(self.c_struct()), int(room), ctypes.byref(values)))
+            col_idx = torch.empty(values.value, dtype=torch.int32, device=row_ptr.device)
             t = BlockMask(row_ptr, col_idx, self.block, self.n_qblk, int(room), self.n_masks)
-            lib = _lib.load()
             _lib.check("rt_index_transpose", lib.rt_index_transpose(
                 ctypes.byref(self.c_struct()), self.n_qblk * self.block, ctypes.byref(t.c_struct()), raw))
             if not capturing:
@@ -559,12 +561,12 @@ def attn_sparse_backward(q, k, v, o, row_max, row_sum, d_o, mask: BlockMask, rho
     if rho is not None and not _same(rho, torch.float32, q.shape[:3], q):
         _stat(rho, q.shape[:3], "rho", q.device)
     dq, dk, dv = _grads(out, q)
-    bsr, need = mask.c_struct(), ctypes.c_int64(0)
-    _lib.check("rt_attn_sparse_backward_workspace",
-               lib.rt_attn_sparse_backward_workspace(dims, ctypes.byref(bsr), ctypes.byref(need)))
     if q.numel() == 0:
         return (dq, dk, dv) if rho is None else (dq, dk, dv, torch.empty_like(rho))
     t = mask.transposed()
+    bsr, need = mask.c_struct(), ctypes.c_int64(0)
+    _lib.check("rt_attn_sparse_backward_workspace",
+               lib.rt_attn_sparse_backward_workspace(dims, ctypes.byref(bsr), t.nnz, ctypes.byref(need)))
     d_rho = torch.empty_like(rho) if rho is not None else None
     work = _workspace(need.value, q)
     with _on(q):

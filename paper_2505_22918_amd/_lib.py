@@ -93,10 +93,11 @@ _SIGS = {
                                          c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p,
                                          c_void_p]),
     "rt_reshape_apply": (c_int32, [c_void_p, c_void_p, c_void_p, c_float, RtDims, c_void_p, c_void_p]),
+    "rt_index_transpose_size": (c_int32, [ctypes.POINTER(RtBsr), c_int32, ctypes.POINTER(c_int64)]),
     "rt_index_transpose": (c_int32, [ctypes.POINTER(RtBsr), c_int32, ctypes.POINTER(RtBsr), c_void_p]),
     "rt_attn_full_backward_workspace": (c_int32, [RtDims, ctypes.POINTER(c_int64)]),
     "rt_attn_full_backward": (c_int32, [c_void_p] * 7 + [RtDims] + [c_void_p] * 4 + [c_int64, c_void_p]),
-    "rt_attn_sparse_backward_workspace": (c_int32, [RtDims, ctypes.POINTER(RtBsr), ctypes.POINTER(c_int64)]),
+    "rt_attn_sparse_backward_workspace": (c_int32, [RtDims, ctypes.POINTER(RtBsr), c_int32, ctypes.POINTER(c_int64)]),
     "rt_attn_sparse_backward": (c_int32, [c_void_p] * 7 + [RtDims, ctypes.POINTER(RtBsr), ctypes.POINTER(RtBsr),
                                                           c_void_p, c_float] + [c_void_p] * 5 + [c_int64, c_void_p]),
     "rt_layer_norm": (c_int32, [c_void_p, Strides, c_void_p, c_void_p, RtNormDims, c_float, c_void_p, Strides,

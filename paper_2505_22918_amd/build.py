@@ -18,8 +18,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librettention.so")
-SOURCES = ["attn.hip", "attn_dense.hip", "elementwise.hip", "index.hip", "dynamic.hip", "attn_grad.hip", "norm.hip",
-           "api.cpp"]
+SOURCES = ["attn.hip", "attn_dense.hip", "elementwise.hip", "index.hip", "dynamic.hip", "norm.hip", "api.cpp"]
+GRAD_SOURCES = ["attn_grad.hip"]  # beside them: LDS DMAs of its own
 ARCH = "gfx950"
 
 
@@ -40,7 +40,7 @@ def command(out=LIB, extra=()):
         "-Wno-unused-command-line-argument",
         "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
         "-I", os.path.join(ROOT, "include"),
-        *[os.path.join(CSRC, s) for s in SOURCES],
+        *[os.path.join(CSRC, s) for s in SOURCES + GRAD_SOURCES],
         *extra,
         "-o", out,
     ]

@@ -601,7 +601,29 @@ rt_status check_transposed(const rt_bsr* t, const rt_bsr* m) {
     if (t->nnz < m->nnz)
         return fail(RT_ECAPACITY, "the transposed mask has room for %d entries, the mask has %d", t->nnz, m->nnz);
     RT_TRY(check_stat(t->row_ptr, "the transposed mask's row_ptr"));
-    RT_TRY(check_stat(t->col_idx, "the transposed mask's col_idx"));
+    RT_TRY(check_tensor(t->col_idx, "the transposed mask's col_idx"));
+    return RT_OK;
+}
+
+// How the lists of a transposed mask with room for `entries` are split over workgroups: after `seg` entries, four times
+// the mean list (and 32 at least), so that few are and none holds the others up; and what the plan and the parts
+// of split lists take at most.
+struct Plan {
+    int32_t seg, max_items, max_slots, max_splits;
+    int64_t first, values;  // the plan's place behind the entries, and the size of it all
+};
+
+rt_status plan_of(const rt_bsr* m, int32_t entries, Plan* out) {
+    const int64_t rows = (int64_t)(m->n_masks > 1 ? m->n_masks : 1) * m->n_qblk;
+    const int64_t seg = std::max<int64_t>(32, 4 * ceil_div(entries, std::max<int64_t>(rows, 1)));
+    const int64_t splits = m->n_qblk > seg ? entries / seg : 0;
+    if (rows + 2 * splits > INT32_MAX / 8) return fail(RT_EINVAL, "too many mask rows");
+    out->seg = (int32_t)seg;
+    out->max_items = (int32_t)(rows + splits);
+    out->max_slots = (int32_t)(2 * splits);
+    out->max_splits = (int32_t)splits;
+    out->first = ceil_div(entries, 4) * 4;
+    out->values = out->first + 4 + 4 * (rows + 2 * splits);
     return RT_OK;
 }
 
@@ -623,7 +645,11 @@ rt_status check_ranges(std::initializer_list<std::pair<range, const char*>> outs
     return RT_OK;
 }
 
-int64_t backward_workspace(const rt_dims& d) { return (int64_t)d.B * d.H * d.T * 8; }
+// Row values, and the parts of split lists.
+int64_t backward_workspace(const rt_dims& d, const rt_bsr* m, const Plan& p) {
+    const int64_t uses = m ? (int64_t)d.B * d.H / (m->n_masks > 1 ? m->n_masks : 1) : 0;
+    return ceil_div((int64_t)d.B * d.H * d.T * 8, 16) * 16 + (m ? uses * p.max_slots * 2 * m->block * d.D * 4 : 0);
+}
 
 // What the dense and the sparse gradient call check and set alike (rho and the mask aside).
 rt_status grad_args(const void* q, const void* k, const void* v, const void* o, const float* row_max,
@@ -769,6 +795,18 @@ int64_t norm_workspace(const rt_norm_dims& d) {
 
 }  // namespace
 
+rt_status rt_index_transpose_size(const rt_bsr* mask, int32_t entries, int64_t* values) {
+    if (!values) return fail(RT_EINVAL, "values is NULL");
+    if (!mask) return fail(RT_EINVAL, "mask is NULL");
+    RT_TRY(check_block(mask->block));
+    if (mask->n_qblk < 0 || mask->n_masks < 0 || entries < 0)
+        return fail(RT_EINVAL, "n_qblk=%d n_masks=%d entries=%d", mask->n_qblk, mask->n_masks, entries);
+    Plan p{};
+    RT_TRY(plan_of(mask, entries, &p));
+    *values = p.values;
+    return ok();
+}
+
 rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, void* stream) {
     if (!mask) return fail(RT_EINVAL, "mask is NULL");
     if (T < 0) return fail(RT_EINVAL, "T=%d", T);
@@ -777,9 +815,10 @@ rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, voi
     RT_TRY(check_bsr(mask, rt_dims{1, (int32_t)nm, T, 64}));
     if (mask->n_qblk == 0) return ok();
     RT_TRY(check_transposed(t, mask));
-    if (nm * mask->n_qblk > INT32_MAX) return fail(RT_EINVAL, "too many mask rows");
-    const int64_t np = mask_ptr_bytes(mask), nc = (int64_t)mask->nnz * 4, tc = (int64_t)t->nnz * 4;
-    RT_TRY(check_ranges({{{t->row_ptr, np}, "the transposed row_ptr"}, {{t->col_idx, tc}, "the transposed col_idx"}},
+    Plan p{};
+    RT_TRY(plan_of(mask, t->nnz, &p));
+    const int64_t np = mask_ptr_bytes(mask), nc = (int64_t)mask->nnz * 4;
+    RT_TRY(check_ranges({{{t->row_ptr, np}, "the transposed row_ptr"}, {{t->col_idx, p.values * 4}, "the transposed col_idx"}},
                         {{mask->row_ptr, np}, {mask->col_idx, nc}}));
     rt::TransposeArgs a{};
     a.row_ptr = mask->row_ptr;
@@ -790,6 +829,9 @@ rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, voi
     a.t_row_ptr = const_cast<int32_t*>(t->row_ptr);
     a.t_col_idx = const_cast<int32_t*>(t->col_idx);
     a.t_nnz = t->nnz;
+    a.plan = a.t_col_idx + p.first;
+    a.seg = p.seg;
+    a.max_items = p.max_items;
     return hip_status(rt::launch_index_transpose(a, static_cast<hipStream_t>(stream)), "index transpose launch");
 }
 
@@ -797,7 +839,7 @@ rt_status rt_attn_full_backward_workspace(rt_dims dims, int64_t* bytes) {
     if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
     bool empty = false;
     RT_TRY(check_dims(dims, &empty));
-    *bytes = backward_workspace(dims);
+    *bytes = backward_workspace(dims, nullptr, Plan{});
     return ok();
 }
 
@@ -808,7 +850,8 @@ rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, con
     RT_TRY(check_dims(dims, &empty));
     if (empty) return ok();
     RT_TRY(check_items(dims, 32));
-    const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D, need = backward_workspace(dims);
+    const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D;
+    const int64_t need = backward_workspace(dims, nullptr, Plan{});
     rt::GradArgs a{};
     RT_TRY(grad_args(q, k, v, o, row_max, row_sum, d_o, dims, dq, dk, dv, workspace, workspace_bytes, need, &a));
     RT_TRY(check_ranges({{{dq, nt}, "dq"}, {{dk, nt}, "dk"}, {{dv, nt}, "dv"}, {{workspace, need}, "workspace"}},
@@ -817,12 +860,16 @@ rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, con
                       "full attention gradient launch");
 }
 
-rt_status rt_attn_sparse_backward_workspace(rt_dims dims, const rt_bsr* mask, int64_t* bytes) {
+rt_status rt_attn_sparse_backward_workspace(rt_dims dims, const rt_bsr* mask, int32_t room, int64_t* bytes) {
     if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
     bool empty = false;
     RT_TRY(check_dims(dims, &empty));
     RT_TRY(check_bsr(mask, dims));
-    *bytes = backward_workspace(dims);
+    const int32_t entries = room > 0 ? room : mask->nnz;
+    if (entries < mask->nnz) return fail(RT_ECAPACITY, "room for %d entries, the mask has %d", entries, mask->nnz);
+    Plan p{};
+    RT_TRY(plan_of(mask, entries, &p));
+    *bytes = backward_workspace(dims, mask, p);
     return ok();
 }
 
@@ -840,24 +887,34 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     RT_TRY(check_items(dims, 32));
     if (rho) RT_TRY(check_stat(rho, "rho"));
     if (d_rho) RT_TRY(check_stat(d_rho, "d_rho"));
-    const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D, need = backward_workspace(dims);
+    const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D;
+    Plan p{};
+    RT_TRY(plan_of(mask, t->nnz, &p));
+    const int64_t need = backward_workspace(dims, mask, p), bh = (int64_t)dims.B * dims.H;
+    const int64_t uses = bh / (mask->n_masks > 1 ? mask->n_masks : 1);
+    if (uses * p.max_items + bh * mask->n_qblk + 16 > INT32_MAX || uses * p.max_splits > INT32_MAX)
+        return fail(RT_EINVAL, "too many key blocks");
     rt::GradArgs a{};
     RT_TRY(grad_args(q, k, v, o, row_max, row_sum, d_o, dims, dq, dk, dv, workspace, workspace_bytes, need, &a));
     const int64_t np = mask_ptr_bytes(mask), nc = (int64_t)mask->nnz * 4;
     RT_TRY(check_ranges({{{dq, nt}, "dq"}, {{dk, nt}, "dk"}, {{dv, nt}, "dv"}, {{d_rho, ns}, "d_rho"},
                          {{workspace, need}, "workspace"}},
                         {{q, nt}, {k, nt}, {v, nt}, {o, nt}, {d_o, nt}, {row_max, ns}, {row_sum, ns}, {rho, ns},
-                         {mask->row_ptr, np}, {mask->col_idx, nc}, {t->row_ptr, np}, {t->col_idx, (int64_t)t->nnz * 4}}));
+                         {mask->row_ptr, np}, {mask->col_idx, nc}, {t->row_ptr, np}, {t->col_idx, p.values * 4}}));
     a.rho = rho;
     a.rho_delta = rho_delta;
     a.d_rho = d_rho;
     a.row_ptr = mask->row_ptr;
     a.col_idx = mask->col_idx;
     a.nnz = mask->nnz;
-    a.t_row_ptr = t->row_ptr;
     a.t_col_idx = t->col_idx;
-    a.t_nnz = t->nnz;
+    a.plan = t->col_idx + p.first;
+    a.max_items = p.max_items;
+    a.max_slots = p.max_slots;
+    a.max_splits = p.max_splits;
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + ceil_div(bh * dims.T * 8, 16) * 16);
     a.n_masks = mask->n_masks > 1 ? mask->n_masks : 1;
+    a.n_blk = mask->n_qblk;
     a.block = mask->block;
     return hip_status(rt::launch_attention_backward(a, dims.D, static_cast<hipStream_t>(stream)),
                       "sparse attention gradient launch");

@@ -244,27 +244,61 @@ __global__ __launch_bounds__(64) void transpose_rows(TransposeArgs a) {
     if (!FILL && lane == 0) row[1] = at;
 }
 
-// counts in row_ptr[m][kb + 1] become absolute offsets; all -1 if they do not fit
+// One workgroup: counts in row_ptr[m][kb + 1] become absolute offsets, and the plan is written; offsets and the plan's
+// item count are -1 if the entries do not fit.
 __global__ __launch_bounds__(1024) void transpose_scan(TransposeArgs a) {
-    __shared__ int64_t part[1025];
+    __shared__ int64_t part[4][1024];  // entries, items, parts of split lists, split lists
     const int64_t rows = (int64_t)a.n_masks * a.n_blk, seg = (rows + 1023) / 1024;
     const int64_t i0 = threadIdx.x * seg, i1 = i0 + seg < rows ? i0 + seg : rows;
-    int64_t sum = 0;
-    for (int64_t i = i0; i < i1; ++i) sum += a.t_row_ptr[i + i / a.n_blk + 1];
-    part[threadIdx.x + 1] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        part[0] = 0;
-        for (int i = 1; i <= 1024; ++i) part[i] += part[i - 1];
+    auto pieces = [&](int c) { return c <= a.seg ? 1 : (c + a.seg - 1) / a.seg; };
+    int64_t sum[4] = {0, 0, 0, 0};
+    for (int64_t i = i0; i < i1; ++i) {
+        const int c = a.t_row_ptr[i + i / a.n_blk + 1], n = pieces(c);
+        sum[0] += c;
+        sum[1] += n;
+        sum[2] += n > 1 ? n : 0;
+        sum[3] += n > 1;
+    }
+    int64_t own[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        own[k] = sum[k];
+        part[k][threadIdx.x] = sum[k];
     }
     __syncthreads();
-    const bool fits = part[1024] <= a.t_nnz;
-    int64_t at = part[threadIdx.x];
+    for (int d = 1; d < 1024; d *= 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[k] = (int)threadIdx.x >= d ? part[k][threadIdx.x - d] : 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) part[k][threadIdx.x] += sum[k];
+        __syncthreads();
+    }
+    const bool fits = part[0][1023] <= a.t_nnz;
+    int64_t at[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) at[k] = part[k][threadIdx.x] - own[k];
+    if (threadIdx.x < 4) a.plan[threadIdx.x] = threadIdx.x == 3 ? 0 : (fits ? (int32_t)part[threadIdx.x + 1][1023] : (threadIdx.x == 0 ? -1 : 0));
     for (int64_t i = i0; i < i1; ++i) {
         const int64_t m = i / a.n_blk;
-        if (i == m * a.n_blk) a.t_row_ptr[i + m] = fits ? (int32_t)at : -1;
-        at += a.t_row_ptr[i + m + 1];
-        a.t_row_ptr[i + m + 1] = fits ? (int32_t)at : -1;
+        const int c = a.t_row_ptr[i + m + 1];
+        if (i == m * a.n_blk) a.t_row_ptr[i + m] = fits ? (int32_t)at[0] : -1;
+        a.t_row_ptr[i + m + 1] = fits ? (int32_t)(at[0] + c) : -1;
+        if (fits) {
+            const int n = pieces(c);
+            int4* item = reinterpret_cast<int4*>(a.plan + 4) + at[1];
+            for (int j = 0; j < n; ++j) {
+                const int first = j * a.seg, left = c - first;
+                item[j] = int4{(int)i, (int)at[0] + first, left < a.seg ? left : a.seg, n > 1 ? (int)at[2] + j : -1};
+            }
+            if (n > 1) {
+                reinterpret_cast<int4*>(a.plan + 4)[a.max_items + at[3]] = int4{(int)i, (int)at[2], n, 0};
+                at[2] += n;
+                ++at[3];
+            }
+            at[1] += n;
+        }
+        at[0] += c;
     }
 }
 

@@ -99,14 +99,20 @@ hipError_t dynamic_scratch(float** ptr);
 // The launchers below are declared weak so that a host-only build of api.cpp (the checks
 // under a sanitizer) can leave out those that it has no stand-in for.
 
-// Transpose of a block mask (index.hip): row kb of mask m lists the query blocks that keep kb.
+// Transpose of a block mask (index.hip): row kb of mask m lists the query blocks that keep kb.  The plan that follows
+// says which workgroup of the gradients' call walks what: lists of more than `seg` entries are split.
+//   plan[0 .. 2]  items, parts of split lists, split lists; items -1: the entries did not fit, no plan
+//   then max_items of {mask * n_blk + kb, first entry, entries, part or -1}
+//   then max_splits of {mask * n_blk + kb, first part, parts, 0}
 struct TransposeArgs {
     const int32_t* row_ptr;  // [n_masks][n_blk + 1]
     const int32_t* col_idx;
     int32_t nnz, n_blk, n_masks;
     int32_t* t_row_ptr;
     int32_t* t_col_idx;
-    int32_t t_nnz;           // room in t_col_idx
+    int32_t t_nnz;           // room for entries in t_col_idx
+    int32_t* plan;           // behind them
+    int32_t seg, max_items;
 };
 __attribute__((weak)) hipError_t launch_index_transpose(const TransposeArgs& a, hipStream_t stream);
 
@@ -126,12 +132,14 @@ struct GradArgs {
     uint16_t* dk;
     uint16_t* dv;
     float* row_log;     // workspace [B,H,T]: log2 of the denominator over the row's factor, in score units
-    float* row_delta;   // workspace [B,H,T]: dO . O
+    float* row_delta;   // workspace [B,H,T]: -dO . O
+    float* part;        // workspace: fp32 dK and dV [slot][2][block][D] of split lists, max_slots for each use of a mask
+    const int32_t* plan;  // of the transposed mask
+    int32_t max_items, max_slots, max_splits;
     const int32_t* row_ptr;  // null: dense
     const int32_t* col_idx;
-    const int32_t* t_row_ptr;
     const int32_t* t_col_idx;
-    int32_t nnz, t_nnz, n_masks, heads;
+    int32_t nnz, n_masks, heads;
     int32_t T, n_blk, block;
     int32_t n_bh;
     float scale_log2;   // log2(e) / sqrt(D)

@@ -118,6 +118,24 @@ def test_sparse(gpu, D, block, T, masks, ratio):
         assert (np.abs(to_np(out[3]) - ref) <= tol).all()
 
 
+@pytest.mark.parametrize("D", [64, 72])
+@pytest.mark.parametrize("block,T,masks", [(32, 2300, 1), (32, 1500, 2), (32, 1111, 4), (64, 2700, 1), (64, 2139, 2)])
+def test_lists_that_are_split(gpu, D, block, T, masks):
+    """A key block that every query block keeps: its list is walked in parts, which are joined."""
+    print(f"[sparse backward, split] T={T} D={D} block={block} masks={masks}", flush=True)
+    B, H = (1, 1) if masks == 1 else (2, 2)
+    n = -(-T // block)
+    rp, ci = _masks(n, masks, 3, T, column=n - 1)
+    mask = rt.BlockMask.from_csr(rp, ci, block, n_masks=masks)
+    plan = mask.transposed().col_idx[-(-len(ci) // 4) * 4:][:4].tolist()
+    assert plan[2] == masks and plan[0] == masks * n + plan[1] - masks  # one split list to a mask
+    dev, host = _inputs(B, H, T, D, T + D + block)
+    stats = rt.attn_sparse(*dev[:3], mask)
+    out = rt.attn_sparse_backward(*dev[:3], *stats, dev[3], mask)
+    rows = rp.reshape(masks, n + 1)
+    _compare(host, stats, out, lambda b, h: og.token_mask(rows[{1: 0, 2: h, 4: b * H + h}[masks]], ci, block, T))
+
+
 @pytest.mark.parametrize("block", [32, 64])
 def test_a_key_block_that_no_query_keeps_gets_zero(gpu, block):
     T = 5 * block - 7

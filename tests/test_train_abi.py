@@ -102,11 +102,16 @@ def test_sparse_gradient_refusals(lib):
 def test_workspace_sizes(lib):
     n = ctypes.c_int64(-1)
     assert lib.rt_attn_full_backward_workspace(_dims(), ctypes.byref(n)) == _lib.RT_OK and n.value >= 256 * 2 * 8
-    assert lib.rt_attn_sparse_backward_workspace(_dims(), ctypes.byref(_bsr()), ctypes.byref(n)) == _lib.RT_OK
+    assert lib.rt_attn_sparse_backward_workspace(_dims(), ctypes.byref(_bsr()), 0, ctypes.byref(n)) == _lib.RT_OK
     assert n.value >= 256 * 2 * 8
     assert lib.rt_attn_full_backward_workspace(_dims(D=80), ctypes.byref(n)) == _lib.RT_EUNSUPPORTED
     assert lib.rt_attn_full_backward_workspace(_dims(), None) == _lib.RT_EINVAL
-    assert lib.rt_attn_sparse_backward_workspace(_dims(), ctypes.byref(_bsr(n=3)), ctypes.byref(n)) == _lib.RT_EINVAL
+    assert lib.rt_attn_sparse_backward_workspace(_dims(), ctypes.byref(_bsr(n=3)), 0, ctypes.byref(n)) == _lib.RT_EINVAL
+    assert lib.rt_attn_sparse_backward_workspace(_dims(), ctypes.byref(_bsr()), 7, ctypes.byref(n)) == _lib.RT_ECAPACITY
+    assert lib.rt_index_transpose_size(ctypes.byref(_bsr()), 8, ctypes.byref(n)) == _lib.RT_OK and n.value >= 8 + 4 * 5
+    assert lib.rt_index_transpose_size(ctypes.byref(_bsr()), -1, ctypes.byref(n)) == _lib.RT_EINVAL
+    assert lib.rt_index_transpose_size(None, 8, ctypes.byref(n)) == _lib.RT_EINVAL
+    assert lib.rt_index_transpose_size(ctypes.byref(_bsr()), 8, None) == _lib.RT_EINVAL
 
 
 def test_transpose_refusals(lib):
