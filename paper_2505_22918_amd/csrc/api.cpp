@@ -609,7 +609,7 @@ rt_status check_transposed(const rt_bsr* t, const rt_bsr* m) {
 // the mean list (and 32 at least), so that few are and none holds the others up; and what the plan and the parts
 // of split lists take at most.
 struct Plan {
-    int32_t seg, max_items, max_slots, max_splits;
+    int32_t seg, max_more, max_slots, max_splits;
     int64_t first, values;  // the plan's place behind the entries, and the size of it all
 };
 
@@ -619,7 +619,7 @@ rt_status plan_of(const rt_bsr* m, int32_t entries, Plan* out) {
     const int64_t splits = m->n_qblk > seg ? entries / seg : 0;
     if (rows + 2 * splits > INT32_MAX / 8) return fail(RT_EINVAL, "too many mask rows");
     out->seg = (int32_t)seg;
-    out->max_items = (int32_t)(rows + splits);
+    out->max_more = (int32_t)splits;
     out->max_slots = (int32_t)(2 * splits);
     out->max_splits = (int32_t)splits;
     out->first = ceil_div(entries, 4) * 4;
@@ -645,10 +645,12 @@ rt_status check_ranges(std::initializer_list<std::pair<range, const char*>> outs
     return RT_OK;
 }
 
+int32_t whole64(int32_t T) { return (int32_t)ceil_div(T, 64) * 64; }
+
 // Row values, and the parts of split lists.
 int64_t backward_workspace(const rt_dims& d, const rt_bsr* m, const Plan& p) {
     const int64_t uses = m ? (int64_t)d.B * d.H / (m->n_masks > 1 ? m->n_masks : 1) : 0;
-    return ceil_div((int64_t)d.B * d.H * d.T * 8, 16) * 16 + (m ? uses * p.max_slots * 2 * m->block * d.D * 4 : 0);
+    return (int64_t)d.B * d.H * whole64(d.T) * 8 + (m ? uses * p.max_slots * 2 * m->block * d.D * 4 : 0);
 }
 
 // What the dense and the sparse gradient call check and set alike (rho and the mask aside).
@@ -676,8 +678,8 @@ rt_status grad_args(const void* q, const void* k, const void* v, const void* o, 
     a.dq = static_cast<uint16_t*>(dq);
     a.dk = static_cast<uint16_t*>(dk);
     a.dv = static_cast<uint16_t*>(dv);
-    a.row_log = static_cast<float*>(workspace);
-    a.row_delta = a.row_log + (size_t)d.B * d.H * d.T;
+    a.row_vals = static_cast<float*>(workspace);
+    a.T64 = whole64(d.T);
     a.T = d.T;
     a.heads = d.H;
     a.n_bh = d.B * d.H;
@@ -831,7 +833,7 @@ rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, voi
     a.t_nnz = t->nnz;
     a.plan = a.t_col_idx + p.first;
     a.seg = p.seg;
-    a.max_items = p.max_items;
+    a.max_more = p.max_more;
     return hip_status(rt::launch_index_transpose(a, static_cast<hipStream_t>(stream)), "index transpose launch");
 }
 
@@ -892,7 +894,7 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     RT_TRY(plan_of(mask, t->nnz, &p));
     const int64_t need = backward_workspace(dims, mask, p), bh = (int64_t)dims.B * dims.H;
     const int64_t uses = bh / (mask->n_masks > 1 ? mask->n_masks : 1);
-    if (uses * p.max_items + bh * mask->n_qblk + 16 > INT32_MAX || uses * p.max_splits > INT32_MAX)
+    if (uses * p.max_more + 2 * bh * mask->n_qblk + 32 > INT32_MAX)
         return fail(RT_EINVAL, "too many key blocks");
     rt::GradArgs a{};
     RT_TRY(grad_args(q, k, v, o, row_max, row_sum, d_o, dims, dq, dk, dv, workspace, workspace_bytes, need, &a));
@@ -909,10 +911,10 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     a.nnz = mask->nnz;
     a.t_col_idx = t->col_idx;
     a.plan = t->col_idx + p.first;
-    a.max_items = p.max_items;
+    a.max_more = p.max_more;
     a.max_slots = p.max_slots;
     a.max_splits = p.max_splits;
-    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + ceil_div(bh * dims.T * 8, 16) * 16);
+    a.part = a.row_vals + bh * 2 * a.T64;
     a.n_masks = mask->n_masks > 1 ? mask->n_masks : 1;
     a.n_blk = mask->n_qblk;
     a.block = mask->block;

@@ -27,12 +27,21 @@ __device__ __forceinline__ float dpp(float x) {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
 }
 
-// 8 lanes a row; of a 72-wide row the first takes the last 8 elements too
+// 8 lanes a row (of a 72-wide row the first takes the last 8 elements too); rows are counted with each head's padded to
+// whole 64, whose values are zeros
 template <int D>
 __global__ __launch_bounds__(256) void grad_rows(GradArgs a, int64_t rows) {
-    const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
     const int c = threadIdx.x & 7;
-    if (row >= rows) return;
+    if (i >= rows) return;
+    const int64_t bh = i / a.T64;
+    const int t = (int)(i - bh * a.T64);
+    float* vals = a.row_vals + bh * 2 * a.T64 + t;
+    if (t >= a.T) {
+        if (c == 0) vals[0] = vals[a.T64] = 0.f;
+        return;
+    }
+    const int64_t row = bh * a.T + t;
     float s = 0.f;
     auto add = [&](int ch) {
         const size_t at = (size_t)row * D + 8 * ch;
@@ -55,8 +64,8 @@ __global__ __launch_bounds__(256) void grad_rows(GradArgs a, int64_t rows) {
             log -= log2f(fminf(1.0f, r));  // a factor of 0: +inf, no probability
             if (a.d_rho) a.d_rho[row] = r <= 1.0f ? s : 0.f;
         }
-        a.row_log[row] = log;
-        a.row_delta[row] = -s;
+        vals[0] = log;
+        vals[a.T64] = -s;
     }
 }
 
@@ -69,25 +78,25 @@ __device__ __forceinline__ void dense_walk(const GradArgs& a, lds_u8* lds, int i
     const int T = a.T, n64 = (T + 63) >> 6, n_tile = (T + 32 * W - 1) / (32 * W);
     const int bh = item / n_tile;
     const int row0 = ((item - bh * n_tile) * W + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 32;
-    const size_t head_off = (size_t)bh * (size_t)T * D, stat_off = (size_t)bh * T;
+    const size_t head_off = (size_t)bh * (size_t)T * D;
+    const float* vals = a.row_vals + (size_t)bh * 2 * a.T64;
     R ring;
-    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, a.row_log + stat_off,
-              a.row_delta + stat_off, T);
+    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, vals, T, a.T64);
     ring.load(0, 0);
     ring.load(R::STAGE, 64);
-    GradTile<D, KV, R::ZERO, R::TENSOR, 64 * 4> t;
+    GradTile<D, KV, R::ZERO, R::TENSOR> t;
     t.init(lds, a.scale_log2);
-    t.load_own(a, head_off, stat_off, row0, T);
+    t.load_own(a, head_off, vals, row0, T);
     int st = 0;  // LDS offset of the stage in use
     for (int s = 0; s < n64; ++s) {
         ring.turn();
         ring.load(st == 0 ? 2 * R::STAGE : st - R::STAGE, (s + 2) * 64);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int cx = st + 32 * h * R::ROWB, stat = st + R::STAT + 128 * h;
-            t.scores(cx, stat);
+            const int cx = st + 32 * h * R::ROWB, logs = st + R::STAT + 128 * h;
+            t.scores(cx, logs + 256);
             if (!KV && s * 64 + 32 * h + 32 > T) t.mask(s * 64 + 32 * h, T);
-            t.soft(stat);
+            t.soft(logs);
             t.grads(cx);
         }
         st = st == 2 * R::STAGE ? 0 : st + R::STAGE;
@@ -113,47 +122,50 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) 
 
 // ---- sparse --------------------------------------------------------------------------------
 
+// Stages of 32 rows under way, and waves of a SIMD: three are worth more than a longer lead (CogVideoX 785 us with two
+// waves and four stages, 696 with two of each, 605 with three and two; 32-token blocks have LDS for two).
+constexpr int kStages = 2, kWaves = 3;
+
 // dK and dV (KV) or dQ of one block of a head against the `count` blocks listed from `list` on.  part: null, or where
 // the fp32 sums of a split list go.
 template <int D, bool KV, int W>
 __device__ __forceinline__ void sparse_walk(const GradArgs& a, lds_u8* lds, int bh, int blk, const int32_t* list, int count,
                                             float* part) {
-    constexpr int NS = W > 1 ? 4 : 2;
-    using R = GradRing<D, KV, W, 32, NS>;
+    using R = GradRing<D, KV, W, 32, kStages>;
     const int T = a.T, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = blk * (32 * W) + 32 * wave;
-    const size_t head_off = (size_t)bh * (size_t)T * D, stat_off = (size_t)bh * T;
+    const size_t head_off = (size_t)bh * (size_t)T * D;
+    const float* vals = a.row_vals + (size_t)bh * 2 * a.T64;
     const csr_ptr idx = (csr_ptr)list;
     const int n = count * W;
     R ring;
-    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, a.row_log + stat_off,
-              a.row_delta + stat_off, T);
+    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, vals, T, a.T64);
     auto row_at = [&](int s) {  // first row of stage s; none past the list or for an index out of range
         if (s >= n) return -1;
         const int c = idx[s / W];
         return c < 0 || c >= a.n_blk ? -1 : c * (32 * W) + 32 * (s % W);
     };
-    int rows[NS];  // of the stages under way; the last one is the next to be asked for
+    int rows[kStages];  // of the stages under way; the last one is the next to be asked for
 #pragma unroll
-    for (int i = 0; i < NS; ++i) rows[i] = row_at(i);
+    for (int i = 0; i < kStages; ++i) rows[i] = row_at(i);
 #pragma unroll
-    for (int i = 0; i < NS - 1; ++i) ring.load(i * R::STAGE, rows[i]);
-    GradTile<D, KV, R::ZERO, R::TENSOR, 32 * 4> t;
+    for (int i = 0; i < kStages - 1; ++i) ring.load(i * R::STAGE, rows[i]);
+    GradTile<D, KV, R::ZERO, R::TENSOR> t;
     t.init(lds, a.scale_log2);
-    t.load_own(a, head_off, stat_off, row0, T);
+    t.load_own(a, head_off, vals, row0, T);
     int st = 0;
     for (int s = 0; s < n; ++s) {
         ring.turn();
-        ring.load(st == 0 ? (NS - 1) * R::STAGE : st - R::STAGE, rows[NS - 1]);
+        ring.load(st == 0 ? (kStages - 1) * R::STAGE : st - R::STAGE, rows[kStages - 1]);
         const int at = rows[0];
 #pragma unroll
-        for (int i = 0; i < NS - 1; ++i) rows[i] = rows[i + 1];
-        rows[NS - 1] = row_at(s + NS);
-        t.scores(st, st + R::STAT);
+        for (int i = 0; i < kStages - 1; ++i) rows[i] = rows[i + 1];
+        rows[kStages - 1] = row_at(s + kStages);
+        t.scores(st, st + R::STAT + 128);
         if (!KV && (at < 0 || at + 32 > T)) t.mask(at < 0 ? T : at, T);
         t.soft(st + R::STAT);
         t.grads(st);
-        st = st == (NS - 1) * R::STAGE ? 0 : st + R::STAGE;
+        st = st == (kStages - 1) * R::STAGE ? 0 : st + R::STAGE;
     }
     wait_vm<0>();
     if (part) {
@@ -166,45 +178,50 @@ __device__ __forceinline__ void sparse_walk(const GradArgs& a, lds_u8* lds, int 
     t.store_all(a, head_off, row0, T);
 }
 
-// W: waves of a block (32 rows each)
+// W: waves of a block (32 rows each).  Workgroups: the further parts of split lists, dK and dV of every block, then dQ,
+// so that what takes longest begins first.  (A block's dK and dV next to its dQ, which reads the same rows, was no
+// faster at the CogVideoX shape and 20 % slower where the lists are random.)
 template <int D, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_sparse(GradArgs a, int kv_items,
-                                                                                               int kv_xcd, int q_items,
-                                                                                               int q_xcd) {
-    constexpr int NS = W > 1 ? 4 : 2;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[GradRing<D, true, W, 32, NS>::LDS];
-    if ((int)blockIdx.x < 8 * kv_xcd) {
-        // a list of a key block, or a part of one, by the transpose's plan
-        const int item = (blockIdx.x & 7) * kv_xcd + (blockIdx.x >> 3);
-        if (item >= kv_items) return;
-        const int rep = item / a.max_items, i = item - rep * a.max_items;
-        const csr_ptr plan = (csr_ptr)a.plan;
-        const int n = plan[0];
-        const bool bad = n < 0;  // the transpose did not fit its array
-        if (i >= (bad ? a.n_masks * a.n_blk : n)) return;
-        const csr_ptr p = plan + 4 + 4 * i;
-        const int row = bad ? i : p[0], m = row / a.n_blk, blk = row - m * a.n_blk;
-        const int bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
-        if (bad) {
-            const size_t head_off = (size_t)bh * (size_t)a.T * D;
-            const int r0 = blk * 32 * W, rows = a.T - r0 < 32 * W ? a.T - r0 : 32 * W;
-            for (int j = threadIdx.x; j < rows * D; j += 64 * W)
-                a.dk[head_off + (size_t)r0 * D + j] = a.dv[head_off + (size_t)r0 * D + j] = 0x7fc0;
-            return;
-        }
-        float* part = nullptr;
-        if (p[3] >= 0) part = a.part + ((size_t)rep * a.max_slots + p[3]) * (2 * 32 * W * D);
-        sparse_walk<D, true, W>(a, (lds_u8*)smem, bh, blk, a.t_col_idx + p[1], p[2], part);
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(kWaves, kWaves))) void grad_sparse(
+    GradArgs a, int more, int n_items, int per_xcd) {
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[GradRing<D, true, W, 32, kStages>::LDS];
+    lds_u8* const lds = (lds_u8*)smem;
+    const csr_ptr plan = (csr_ptr)a.plan;
+    int bh, blk, m, item;
+    if ((int)blockIdx.x < more) {
+        const int rep = blockIdx.x / a.max_more, i = blockIdx.x - rep * a.max_more;
+        if (i >= plan[0]) return;
+        item = a.n_masks * a.n_blk + i;
+        m = plan[4 + 4 * item] / a.n_blk;
+        blk = plan[4 + 4 * item] - m * a.n_blk;
+        bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
     } else {
-        const int g = blockIdx.x - 8 * kv_xcd, item = (g & 7) * q_xcd + (g >> 3);
-        if (item >= q_items) return;
-        const int bh = item / a.n_blk, blk = item - bh * a.n_blk;
-        const int m = a.n_masks == 1 ? 0 : (a.n_masks == a.heads ? bh % a.heads : bh);
+        const int g = blockIdx.x - more, half = g < 8 * per_xcd ? 0 : 8 * per_xcd;
+        const int i = ((g - half) & 7) * per_xcd + ((g - half) >> 3);
+        if (i >= n_items) return;
+        bh = i / a.n_blk;
+        blk = i - bh * a.n_blk;
+        m = a.n_masks == 1 ? 0 : (a.n_masks == a.heads ? bh % a.heads : bh);
+        item = half ? -1 : m * a.n_blk + blk;
+    }
+    if (item < 0) {
         const csr_ptr p = (csr_ptr)a.row_ptr + (size_t)m * (a.n_blk + 1) + blk;
         int b = p[0], e = p[1];
         b = b < 0 ? 0 : (b > a.nnz ? a.nnz : b);
         e = e < b ? b : (e > a.nnz ? a.nnz : e);
-        sparse_walk<D, false, W>(a, (lds_u8*)smem, bh, blk, a.col_idx + b, e - b, nullptr);
+        sparse_walk<D, false, W>(a, lds, bh, blk, a.col_idx + b, e - b, nullptr);
+    } else if (plan[0] >= 0) {
+        const csr_ptr p = plan + 4 + 4 * item;
+        float* part = nullptr;
+        if (p[3] >= 0) {
+            const int rep = a.n_masks == 1 ? bh : (a.n_masks == a.heads ? bh / a.heads : 0);
+            part = a.part + ((size_t)rep * a.max_slots + p[3]) * (2 * 32 * W * D);
+        }
+        sparse_walk<D, true, W>(a, lds, bh, blk, a.t_col_idx + p[1], p[2], part);
+    } else {  // the transpose did not fit its array
+        const size_t at = (size_t)bh * (size_t)a.T * D + (size_t)blk * 32 * W * D;
+        const int left = a.T - blk * 32 * W, size = (left < 32 * W ? left : 32 * W) * D;
+        for (int j = threadIdx.x; j < size; j += 64 * W) a.dk[at + j] = a.dv[at + j] = 0x7fc0;
     }
 }
 
@@ -214,7 +231,7 @@ __global__ __launch_bounds__(256) void grad_join(GradArgs a, int max_splits) {
     const int rep = blockIdx.x / max_splits, i = blockIdx.x - rep * max_splits;
     const csr_ptr plan = (csr_ptr)a.plan;
     if (i >= plan[2]) return;
-    const csr_ptr p = plan + 4 + 4 * (a.max_items + i);
+    const csr_ptr p = plan + 4 + 4 * (a.n_masks * a.n_blk + a.max_more + i);
     const int row = p[0], m = row / a.n_blk, blk = row - m * a.n_blk, n = p[2];
     const int bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
     constexpr int SIZE = 32 * W * D;
@@ -231,9 +248,8 @@ __global__ __launch_bounds__(256) void grad_join(GradArgs a, int max_splits) {
 
 template <int D, int W>
 hipError_t launch_sparse(const GradArgs& a, hipStream_t stream) {
-    const int rep = a.n_bh / a.n_masks;
-    const int kv = rep * a.max_items, kv_xcd = (kv + 7) / 8, q = a.n_bh * a.n_blk, q_xcd = (q + 7) / 8;
-    hipLaunchKernelGGL((grad_sparse<D, W>), dim3(8 * (kv_xcd + q_xcd)), dim3(64 * W), 0, stream, a, kv, kv_xcd, q, q_xcd);
+    const int rep = a.n_bh / a.n_masks, more = rep * a.max_more, n = a.n_bh * a.n_blk, per = (n + 7) / 8;
+    hipLaunchKernelGGL((grad_sparse<D, W>), dim3(more + 16 * per), dim3(64 * W), 0, stream, a, more, n, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.max_splits == 0) return e;
     hipLaunchKernelGGL((grad_join<D, W>), dim3(rep * a.max_splits, 2), dim3(256), 0, stream, a, a.max_splits);
@@ -242,7 +258,7 @@ hipError_t launch_sparse(const GradArgs& a, hipStream_t stream) {
 
 template <int D>
 hipError_t launch_d(const GradArgs& a, hipStream_t stream) {
-    const int64_t rows = (int64_t)a.n_bh * a.T;
+    const int64_t rows = (int64_t)a.n_bh * a.T64;
     hipLaunchKernelGGL((grad_rows<D>), dim3((uint32_t)((rows * 8 + 255) / 256)), dim3(256), 0, stream, a, rows);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

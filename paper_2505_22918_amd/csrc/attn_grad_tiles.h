@@ -44,9 +44,8 @@ __device__ __forceinline__ int swz(int r) {
     return Geo<D>::SWZ ? ((r & 2) << 1) | ((r & 8) >> 2) | ((r & 4) >> 2) : 0;
 }
 
-// ZERO: LDS offset of 16 zero bytes.  A chunk's 32 rows of Y lie CHUNK_Y behind those of X, its rows' deltas DELTA
-// behind their logs.
-template <int D, bool KV, int ZERO, int CHUNK_Y, int DELTA>
+// ZERO: LDS offset of 16 zero bytes.  A chunk's 32 rows of Y lie CHUNK_Y behind those of X.
+template <int D, bool KV, int ZERO, int CHUNK_Y>
 struct GradTile {
     using G = Geo<D>;
     static constexpr int ROWB = 2 * D;
@@ -85,7 +84,7 @@ struct GradTile {
     }
 
     // own rows row0 .. + 31 of a head (zeros past its end): lane holds row l32, dims 16 s + 8 hi ..
-    __device__ __forceinline__ void load_own(const GradArgs& a, size_t head_off, size_t stat_off, int row0, int T) {
+    __device__ __forceinline__ void load_own(const GradArgs& a, size_t head_off, const float* vals, int row0, int T) {
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
             const uint16_t* x = (KV ? (y ? a.v : a.k) : (y ? a.d_o : a.q)) + head_off;
@@ -99,8 +98,8 @@ struct GradTile {
         }
         if (!KV) {
             const int row = row0 + l32;
-            log = row < T ? a.row_log[stat_off + row] : INFINITY;
-            nd = row < T ? a.row_delta[stat_off + row] : 0.f;
+            log = row < T ? vals[row] : INFINITY;
+            nd = row < T ? vals[a.T64 + row] : 0.f;
         }
     }
 
@@ -143,12 +142,12 @@ struct GradTile {
             tacc[g][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, op(y, h), tacc[g][h], 0, 0, 0);
     }
 
-    // scores and dP of the chunk at LDS offset cx, its row values at stat
-    __device__ __forceinline__ void scores(int cx, int stat) {
+    // scores and dP of the chunk at LDS offset cx, its rows' -deltas at minus
+    __device__ __forceinline__ void scores(int cx, int minus) {
         if (KV) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f32x4 v = value_read(stat + DELTA, j);
+                const f32x4 v = value_read(minus, j);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) dp[4 * j + i] = v[i];
             }
@@ -166,12 +165,12 @@ struct GradTile {
             dp = mma(row_tail(cx + CHUNK_Y), own_tail[1], dp);
         }
     }
-    // P and dS of it
-    __device__ __forceinline__ void soft(int stat) {
+    // P and dS of it, its rows' logs at logs
+    __device__ __forceinline__ void soft(int logs) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             f32x4 v = {log, log, log, log};
-            if (KV) v = value_read(stat, j);
+            if (KV) v = value_read(logs, j);
 #pragma unroll
             for (int i = 0; i < 4; i += 2) {
                 const int x = 4 * j + i;
@@ -252,48 +251,39 @@ struct GradTile {
     }
 };
 
-// 4 bytes per lane into LDS at m0 + 4 * lane, see dma16
-__device__ __forceinline__ void dma4(uint32_t lds_addr, int voff, i32x4 rsrc) {
-    asm volatile(
-        "s_mov_b32 m0, %0\n\t"
-        "s_nop 0\n\t"
-        "buffer_load_dword %1, %2, 0 offen lds"
-        :
-        : "s"(lds_addr), "v"(voff), "s"(rsrc)
-        : "memory");
-}
-
-// The ring of NS stages of BS rows of X and Y (and, KV, of their logs and deltas) that W waves fill and read: stage
-// s + NS - 1 is asked for when all waves are through s - 1, whose place it takes.  The first half of the waves loads X and
-// logs, the other half Y and deltas (a lone wave all).  Rows past the head's end read as zeros.
+// The ring of NS stages of BS rows of X and Y (and, KV, of their logs and -deltas) that W waves fill and read: stage
+// s + NS - 1 is asked for when all waves are through s - 1, whose place it takes.  The first half of the waves loads X,
+// the other half Y (a lone wave both), the first wave the row values.  Rows past the head's end read as zeros.
 template <int D, bool KV, int W, int BS, int NS>
 struct GradRing {
-    static constexpr int ROWB = 2 * D, TENSOR = BS * ROWB, STAT = 2 * TENSOR, STAGE = STAT + 2 * BS * 4;
+    static constexpr int ROWB = 2 * D, TENSOR = BS * ROWB, STAT = 2 * TENSOR, STAGE = STAT + BS * 8;
     static constexpr int ZERO = NS * STAGE, LDS = ZERO + 64;
     static constexpr int WT = W > 1 ? W / 2 : 1;                 // waves of a tensor
     static constexpr int SL = BS * Geo<D>::SLOTS;                // its 16-byte slots
     static constexpr int FULL = SL / (64 * WT);                  // whole loads of a wave
     static constexpr int REST = (SL - FULL * 64 * WT) / WT;      // lanes of one more
-    static constexpr int LOADS = (W > 1 ? 1 : 2) * (FULL + (REST ? 1 : 0) + (KV ? 1 : 0));
-    static_assert(FULL * 64 * WT + REST * WT == SL && BS % WT == 0 && (WT == 1 || WT % 2 == 0), "even shares");
+    static constexpr int LOADS = (W > 1 ? 1 : 2) * (FULL + (REST ? 1 : 0));  // (and one of the row values)
+    static_assert(FULL * 64 * WT + REST * WT == SL && (WT == 1 || WT % 2 == 0), "even shares");
 
     uint32_t lds0;
-    int lane, wt, first;
+    int lane, w, wt, first;
     int from[2];  // a lane's source offset in an even and in an odd kilobyte of a stage
-    i32x4 rs[2], st[2];
+    int from_st;
+    i32x4 rs[2], st;
 
-    __device__ __forceinline__ void init(lds_u8* lds, const uint16_t* x, const uint16_t* y, const float* log,
-                                         const float* delta, int T) {
+    __device__ __forceinline__ void init(lds_u8* lds, const uint16_t* x, const uint16_t* y, const float* vals,
+                                         int T, int T64) {
         lds0 = (uint32_t)(uintptr_t)lds;
         lane = threadIdx.x & 63;
-        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         first = W > 1 ? w / WT : 0;
         wt = W > 1 ? w % WT : 0;
         rs[0] = buffer_rsrc(x, T * ROWB);
         rs[1] = buffer_rsrc(y, T * ROWB);
+        // lanes of the first half of BS values take logs, the others -deltas
         if (KV) {
-            st[0] = buffer_rsrc(log, T * 4);
-            st[1] = buffer_rsrc(delta, T * 4);
+            st = buffer_rsrc(vals, T64 * 8);
+            from_st = lane < BS / 4 ? lane * 16 : T64 * 4 + (lane - BS / 4) * 16;
         }
 #pragma unroll
         for (int p = 0; p < 2; ++p)
@@ -317,16 +307,16 @@ struct GradRing {
                 const int b = FULL * WT * 1024 + wt * REST * 16;
                 if (lane < REST) dma16(__builtin_amdgcn_readfirstlane(dst + b), from[0] + at + b, r);
             }
-            if (KV) {
-                const int b = wt * (BS / WT) * 4;
-                if (lane < BS / WT)
-                    dma4(__builtin_amdgcn_readfirstlane(lds0 + to + STAT + y * BS * 4 + b), lane * 4 + at4 + b, y ? st[1] : st[0]);
-            }
         }
+        if (KV && w == 0 && lane < BS / 2)
+            dma16(__builtin_amdgcn_readfirstlane(lds0 + to + STAT), from_st + at4, st);
     }
     // the oldest of NS - 1 stages asked for has landed, and every wave is through the stage before it
     __device__ __forceinline__ void turn() {
-        wait_vm<(NS - 2) * LOADS>();
+        if (KV && w == 0)
+            wait_vm<(NS - 2) * (LOADS + 1)>();
+        else
+            wait_vm<(NS - 2) * LOADS>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (W > 1) __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");

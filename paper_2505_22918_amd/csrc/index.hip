@@ -247,7 +247,7 @@ __global__ __launch_bounds__(64) void transpose_rows(TransposeArgs a) {
 // One workgroup: counts in row_ptr[m][kb + 1] become absolute offsets, and the plan is written; offsets and the plan's
 // item count are -1 if the entries do not fit.
 __global__ __launch_bounds__(1024) void transpose_scan(TransposeArgs a) {
-    __shared__ int64_t part[4][1024];  // entries, items, parts of split lists, split lists
+    __shared__ int64_t part[4][1024];  // entries, parts past a list's first, parts of split lists, split lists
     const int64_t rows = (int64_t)a.n_masks * a.n_blk, seg = (rows + 1023) / 1024;
     const int64_t i0 = threadIdx.x * seg, i1 = i0 + seg < rows ? i0 + seg : rows;
     auto pieces = [&](int c) { return c <= a.seg ? 1 : (c + a.seg - 1) / a.seg; };
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(1024) void transpose_scan(TransposeArgs a) {
     for (int64_t i = i0; i < i1; ++i) {
         const int c = a.t_row_ptr[i + i / a.n_blk + 1], n = pieces(c);
         sum[0] += c;
-        sum[1] += n;
+        sum[1] += n - 1;
         sum[2] += n > 1 ? n : 0;
         sum[3] += n > 1;
     }
@@ -286,17 +286,16 @@ __global__ __launch_bounds__(1024) void transpose_scan(TransposeArgs a) {
         a.t_row_ptr[i + m + 1] = fits ? (int32_t)(at[0] + c) : -1;
         if (fits) {
             const int n = pieces(c);
-            int4* item = reinterpret_cast<int4*>(a.plan + 4) + at[1];
+            int4* item = reinterpret_cast<int4*>(a.plan + 4);
             for (int j = 0; j < n; ++j) {
                 const int first = j * a.seg, left = c - first;
-                item[j] = int4{(int)i, (int)at[0] + first, left < a.seg ? left : a.seg, n > 1 ? (int)at[2] + j : -1};
+                item[j ? rows + at[1]++ : i] =
+                    int4{(int)i, (int)at[0] + first, left < a.seg ? left : a.seg, n > 1 ? (int)at[2] + j : -1};
             }
             if (n > 1) {
-                reinterpret_cast<int4*>(a.plan + 4)[a.max_items + at[3]] = int4{(int)i, (int)at[2], n, 0};
+                item[rows + a.max_more + at[3]++] = int4{(int)i, (int)at[2], n, 0};
                 at[2] += n;
-                ++at[3];
             }
-            at[1] += n;
         }
         at[0] += c;
     }

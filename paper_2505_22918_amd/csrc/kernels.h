@@ -101,8 +101,9 @@ hipError_t dynamic_scratch(float** ptr);
 
 // Transpose of a block mask (index.hip): row kb of mask m lists the query blocks that keep kb.  The plan that follows
 // says which workgroup of the gradients' call walks what: lists of more than `seg` entries are split.
-//   plan[0 .. 2]  items, parts of split lists, split lists; items -1: the entries did not fit, no plan
-//   then max_items of {mask * n_blk + kb, first entry, entries, part or -1}
+//   plan[0 .. 2]  further parts, parts of split lists, split lists; plan[0] -1: the entries did not fit, no plan
+//   then {mask * n_blk + kb, first entry, entries, part or -1} of every row, the first part of a split one,
+//   then max_more of the like for further parts,
 //   then max_splits of {mask * n_blk + kb, first part, parts, 0}
 struct TransposeArgs {
     const int32_t* row_ptr;  // [n_masks][n_blk + 1]
@@ -112,7 +113,7 @@ struct TransposeArgs {
     int32_t* t_col_idx;
     int32_t t_nnz;           // room for entries in t_col_idx
     int32_t* plan;           // behind them
-    int32_t seg, max_items;
+    int32_t seg, max_more;
 };
 __attribute__((weak)) hipError_t launch_index_transpose(const TransposeArgs& a, hipStream_t stream);
 
@@ -131,11 +132,11 @@ struct GradArgs {
     uint16_t* dq;
     uint16_t* dk;
     uint16_t* dv;
-    float* row_log;     // workspace [B,H,T]: log2 of the denominator over the row's factor, in score units
-    float* row_delta;   // workspace [B,H,T]: -dO . O
+    float* row_vals;    // workspace [B,H][2][T64]: log2 of the denominator over the row's factor, and -dO . O
+    int32_t T64;        // T in whole 64
     float* part;        // workspace: fp32 dK and dV [slot][2][block][D] of split lists, max_slots for each use of a mask
     const int32_t* plan;  // of the transposed mask
-    int32_t max_items, max_slots, max_splits;
+    int32_t max_more, max_slots, max_splits;
     const int32_t* row_ptr;  // null: dense
     const int32_t* col_idx;
     const int32_t* t_col_idx;

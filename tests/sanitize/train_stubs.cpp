@@ -19,21 +19,21 @@ namespace rt {
 hipError_t launch_index_transpose(const TransposeArgs& a, hipStream_t) {
     EXPECT(a.row_ptr && a.col_idx && a.t_row_ptr && a.t_col_idx);
     EXPECT(a.n_blk > 0 && a.n_masks > 0 && a.nnz > 0 && a.t_nnz >= a.nnz);
-    EXPECT(a.plan >= a.t_col_idx + a.t_nnz && a.seg >= 32 && a.max_items >= a.n_blk * a.n_masks);
+    EXPECT(a.plan >= a.t_col_idx + a.t_nnz && a.seg >= 32 && a.max_more >= 0);
     return hipSuccess;
 }
 
 hipError_t launch_attention_backward(const GradArgs& a, int D, hipStream_t) {
     EXPECT(D == 64 || D == 72);
     EXPECT(a.q && a.k && a.v && a.o && a.d_o && a.row_max && a.row_sum && a.dq && a.dk && a.dv);
-    EXPECT(a.row_log && a.row_delta == a.row_log + (size_t)a.n_bh * a.T);
+    EXPECT(a.row_vals && a.T64 >= a.T && a.T64 < a.T + 64 && a.T64 % 64 == 0);
     EXPECT(a.T > 0 && a.n_bh > 0 && (long long)a.T * D * 2 <= (1LL << 30));
     EXPECT(!a.d_rho || a.rho);
     if (a.row_ptr) {
         EXPECT(a.col_idx && a.t_col_idx && a.plan > a.t_col_idx && a.nnz > 0);
         EXPECT(a.n_blk == (a.T + a.block - 1) / a.block && a.n_bh % a.n_masks == 0);
-        EXPECT(a.max_items >= a.n_blk * a.n_masks && a.max_slots == 2 * a.max_splits);
-        EXPECT((char*)a.part >= (char*)(a.row_delta + (size_t)a.n_bh * a.T) && ((uintptr_t)a.part & 15) == 0);
+        EXPECT(a.max_more == a.max_splits && a.max_slots == 2 * a.max_splits);
+        EXPECT((char*)a.part >= (char*)(a.row_vals + 2 * (size_t)a.n_bh * a.T64) && ((uintptr_t)a.part & 15) == 0);
         EXPECT((a.block == 32 || a.block == 64) && a.n_masks >= 1);
     }
     return hipSuccess;

@@ -128,7 +128,7 @@ def test_lists_that_are_split(gpu, D, block, T, masks):
     rp, ci = _masks(n, masks, 3, T, column=n - 1)
     mask = rt.BlockMask.from_csr(rp, ci, block, n_masks=masks)
     plan = mask.transposed().col_idx[-(-len(ci) // 4) * 4:][:4].tolist()
-    assert plan[2] == masks and plan[0] == masks * n + plan[1] - masks  # one split list to a mask
+    assert plan[2] == masks and plan[0] == plan[1] - masks > 0  # one split list to a mask
     dev, host = _inputs(B, H, T, D, T + D + block)
     stats = rt.attn_sparse(*dev[:3], mask)
     out = rt.attn_sparse_backward(*dev[:3], *stats, dev[3], mask)
