@@ -24,6 +24,7 @@ library (the binding only marshals pointers and sizes).
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 
 from . import _lib
@@ -227,14 +228,14 @@ class BlockMask:
         it is built anew as part of the graph and not kept.  n_masks > 1: masks that share entries of col_idx
         (from_csr allows for them) do not fit and make the gradients dk and dv NaN."""
         torch = _torch()
+        kept = self.__dict__.get("_t")
+        if kept is not None and kept[1] is None:  # known to be complete
+            return kept[0]
         with _on(self.row_ptr):
             raw = _stream(self.row_ptr)
             capturing = torch.cuda.is_current_stream_capturing()
-            kept = self.__dict__.get("_t")
             if kept is not None:
                 t, done, built_on = kept
-                if done is None:
-                    return t
                 if not capturing:
                     if done.query():
                         self.__dict__["_t"] = (t, None, None)
@@ -530,6 +531,21 @@ def _workspace(nbytes, like):
     return _torch().empty(max(int(nbytes) // 4, 4), dtype=_torch().float32, device=like.device)
 
 
+@functools.lru_cache(maxsize=1024)
+def _backward_bytes(shape, mask):
+    """Workspace of the gradient calls for q's shape and a mask's (block, n_qblk, nnz, n_masks, room) or None."""
+    lib, need, dims = _lib.load(), ctypes.c_int64(0), _lib.RtDims(*shape)
+    if mask is None:
+        _lib.check("rt_attn_full_backward_workspace", lib.rt_attn_full_backward_workspace(dims, ctypes.byref(need)))
+    else:
+        block, n_qblk, nnz, n_masks, room = mask
+        at = ctypes.cast(ctypes.byref(need), ctypes.c_void_p).value  # any address: the arrays are not read
+        bsr = _lib.RtBsr(at, at, block, n_qblk, nnz, n_masks)
+        _lib.check("rt_attn_sparse_backward_workspace",
+                   lib.rt_attn_sparse_backward_workspace(dims, ctypes.byref(bsr), room, ctypes.byref(need)))
+    return need.value
+
+
 def attn_full_backward(q, k, v, o, row_max, row_sum, d_o, out=None):
     """Gradients (dq, dk, dv) of dense attention (Eq.1) for the gradient d_o of its output: o, row_max and
     row_sum are attn_full's for these q, k, v.  out: three tensors to write instead of new ones."""
@@ -537,13 +553,12 @@ def attn_full_backward(q, k, v, o, row_max, row_sum, d_o, out=None):
     dims = _check_qkv(q, k, v)
     _grad_inputs(q, o, row_max, row_sum, d_o)
     dq, dk, dv = _grads(out, q)
-    need = ctypes.c_int64(0)
-    _lib.check("rt_attn_full_backward_workspace", lib.rt_attn_full_backward_workspace(dims, ctypes.byref(need)))
-    work = _workspace(need.value, q)
+    need = _backward_bytes(tuple(q.shape), None)
+    work = _workspace(need, q)
     with _on(q):
         _lib.check("rt_attn_full_backward",
                    lib.rt_attn_full_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(row_max), _ptr(row_sum),
-                                             _ptr(d_o), dims, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(work), need.value,
+                                             _ptr(d_o), dims, _ptr(dq), _ptr(dk), _ptr(dv), _ptr(work), need,
                                              _stream(q)))
     return dq, dk, dv
 
@@ -564,55 +579,79 @@ def attn_sparse_backward(q, k, v, o, row_max, row_sum, d_o, mask: BlockMask, rho
     if q.numel() == 0:
         return (dq, dk, dv) if rho is None else (dq, dk, dv, torch.empty_like(rho))
     t = mask.transposed()
-    bsr, need = mask.c_struct(), ctypes.c_int64(0)
-    _lib.check("rt_attn_sparse_backward_workspace",
-               lib.rt_attn_sparse_backward_workspace(dims, ctypes.byref(bsr), t.nnz, ctypes.byref(need)))
+    bsr = mask.c_struct()
+    need = _backward_bytes(tuple(q.shape), (mask.block, mask.n_qblk, mask.nnz, mask.n_masks, t.nnz))
     d_rho = torch.empty_like(rho) if rho is not None else None
-    work = _workspace(need.value, q)
+    work = _workspace(need, q)
     with _on(q):
         _lib.check("rt_attn_sparse_backward",
                    lib.rt_attn_sparse_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(row_max), _ptr(row_sum),
                                                _ptr(d_o), dims, ctypes.byref(bsr), ctypes.byref(t.c_struct()),
                                                _ptr(rho), float(rho_delta), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_rho),
-                                               _ptr(work), need.value, _stream(q)))
+                                               _ptr(work), need, _stream(q)))
     return (dq, dk, dv) if rho is None else (dq, dk, dv, d_rho)
 
 
 _NORM_TYPES = None
 
 
-def _norm_rows(x, name, like=None):
-    """x as rows of its last dimension: (sizes, strides) of three leading indices."""
+def _norm_types():
     global _NORM_TYPES
-    torch = _torch()
     if _NORM_TYPES is None:
+        torch = _torch()
         _NORM_TYPES = {torch.bfloat16: _lib.RT_BF16, torch.float16: _lib.RT_F16, torch.float32: _lib.RT_F32}
-    _on_device(x, name, like.device if like is not None else None)
-    if x.dtype not in _NORM_TYPES or not 2 <= x.dim() <= 4 or (x.shape[-1] > 1 and x.stride(-1) != 1):
+    return _NORM_TYPES
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_strides(shape, stride, dtype, name):
+    """The row strides of a tensor of this layout, for three leading indices."""
+    if dtype not in _norm_types() or not 2 <= len(shape) <= 4 or (shape[-1] > 1 and stride[-1] != 1):
         raise ValueError(f"{name} must be a bf16, fp16 or fp32 tensor of 2 to 4 dimensions, its last one contiguous")
-    if like is not None and (x.dtype is not like.dtype or x.shape != like.shape):
-        raise ValueError(f"{name} must have the type and shape of x")
-    shape, stride = tuple(x.shape[:-1]), x.stride()[:-1]
     # leading indices first: the weight sets go by the first dimension of x
-    pad = 3 - len(shape)
-    return shape[:1] + (1,) * pad + shape[1:], _lib.Strides(*(stride[:1] + (0,) * pad + stride[1:]))
+    pad = 4 - len(shape)
+    return _lib.Strides(*(stride[:1] + (0,) * pad + stride[1:-1]))
 
 
-def _norm_dims(x, sizes, weight, bias):
+@functools.lru_cache(maxsize=1024)
+def _norm_dims(shape, dtype, weight, bias):
+    """The rt_norm_dims of rows `shape` with a weight and a bias of these (shape, type) or None, and the
+    workspace of their gradient."""
     torch = _torch()
     wt, sets = torch.float32, 1
     for name, t in (("weight", weight), ("bias", bias)):
         if t is None:
             continue
-        _on_device(t, name, x.device)
-        if t.dtype not in (torch.float32, x.dtype) or not t.is_contiguous():
+        if t[1] not in (torch.float32, dtype):
             raise ValueError(f"{name} must be a contiguous fp32 tensor, or one of x's type")
-        if tuple(t.shape) not in ((x.shape[-1],), (x.shape[0], x.shape[-1])):
-            raise ValueError(f"{name} must have the shape [{x.shape[-1]}] or [{x.shape[0]}, {x.shape[-1]}]")
-        if t is bias and weight is not None and (t.dtype is not weight.dtype or t.shape != weight.shape):
-            raise ValueError("weight and bias must share type and shape")
-        wt, sets = t.dtype, 1 if t.dim() == 1 else x.shape[0]
-    return _lib.RtNormDims(*sizes, x.shape[-1], _NORM_TYPES[x.dtype], _NORM_TYPES[wt], sets)
+        if t[0] not in (shape[-1:], (shape[0], shape[-1])):
+            raise ValueError(f"{name} must have the shape [{shape[-1]}] or [{shape[0]}, {shape[-1]}]")
+        wt, sets = t[1], 1 if len(t[0]) == 1 else shape[0]
+    if weight is not None and bias is not None and weight != bias:
+        raise ValueError("weight and bias must share type and shape")
+    sizes = shape[:1] + (1,) * (4 - len(shape)) + shape[1:-1]
+    dims = _lib.RtNormDims(*sizes, shape[-1], _norm_types()[dtype], _norm_types()[wt], sets)
+    need = ctypes.c_int64(0)
+    _lib.check("rt_layer_norm_backward_workspace",
+               _lib.load().rt_layer_norm_backward_workspace(dims, ctypes.byref(need)))
+    return dims, need.value
+
+
+def _norm_like(t, name, x):
+    """Row strides of t, a tensor of x's shape, type and device."""
+    _on_device(t, name, x.device)
+    if t.dtype is not x.dtype or t.shape != x.shape:
+        raise ValueError(f"{name} must have the type and shape of x")
+    return _norm_strides(tuple(t.shape), t.stride(), t.dtype, name)
+
+
+def _norm_weight(t, name, x):
+    if t is None:
+        return None
+    if not (t.is_cuda and t.get_device() == x.get_device() and t.is_contiguous()):
+        _on_device(t, name, x.device)
+        raise ValueError(f"{name} must be contiguous")
+    return tuple(t.shape), t.dtype
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None):
@@ -623,13 +662,19 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None):
     contiguous tensor or `out` (any row strides); with stats (y, mean, rstd), fp32 of x.shape[:-1]."""
     torch = _torch()
     lib = _lib.load()
-    sizes, xs = _norm_rows(x, "x")
-    dims = _norm_dims(x, sizes, weight, bias)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    _, ys = _norm_rows(y, "out", x)
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        _on_device(x, "x", None)
+    shape = tuple(x.shape)
+    xs = _norm_strides(shape, x.stride(), x.dtype, "x")
+    dims, _ = _norm_dims(shape, x.dtype, _norm_weight(weight, "weight", x), _norm_weight(bias, "bias", x))
+    if out is None:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        ys = _norm_strides(shape, y.stride(), x.dtype, "out")
+    else:
+        y, ys = out, _norm_like(out, "out", x)
     mean = rstd = None
     if stats:
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        mean = torch.empty(shape[:-1], dtype=torch.float32, device=x.device)
         rstd = torch.empty_like(mean)
     with _on(x):
         _lib.check("rt_layer_norm", lib.rt_layer_norm(_ptr(x), xs, _ptr(weight), _ptr(bias), dims, float(eps), _ptr(y),
@@ -644,24 +689,29 @@ def layer_norm_backward(d_y, x, mean, rstd, weight=None, bias=True, out=None):
     leaves d_bias out."""
     torch = _torch()
     lib = _lib.load()
-    sizes, xs = _norm_rows(x, "x")
-    _, dys = _norm_rows(d_y, "d_y", x)
-    dims = _norm_dims(x, sizes, weight, None)
-    _stat(mean, x.shape[:-1], "mean", x.device)
-    _stat(rstd, x.shape[:-1], "rstd", x.device)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    _, dxs = _norm_rows(dx, "out", x)
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        _on_device(x, "x", None)
+    shape = tuple(x.shape)
+    xs = _norm_strides(shape, x.stride(), x.dtype, "x")
+    dys = _norm_like(d_y, "d_y", x)
+    dims, need = _norm_dims(shape, x.dtype, _norm_weight(weight, "weight", x), None)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if not _same(t, torch.float32, shape[:-1], x):
+            _stat(t, shape[:-1], name, x.device)
+    if out is None:
+        dx = torch.empty(shape, dtype=x.dtype, device=x.device)
+        dxs = _norm_strides(shape, dx.stride(), x.dtype, "out")
+    else:
+        dx, dxs = out, _norm_like(out, "out", x)
     d_weight = d_bias = None
     if weight is not None:
         d_weight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
         d_bias = torch.empty_like(d_weight) if bias else None
-    need = ctypes.c_int64(0)
-    _lib.check("rt_layer_norm_backward_workspace", lib.rt_layer_norm_backward_workspace(dims, ctypes.byref(need)))
-    work = _workspace(need.value, x)
+    work = _workspace(need, x)
     with _on(x):
         _lib.check("rt_layer_norm_backward",
                    lib.rt_layer_norm_backward(_ptr(d_y), dys, _ptr(x), xs, _ptr(mean), _ptr(rstd), _ptr(weight), dims,
-                                              _ptr(dx), dxs, _ptr(d_weight), _ptr(d_bias), _ptr(work), need.value,
+                                              _ptr(dx), dxs, _ptr(d_weight), _ptr(d_bias), _ptr(work), need,
                                               _stream(x)))
     return dx, d_weight, d_bias
 
