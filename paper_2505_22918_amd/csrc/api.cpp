@@ -609,7 +609,7 @@ rt_status check_transposed(const rt_bsr* t, const rt_bsr* m) {
 // the mean list (and 32 at least), so that few are and none holds the others up; and what the plan and the parts
 // of split lists take at most.
 struct Plan {
-    int32_t seg, max_more, max_slots, max_splits;
+    int32_t seg, max_more, max_slots;
     int64_t first, values;  // the plan's place behind the entries, and the size of it all
 };
 
@@ -621,9 +621,8 @@ rt_status plan_of(const rt_bsr* m, int32_t entries, Plan* out) {
     out->seg = (int32_t)seg;
     out->max_more = (int32_t)splits;
     out->max_slots = (int32_t)(2 * splits);
-    out->max_splits = (int32_t)splits;
     out->first = ceil_div(entries, 4) * 4;
-    out->values = out->first + 4 + 4 * (rows + 2 * splits);
+    out->values = out->first + 4 * (rows + 2 * splits);
     return RT_OK;
 }
 
@@ -915,7 +914,6 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     a.plan = t->col_idx + p.first;
     a.max_more = p.max_more;
     a.max_slots = p.max_slots;
-    a.max_splits = p.max_splits;
     a.part = a.row_vals + bh * 2 * a.T64;
     a.n_masks = mask->n_masks > 1 ? mask->n_masks : 1;
     a.n_blk = mask->n_qblk;

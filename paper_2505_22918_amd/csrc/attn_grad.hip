@@ -190,10 +190,11 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(kWaves, 
     int bh, blk, m, item;
     if ((int)blockIdx.x < more) {
         const int rep = blockIdx.x / a.max_more, i = blockIdx.x - rep * a.max_more;
-        if (i >= plan[0]) return;
         item = a.n_masks * a.n_blk + i;
-        m = plan[4 + 4 * item] / a.n_blk;
-        blk = plan[4 + 4 * item] - m * a.n_blk;
+        const int row = plan[4 * item];
+        if (row < 0) return;
+        m = row / a.n_blk;
+        blk = row - m * a.n_blk;
         bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
     } else {
         const int g = blockIdx.x - more, half = g < 8 * per_xcd ? 0 : 8 * per_xcd;
@@ -210,8 +211,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(kWaves, 
         b = b < 0 ? 0 : (b > a.nnz ? a.nnz : b);
         e = e < b ? b : (e > a.nnz ? a.nnz : e);
         sparse_walk<D, false, W>(a, lds, bh, blk, a.col_idx + b, e - b, nullptr);
-    } else if (plan[0] >= 0) {
-        const csr_ptr p = plan + 4 + 4 * item;
+    } else if (plan[4 * item + 1] >= 0) {
+        const csr_ptr p = plan + 4 * item;
         float* part = nullptr;
         if (p[3] >= 0) {
             const int rep = a.n_masks == 1 ? bh : (a.n_masks == a.heads ? bh / a.heads : 0);
@@ -227,12 +228,12 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(kWaves, 
 
 // dK (blockIdx.y 0) or dV of one split key block: its parts in order
 template <int D, int W>
-__global__ __launch_bounds__(256) void grad_join(GradArgs a, int max_splits) {
-    const int rep = blockIdx.x / max_splits, i = blockIdx.x - rep * max_splits;
-    const csr_ptr plan = (csr_ptr)a.plan;
-    if (i >= plan[2]) return;
-    const csr_ptr p = plan + 4 + 4 * (a.n_masks * a.n_blk + a.max_more + i);
-    const int row = p[0], m = row / a.n_blk, blk = row - m * a.n_blk, n = p[2];
+__global__ __launch_bounds__(256) void grad_join(GradArgs a) {
+    const int rep = blockIdx.x / a.max_more, i = blockIdx.x - rep * a.max_more;
+    const csr_ptr p = (csr_ptr)a.plan + 4 * (a.n_masks * a.n_blk + a.max_more + i);
+    const int row = p[0];
+    if (row < 0) return;
+    const int m = row / a.n_blk, blk = row - m * a.n_blk, n = p[2];
     const int bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
     constexpr int SIZE = 32 * W * D;
     const float* part = a.part + ((size_t)rep * a.max_slots + p[1]) * (2 * SIZE) + blockIdx.y * SIZE;
@@ -251,8 +252,8 @@ hipError_t launch_sparse(const GradArgs& a, hipStream_t stream) {
     const int rep = a.n_bh / a.n_masks, more = rep * a.max_more, n = a.n_bh * a.n_blk, per = (n + 7) / 8;
     hipLaunchKernelGGL((grad_sparse<D, W>), dim3(more + 16 * per), dim3(64 * W), 0, stream, a, more, n, per);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.max_splits == 0) return e;
-    hipLaunchKernelGGL((grad_join<D, W>), dim3(rep * a.max_splits, 2), dim3(256), 0, stream, a, a.max_splits);
+    if (e != hipSuccess || more == 0) return e;
+    hipLaunchKernelGGL((grad_join<D, W>), dim3(more, 2), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

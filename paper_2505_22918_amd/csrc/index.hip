@@ -203,10 +203,119 @@ __global__ __launch_bounds__(kThreads) void row_fill(IndexArgs a) {
 
 // ---- transpose of a block mask -------------------------------------------------------------
 //
-// Row kb of the transposed mask lists the query blocks whose rows hold kb, ascending.  One wave per (mask, kb)
-// looks at 64 rows at a time, each lane with a binary search of its row (rows are ascending), once to count and
-// once, after a scan of the counts, to write; ballots keep the order.  Work of n_blk^2 log2(kept) for each mask, in
-// parallel over its rows: 6 us for 278 blocks, beside the gradient calls it serves.
+// Row kb of the transposed mask lists the query blocks whose rows hold kb, ascending, and a plan says how the
+// gradients' call splits long rows (kernels.h).
+//
+// Up to kSmall blocks: one workgroup to a mask sets a bit for each entry in LDS, and a thread to a key block counts its
+// row of bits and writes it out in order.  Masks keep their places by what row_ptr says they hold.  More blocks: one
+// wave to a (mask, kb) looks at 64 rows at a time, each lane with a binary search of its row (rows are ascending),
+// once to count and once, after a scan of the counts, to write; ballots keep the order.
+//
+// Latency: 12 masks of 83 blocks 16 us in three launches, 9 in one.
+
+constexpr int kSmall = 640;  // its bits take 51 KB
+
+// item j's entry of a list of n pieces, {row, first, entries, part or -1}
+__device__ __forceinline__ int4 plan_item(int row, int at, int count, int seg, int j, int n, int part) {
+    const int first = j * seg, left = count - first;
+    return int4{row, at < 0 ? -1 : at + first, left < seg ? left : seg, n > 1 ? part + j : -1};
+}
+__device__ __forceinline__ int pieces_of(int count, int seg) { return count <= seg ? 1 : (count + seg - 1) / seg; }
+
+__global__ __launch_bounds__(1024) void transpose_small(TransposeArgs a) {
+    extern __shared__ uint32_t bits[];
+    // entries of the masks before this one, their room for further parts, entries of all masks
+    __shared__ unsigned long long before[3];
+    __shared__ int waves[16][4];
+    const int m = blockIdx.x, n = a.n_blk, words = (n + 31) >> 5, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    for (int i = tid; i < n * words; i += 1024) bits[i] = 0u;
+    if (tid < 3) before[tid] = 0;
+    __syncthreads();
+    auto entries = [&](int k) {  // of mask k, by its row offsets (as far as the array goes)
+        const int32_t* p = a.row_ptr + (size_t)k * (n + 1);
+        const int b = p[0] < 0 ? 0 : p[0], e = p[n] > a.nnz ? a.nnz : p[n];
+        return e < b ? 0 : e - b;
+    };
+    for (int k = tid; k < a.n_masks; k += 1024) {
+        const int c = entries(k);
+        atomicAdd(&before[2], (unsigned long long)c);
+        if (k >= m) continue;
+        atomicAdd(&before[0], (unsigned long long)c);
+        if (n > a.seg) atomicAdd(&before[1], (unsigned long long)(c / a.seg));
+    }
+    const int32_t* rp = a.row_ptr + (size_t)m * (n + 1);
+    for (int q = tid >> 4; q < n; q += 64) {  // 16 lanes a row
+        int b = rp[q], e = rp[q + 1];
+        b = b < 0 ? 0 : (b > a.nnz ? a.nnz : b);
+        e = e < b ? b : (e > a.nnz ? a.nnz : e);
+        for (int j = b + (tid & 15); j < e; j += 16) {
+            const int c = a.col_idx[j];
+            if (c >= 0 && c < n) atomicOr(&bits[c * words + (q >> 5)], 1u << (q & 31));
+        }
+    }
+    __syncthreads();
+    int count = 0;
+    if (tid < n)
+        for (int i = 0; i < words; ++i) count += __popc(bits[tid * words + i]);
+    const int pieces = tid < n ? pieces_of(count, a.seg) : 1;
+    // running sums of entries, further parts, parts of split lists, split lists
+    int own[4] = {count, pieces - 1, pieces > 1 ? pieces : 0, pieces > 1}, sum[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        int s = own[k];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_up(s, d);
+            if (lane >= d) s += x;
+        }
+        if (lane == 63) waves[wave][k] = s;
+        sum[k] = s - own[k];
+    }
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < 16; ++w) {
+        all += waves[w][0];
+        if (w < wave)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += waves[w][k];
+    }
+    // Where all entries fit, so does their room for further parts.
+    const int mine = entries(m);
+    const bool fits = all <= mine && before[2] <= (unsigned long long)a.t_nnz;
+    const int base = fits ? (int)before[0] : -1;
+    const int skip = before[1] < (unsigned long long)a.max_more ? (int)before[1] : a.max_more;
+    int4* item = reinterpret_cast<int4*>(a.plan);
+    int4* more = item + (size_t)a.n_masks * n + skip;
+    // this mask's room for further parts and split lists; the last mask's is all that is left
+    int left = n > a.seg && m < a.n_masks - 1 ? mine / a.seg : a.max_more - skip;
+    left = left < a.max_more - skip ? left : a.max_more - skip;
+    int n_more = 0, n_split = 0;
+    for (int w = 0; w < 16; ++w) {
+        n_more += waves[w][1];
+        n_split += waves[w][3];
+    }
+    for (int i = tid; i < left; i += 1024) {
+        if (!fits || i >= n_more) more[i] = int4{-1, 0, 0, 0};
+        if (!fits || i >= n_split) more[a.max_more + i] = int4{-1, 0, 0, 0};
+    }
+    int32_t* t_rp = a.t_row_ptr + (size_t)m * (n + 1);
+    if (tid == 0) t_rp[0] = base;
+    if (tid < n) {
+        const int at = fits ? base + sum[0] : -1, row = m * n + tid;
+        t_rp[tid + 1] = fits ? at + count : -1;
+        for (int j = 0; j < (fits ? pieces : 1); ++j) {
+            const int4 x = plan_item(row, at, count, a.seg, j, pieces, 2 * skip + sum[2]);
+            if (j == 0)
+                item[row] = x;
+            else
+                more[sum[1] + j - 1] = x;
+        }
+        if (fits && pieces > 1) more[a.max_more + sum[3]] = int4{row, 2 * skip + sum[2], pieces, 0};
+        int to = at;
+        for (int i = 0; fits && i < words; ++i)
+            for (uint32_t w = bits[tid * words + i]; w; w &= w - 1) a.t_col_idx[to++] = 32 * i + __ffs(w) - 1;
+    }
+}
 
 // whether row qb of mask m holds key block kb
 __device__ __forceinline__ bool row_holds(const TransposeArgs& a, int m, int qb, int kb) {
@@ -244,22 +353,20 @@ __global__ __launch_bounds__(64) void transpose_rows(TransposeArgs a) {
     if (!FILL && lane == 0) row[1] = at;
 }
 
-// One workgroup: counts in row_ptr[m][kb + 1] become absolute offsets, and the plan is written; offsets and the plan's
-// item count are -1 if the entries do not fit.
+// One workgroup: counts in row_ptr[m][kb + 1] become absolute offsets (-1 if the entries do not fit), and the plan is
+// written.
 __global__ __launch_bounds__(1024) void transpose_scan(TransposeArgs a) {
-    __shared__ int64_t part[4][1024];  // entries, parts past a list's first, parts of split lists, split lists
-    const int64_t rows = (int64_t)a.n_masks * a.n_blk, seg = (rows + 1023) / 1024;
-    const int64_t i0 = threadIdx.x * seg, i1 = i0 + seg < rows ? i0 + seg : rows;
-    auto pieces = [&](int c) { return c <= a.seg ? 1 : (c + a.seg - 1) / a.seg; };
-    int64_t sum[4] = {0, 0, 0, 0};
+    __shared__ int64_t part[4][1024];  // entries, further parts, parts of split lists, split lists
+    const int64_t rows = (int64_t)a.n_masks * a.n_blk, each = (rows + 1023) / 1024;
+    const int64_t i0 = threadIdx.x * each, i1 = i0 + each < rows ? i0 + each : rows;
+    int64_t sum[4] = {0, 0, 0, 0}, own[4];
     for (int64_t i = i0; i < i1; ++i) {
-        const int c = a.t_row_ptr[i + i / a.n_blk + 1], n = pieces(c);
+        const int c = a.t_row_ptr[i + i / a.n_blk + 1], n = pieces_of(c, a.seg);
         sum[0] += c;
         sum[1] += n - 1;
         sum[2] += n > 1 ? n : 0;
         sum[3] += n > 1;
     }
-    int64_t own[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         own[k] = sum[k];
@@ -278,24 +385,27 @@ __global__ __launch_bounds__(1024) void transpose_scan(TransposeArgs a) {
     int64_t at[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) at[k] = part[k][threadIdx.x] - own[k];
-    if (threadIdx.x < 4) a.plan[threadIdx.x] = threadIdx.x == 3 ? 0 : (fits ? (int32_t)part[threadIdx.x + 1][1023] : (threadIdx.x == 0 ? -1 : 0));
+    int4* item = reinterpret_cast<int4*>(a.plan);
+    int4* more = item + rows;
+    for (int64_t i = threadIdx.x; i < a.max_more; i += 1024) {
+        if (!fits || i >= part[1][1023]) more[i] = int4{-1, 0, 0, 0};
+        if (!fits || i >= part[3][1023]) more[a.max_more + i] = int4{-1, 0, 0, 0};
+    }
     for (int64_t i = i0; i < i1; ++i) {
         const int64_t m = i / a.n_blk;
-        const int c = a.t_row_ptr[i + m + 1];
-        if (i == m * a.n_blk) a.t_row_ptr[i + m] = fits ? (int32_t)at[0] : -1;
-        a.t_row_ptr[i + m + 1] = fits ? (int32_t)(at[0] + c) : -1;
-        if (fits) {
-            const int n = pieces(c);
-            int4* item = reinterpret_cast<int4*>(a.plan + 4);
-            for (int j = 0; j < n; ++j) {
-                const int first = j * a.seg, left = c - first;
-                item[j ? rows + at[1]++ : i] =
-                    int4{(int)i, (int)at[0] + first, left < a.seg ? left : a.seg, n > 1 ? (int)at[2] + j : -1};
-            }
-            if (n > 1) {
-                item[rows + a.max_more + at[3]++] = int4{(int)i, (int)at[2], n, 0};
-                at[2] += n;
-            }
+        const int c = a.t_row_ptr[i + m + 1], n = pieces_of(c, a.seg), to = fits ? (int)at[0] : -1;
+        if (i == m * a.n_blk) a.t_row_ptr[i + m] = to;
+        a.t_row_ptr[i + m + 1] = fits ? to + c : -1;
+        for (int j = 0; j < (fits ? n : 1); ++j) {
+            const int4 x = plan_item((int)i, to, c, a.seg, j, n, (int)at[2]);
+            if (j == 0)
+                item[i] = x;
+            else
+                more[at[1]++] = x;
+        }
+        if (fits && n > 1) {
+            more[a.max_more + at[3]++] = int4{(int)i, (int)at[2], n, 0};
+            at[2] += n;
         }
         at[0] += c;
     }
@@ -304,6 +414,11 @@ __global__ __launch_bounds__(1024) void transpose_scan(TransposeArgs a) {
 }  // namespace
 
 hipError_t launch_index_transpose(const TransposeArgs& a, hipStream_t stream) {
+    if (a.n_blk <= kSmall) {
+        const size_t lds = (size_t)a.n_blk * ((a.n_blk + 31) / 32) * 4;
+        hipLaunchKernelGGL(transpose_small, dim3(a.n_masks), dim3(1024), lds, stream, a);
+        return hipGetLastError();
+    }
     const dim3 rows((uint32_t)a.n_masks * (uint32_t)a.n_blk);
     hipLaunchKernelGGL(transpose_rows<false>, rows, dim3(64), 0, stream, a);
     hipError_t err = hipGetLastError();

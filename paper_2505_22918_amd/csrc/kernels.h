@@ -101,10 +101,10 @@ hipError_t dynamic_scratch(float** ptr);
 
 // Transpose of a block mask (index.hip): row kb of mask m lists the query blocks that keep kb.  The plan that follows
 // says which workgroup of the gradients' call walks what: lists of more than `seg` entries are split.
-//   plan[0 .. 2]  further parts, parts of split lists, split lists; plan[0] -1: the entries did not fit, no plan
-//   then {mask * n_blk + kb, first entry, entries, part or -1} of every row, the first part of a split one,
-//   then max_more of the like for further parts,
-//   then max_splits of {mask * n_blk + kb, first part, parts, 0}
+//   {mask * n_blk + kb, first entry, entries, part or -1} of every row, the first part of a split one,
+//   then max_more of the like for further parts (mask * n_blk + kb is -1: none),
+//   then max_more of {mask * n_blk + kb, first part, parts, 0} of split lists (-1: none)
+// A first entry of -1: the mask's entries did not fit.
 struct TransposeArgs {
     const int32_t* row_ptr;  // [n_masks][n_blk + 1]
     const int32_t* col_idx;
@@ -136,7 +136,7 @@ struct GradArgs {
     int32_t T64;        // T in whole 64
     float* part;        // workspace: fp32 dK and dV [slot][2][block][D] of split lists, max_slots for each use of a mask
     const int32_t* plan;  // of the transposed mask
-    int32_t max_more, max_slots, max_splits;
+    int32_t max_more, max_slots;
     const int32_t* row_ptr;  // null: dense
     const int32_t* col_idx;
     const int32_t* t_col_idx;

@@ -32,7 +32,7 @@ hipError_t launch_attention_backward(const GradArgs& a, int D, hipStream_t) {
     if (a.row_ptr) {
         EXPECT(a.col_idx && a.t_col_idx && a.plan > a.t_col_idx && a.nnz > 0);
         EXPECT(a.n_blk == (a.T + a.block - 1) / a.block && a.n_bh % a.n_masks == 0);
-        EXPECT(a.max_more == a.max_splits && a.max_slots == 2 * a.max_splits);
+        EXPECT(a.max_slots == 2 * a.max_more);
         EXPECT((char*)a.part >= (char*)(a.row_vals + 2 * (size_t)a.n_bh * a.T64) && ((uintptr_t)a.part & 15) == 0);
         EXPECT((a.block == 32 || a.block == 64) && a.n_masks >= 1);
     }
