@@ -2,7 +2,7 @@
 // reshape's factor, the probabilities recomputed from the forward call's row statistics.
 //
 //   grad_rows    per query row: -delta = -dO . O, and log2 of the denominator over the row's factor
-//   grad_dense   dK and dV of 256 keys, or dQ of 256 queries, to a workgroup of eight waves
+//   grad_dense   dK and dV of 128 keys, or dQ of 128 queries, to a workgroup of four waves
 //   grad_sparse  the same for one block, over the blocks its row of the (transposed) mask lists
 //   grad_join    sums of the parts of key blocks whose lists were split
 //
@@ -22,13 +22,7 @@ namespace {
 
 // ---- rows ----------------------------------------------------------------------------------
 
-template <int CTRL>
-__device__ __forceinline__ float dpp(float x) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
-}
-
-// 8 lanes a row (of a 72-wide row the first takes the last 8 elements too); rows are counted with each head's padded to
-// whole 64, whose values are zeros
+// 8 lanes a row; rows are counted with each head's padded to whole 64, whose values are zeros
 template <int D>
 __global__ __launch_bounds__(256) void grad_rows(GradArgs a, int64_t rows) {
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3;
@@ -42,23 +36,9 @@ __global__ __launch_bounds__(256) void grad_rows(GradArgs a, int64_t rows) {
         return;
     }
     const int64_t row = bh * a.T + t;
-    float s = 0.f;
-    auto add = [&](int ch) {
-        const size_t at = (size_t)row * D + 8 * ch;
-        const u32x4 x = *reinterpret_cast<const u32x4*>(a.o + at), y = *reinterpret_cast<const u32x4*>(a.d_o + at);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            s = __builtin_fmaf(lo_f(x[w]), lo_f(y[w]), s);
-            s = __builtin_fmaf(hi_f(x[w]), hi_f(y[w]), s);
-        }
-    };
-    add(c);
-    if (D == 72 && c == 0) add(8);
-    s += dpp<0xB1>(s);
-    s += dpp<0x4E>(s);
-    s += dpp<0x141>(s);
+    const float s = row_delta<D>(a, row, c);
     if (c == 0) {
-        float log = __builtin_fmaf(a.row_max[row], 1.44269504f, log2f(a.row_sum[row]));
+        float log = row_log(a, row);
         if (a.rho) {
             const float r = a.rho[row] + a.rho_delta;
             log -= log2f(fminf(1.0f, r));  // a factor of 0: +inf, no probability
@@ -69,62 +49,89 @@ __global__ __launch_bounds__(256) void grad_rows(GradArgs a, int64_t rows) {
     }
 }
 
+// Stages of the ring.  Two: a longer lead cost more than it gave (three: dense CogVideoX 15.4 against 14.8 ms, all with
+// two waves to a SIMD; its sparse call 785 us with four, 696 with two).
+constexpr int kStages = 2;
+
 // ---- dense ---------------------------------------------------------------------------------
 
+// A head of up to kShort rows: its workgroups form the row values themselves (those of dK and dV all of them, in LDS),
+// which saves the launch of grad_rows.
+constexpr int kShort = 512;
+
 // dK and dV (KV) or dQ of 32 W rows of a head against all of the other side: stages 0, 1, .. of 64 rows.
-template <int D, bool KV, int W>
+template <int D, bool KV, int W, bool SHORT>
 __device__ __forceinline__ void dense_walk(const GradArgs& a, lds_u8* lds, int item) {
-    using R = GradRing<D, KV, W, 64, 3>;
+    using R = GradRing<D, KV && !SHORT, W, 64, kStages>;
     const int T = a.T, n64 = (T + 63) >> 6, n_tile = (T + 32 * W - 1) / (32 * W);
     const int bh = item / n_tile;
     const int row0 = ((item - bh * n_tile) * W + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 32;
     const size_t head_off = (size_t)bh * (size_t)T * D;
-    const float* vals = a.row_vals + (size_t)bh * 2 * a.T64;
     R ring;
-    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, vals, T, a.T64);
+    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, a.row_vals + (size_t)bh * 2 * a.T64, T,
+              a.T64);
     ring.load(0, 0);
-    ring.load(R::STAGE, 64);
     GradTile<D, KV, R::ZERO, R::TENSOR> t;
     t.init(lds, a.scale_log2);
-    t.load_own(a, head_off, vals, row0, T);
+    t.load_own(a, head_off, row0, T);
+    constexpr int LOGS = R::LDS, MINUS = LOGS + kShort * 4;  // SHORT: LDS offsets of all rows' values
+    if (KV && SHORT) {
+        for (int i = threadIdx.x >> 3; i < a.T64; i += 8 * W) {
+            const int c = threadIdx.x & 7;
+            float log = 0.f, minus = 0.f;
+            if (i < T) {
+                const size_t row = (size_t)bh * T + i;
+                minus = -row_delta<D>(a, row, c);
+                log = row_log(a, row);
+            }
+            if (c == 0) {
+                *(__attribute__((address_space(3))) float*)(lds + LOGS + 4 * i) = log;
+                *(__attribute__((address_space(3))) float*)(lds + MINUS + 4 * i) = minus;
+            }
+        }
+    }
+    if (!KV) {
+        if (SHORT)
+            t.make_values(a, bh, row0, T);
+        else
+            t.load_values(a, bh, row0, T);
+    }
     int st = 0;  // LDS offset of the stage in use
     for (int s = 0; s < n64; ++s) {
         ring.turn();
-        ring.load(st == 0 ? 2 * R::STAGE : st - R::STAGE, (s + 2) * 64);
+        ring.load(R::STAGE - st, (s + 1) * 64);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int cx = st + 32 * h * R::ROWB, logs = st + R::STAT + 128 * h;
-            t.scores(cx, logs + 256);
-            if (!KV && s * 64 + 32 * h + 32 > T) t.mask(s * 64 + 32 * h, T);
-            t.soft(logs);
+            const int cx = st + 32 * h * R::ROWB, row = s * 64 + 32 * h;
+            t.scores(cx, SHORT ? MINUS + 4 * row : st + R::STAT + 256 + 128 * h);
+            if (!KV && row + 32 > T) t.mask(row, T);
+            t.soft(SHORT ? LOGS + 4 * row : st + R::STAT + 128 * h);
             t.grads(cx);
         }
-        st = st == 2 * R::STAGE ? 0 : st + R::STAGE;
+        st = R::STAGE - st;
     }
     wait_vm<0>();  // nothing may land in LDS after the workgroup has ended
     t.store_all(a, head_off, row0, T);
 }
 
-template <int D, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2, 2))) void grad_dense(GradArgs a, int n_items,
-                                                                                              int per_xcd) {
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[GradRing<D, true, W, 64, 3>::LDS];
+template <int D, int W, int WAVES, bool SHORT>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) void grad_dense(GradArgs a,
+                                                                                                      int n_items,
+                                                                                                      int per_xcd) {
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[GradRing<D, true, W, 64, kStages>::LDS +
+                                                                 (SHORT ? 2 * kShort * 4 : 0)];
     // the first half of the workgroups, which has more to do, takes dK and dV
     const bool kv = (int)blockIdx.x < 8 * per_xcd;
     const int g = kv ? blockIdx.x : blockIdx.x - 8 * per_xcd;
     const int item = (g & 7) * per_xcd + (g >> 3);
     if (item >= n_items) return;
     if (kv)
-        dense_walk<D, true, W>(a, (lds_u8*)smem, item);
+        dense_walk<D, true, W, SHORT>(a, (lds_u8*)smem, item);
     else
-        dense_walk<D, false, W>(a, (lds_u8*)smem, item);
+        dense_walk<D, false, W, SHORT>(a, (lds_u8*)smem, item);
 }
 
 // ---- sparse --------------------------------------------------------------------------------
-
-// Stages of 32 rows under way, and waves of a SIMD: three are worth more than a longer lead (CogVideoX 785 us with two
-// waves and four stages, 696 with two of each, 605 with three and two; 32-token blocks have LDS for two).
-constexpr int kStages = 2, kWaves = 3;
 
 // dK and dV (KV) or dQ of one block of a head against the `count` blocks listed from `list` on.  part: null, or where
 // the fp32 sums of a split list go.
@@ -135,11 +142,11 @@ __device__ __forceinline__ void sparse_walk(const GradArgs& a, lds_u8* lds, int 
     const int T = a.T, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = blk * (32 * W) + 32 * wave;
     const size_t head_off = (size_t)bh * (size_t)T * D;
-    const float* vals = a.row_vals + (size_t)bh * 2 * a.T64;
     const csr_ptr idx = (csr_ptr)list;
     const int n = count * W;
     R ring;
-    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, vals, T, a.T64);
+    ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, a.row_vals + (size_t)bh * 2 * a.T64, T,
+              a.T64);
     auto row_at = [&](int s) {  // first row of stage s; none past the list or for an index out of range
         if (s >= n) return -1;
         const int c = idx[s / W];
@@ -152,7 +159,8 @@ __device__ __forceinline__ void sparse_walk(const GradArgs& a, lds_u8* lds, int 
     for (int i = 0; i < kStages - 1; ++i) ring.load(i * R::STAGE, rows[i]);
     GradTile<D, KV, R::ZERO, R::TENSOR> t;
     t.init(lds, a.scale_log2);
-    t.load_own(a, head_off, vals, row0, T);
+    t.load_own(a, head_off, row0, T);
+    if (!KV) t.load_values(a, bh, row0, T);
     int st = 0;
     for (int s = 0; s < n; ++s) {
         ring.turn();
@@ -182,7 +190,7 @@ __device__ __forceinline__ void sparse_walk(const GradArgs& a, lds_u8* lds, int 
 // so that what takes longest begins first.  (A block's dK and dV next to its dQ, which reads the same rows, was no
 // faster at the CogVideoX shape and 20 % slower where the lists are random.)
 template <int D, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(kWaves, kWaves))) void grad_sparse(
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(3, 3))) void grad_sparse(
     GradArgs a, int more, int n_items, int per_xcd) {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[GradRing<D, true, W, 32, kStages>::LDS];
     lds_u8* const lds = (lds_u8*)smem;
@@ -259,14 +267,25 @@ hipError_t launch_sparse(const GradArgs& a, hipStream_t stream) {
 
 template <int D>
 hipError_t launch_d(const GradArgs& a, hipStream_t stream) {
-    const int64_t rows = (int64_t)a.n_bh * a.T64;
-    hipLaunchKernelGGL((grad_rows<D>), dim3((uint32_t)((rows * 8 + 255) / 256)), dim3(256), 0, stream, a, rows);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (a.row_ptr) return a.block == 64 ? launch_sparse<D, 2>(a, stream) : launch_sparse<D, 1>(a, stream);
-    constexpr int W = 8;
+    constexpr int W = 4;
     const int n = a.n_bh * ((a.T + 32 * W - 1) / (32 * W)), per = (n + 7) / 8;
-    hipLaunchKernelGGL((grad_dense<D, W>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
+    const bool few = n < 256;  // 2 n workgroups over 256 CUs
+    if (a.row_ptr || a.T > kShort || !few) {
+        const int64_t rows = (int64_t)a.n_bh * a.T64;
+        hipLaunchKernelGGL((grad_rows<D>), dim3((uint32_t)((rows * 8 + 255) / 256)), dim3(256), 0, stream, a, rows);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (a.row_ptr) return a.block == 64 ? launch_sparse<D, 2>(a, stream) : launch_sparse<D, 1>(a, stream);
+    // Workgroups of four waves (eight: 15.6 against 15.4 ms at the CogVideoX shape, 11.4 against 8.4 us at 2 heads of 256
+    // tokens).  64-wide heads fit three waves to a SIMD, which pays where there are as many (14.5 against 14.8 ms; 9.0
+    // against 7.9 us where there are not: a wave with fewer registers waits more); 72-wide ones spill (819 against 533).
+    if (!few)
+        hipLaunchKernelGGL((grad_dense<D, W, D == 64 ? 3 : 2, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
+    else if (a.T > kShort)
+        hipLaunchKernelGGL((grad_dense<D, W, 2, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
+    else
+        hipLaunchKernelGGL((grad_dense<D, W, 2, true>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
     return hipGetLastError();
 }
 

@@ -44,6 +44,34 @@ __device__ __forceinline__ int swz(int r) {
     return Geo<D>::SWZ ? ((r & 2) << 1) | ((r & 8) >> 2) | ((r & 4) >> 2) : 0;
 }
 
+// 8 lanes a row (lane c of them; of a 72-wide row the first takes the last 8 elements too): dO . O, in all of them
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int D>
+__device__ __forceinline__ float row_delta(const GradArgs& a, size_t row, int c) {
+    float s = 0.f;
+    auto add = [&](int ch) {
+        const size_t at = row * D + 8 * ch;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(a.o + at), y = *reinterpret_cast<const u32x4*>(a.d_o + at);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            s = __builtin_fmaf(lo_f(x[w]), lo_f(y[w]), s);
+            s = __builtin_fmaf(hi_f(x[w]), hi_f(y[w]), s);
+        }
+    };
+    add(c);
+    if (D == 72 && c == 0) add(8);
+    s += dpp<0xB1>(s);
+    s += dpp<0x4E>(s);
+    return s + dpp<0x141>(s);
+}
+// log2 of a row's denominator
+__device__ __forceinline__ float row_log(const GradArgs& a, size_t row) {
+    return __builtin_fmaf(a.row_max[row], 1.44269504f, log2f(a.row_sum[row]));
+}
+
 // ZERO: LDS offset of 16 zero bytes.  A chunk's 32 rows of Y lie CHUNK_Y behind those of X.
 template <int D, bool KV, int ZERO, int CHUNK_Y>
 struct GradTile {
@@ -83,24 +111,41 @@ struct GradTile {
         }
     }
 
-    // own rows row0 .. + 31 of a head (zeros past its end): lane holds row l32, dims 16 s + 8 hi ..
-    __device__ __forceinline__ void load_own(const GradArgs& a, size_t head_off, const float* vals, int row0, int T) {
+    // rows row0 .. + 31 of a head's x (zeros past its end): lane holds row l32, dims 16 s + 8 hi ..
+    __device__ __forceinline__ void load_rows(const uint16_t* x, int row0, int T, bf16x8 (&to)[4], bf16x8& to_tail) {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, T * ROWB, 0x00020000);
+        const int off = (row0 + l32) * ROWB;
+        auto load = [&](int o) { return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, o, 0, 0)); };
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const uint16_t* x = (KV ? (y ? a.v : a.k) : (y ? a.d_o : a.q)) + head_off;
-            const __amdgpu_buffer_rsrc_t rs =
-                __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, T * ROWB, 0x00020000);
-            const int off = (row0 + l32) * ROWB;
-            auto load = [&](int o) { return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, o, 0, 0)); };
+        for (int s = 0; s < 4; ++s) to[s] = load(off + 32 * s + 16 * hi);
+        if (TAIL) to_tail = load(hi ? kOob : off + 128);
+    }
+    __device__ __forceinline__ void load_own(const GradArgs& a, size_t head_off, int row0, int T) {
+        load_rows((KV ? a.k : a.q) + head_off, row0, T, own[0], own_tail[0]);
+        load_rows((KV ? a.v : a.d_o) + head_off, row0, T, own[1], own_tail[1]);
+    }
+    // !KV: the own row's log and -delta, as grad_rows left them
+    __device__ __forceinline__ void load_values(const GradArgs& a, int bh, int row0, int T) {
+        const float* vals = a.row_vals + (size_t)bh * 2 * a.T64;
+        const int row = row0 + l32;
+        log = row < T ? vals[row] : INFINITY;
+        nd = row < T ? vals[a.T64 + row] : 0.f;
+    }
+    // or formed from the own rows
+    __device__ __forceinline__ void make_values(const GradArgs& a, int bh, int row0, int T) {
+        bf16x8 o[4], o_tail;
+        load_rows(a.o + (size_t)bh * (size_t)T * D, row0, T, o, o_tail);
+        const int row = row0 + l32;
+        float s = 0.f;
+        auto add = [&](const bf16x8& x, const bf16x8& y) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s) own[y][s] = load(off + 32 * s + 16 * hi);
-            if (TAIL) own_tail[y] = load(hi ? kOob : off + 128);
-        }
-        if (!KV) {
-            const int row = row0 + l32;
-            log = row < T ? vals[row] : INFINITY;
-            nd = row < T ? vals[a.T64 + row] : 0.f;
-        }
+            for (int e = 0; e < 8; ++e) s = __builtin_fmaf((float)x[e], (float)y[e], s);
+        };
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add(o[k], own[1][k]);
+        if (TAIL) add(o_tail, own_tail[1]);
+        log = row < T ? row_log(a, (size_t)bh * T + row) : INFINITY;
+        nd = -pair_sum(s);
     }
 
     __device__ __forceinline__ bf16x8 row_read(int base, int s) const {
@@ -251,10 +296,10 @@ struct GradTile {
     }
 };
 
-// The ring of NS stages of BS rows of X and Y (and, KV, of their logs and -deltas) that W waves fill and read: stage
+// The ring of NS stages of BS rows of X and Y (and, VALS, of their logs and -deltas) that W waves fill and read: stage
 // s + NS - 1 is asked for when all waves are through s - 1, whose place it takes.  The first half of the waves loads X,
 // the other half Y (a lone wave both), the first wave the row values.  Rows past the head's end read as zeros.
-template <int D, bool KV, int W, int BS, int NS>
+template <int D, bool VALS, int W, int BS, int NS>
 struct GradRing {
     static constexpr int ROWB = 2 * D, TENSOR = BS * ROWB, STAT = 2 * TENSOR, STAGE = STAT + BS * 8;
     static constexpr int ZERO = NS * STAGE, LDS = ZERO + 64;
@@ -281,7 +326,7 @@ struct GradRing {
         rs[0] = buffer_rsrc(x, T * ROWB);
         rs[1] = buffer_rsrc(y, T * ROWB);
         // lanes of the first half of BS values take logs, the others -deltas
-        if (KV) {
+        if (VALS) {
             st = buffer_rsrc(vals, T64 * 8);
             from_st = lane < BS / 4 ? lane * 16 : T64 * 4 + (lane - BS / 4) * 16;
         }
@@ -308,12 +353,12 @@ struct GradRing {
                 if (lane < REST) dma16(__builtin_amdgcn_readfirstlane(dst + b), from[0] + at + b, r);
             }
         }
-        if (KV && w == 0 && lane < BS / 2)
+        if (VALS && w == 0 && lane < BS / 2)
             dma16(__builtin_amdgcn_readfirstlane(lds0 + to + STAT), from_st + at4, st);
     }
     // the oldest of NS - 1 stages asked for has landed, and every wave is through the stage before it
     __device__ __forceinline__ void turn() {
-        if (KV && w == 0)
+        if (VALS && w == 0)
             wait_vm<(NS - 2) * (LOADS + 1)>();
         else
             wait_vm<(NS - 2) * LOADS>();

@@ -250,3 +250,21 @@ def test_equal_calls_give_equal_bits(gpu):
         first = bwd(s)
         for _ in range(3):
             assert all(torch.equal(x, y) for x, y in zip(first, bwd(s)))
+
+
+@pytest.mark.parametrize("D", [64, 72])
+@pytest.mark.parametrize("T", [37, 200, 530])
+def test_full_many_heads(gpu, D, T):
+    """More workgroups than CUs: another kernel than few heads take."""
+    B, H = 8, 40
+    dev, host = _inputs(B, H, T, D, T + D)
+    stats = rt.attn_full(*dev[:3])
+    out = rt.attn_full_backward(*dev[:3], *stats, dev[3])
+    pick = [(0, 0), (3, 17), (7, 39)]
+    sub = lambda t: np.stack([to_np(t[b, h]) for b, h in pick])[None]  # noqa: E731
+    q, k, v, d_o = (np.stack([x[b, h] for b, h in pick])[None] for x in host)
+    o, m, l = (sub(x) for x in stats)
+    for i in range(len(pick)):
+        a = (q[0, i], k[0, i], v[0, i], o[0, i], m[0, i], l[0, i], d_o[0, i])
+        for name, g, r, t in zip(("dq", "dk", "dv"), out, og.head_backward(*a), og.head_tolerances(*a)):
+            _check(sub(g)[0, i], r, t, f"{name} of head {pick[i]}")
