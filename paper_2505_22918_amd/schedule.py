@@ -33,19 +33,22 @@ def is_caching_step(t: int, full_steps: int, period: int) -> bool:
     return period > 0 and (t - full_steps + 1) % period == 0
 
 
-def run(mask, qkv, n_steps, full_steps, period, lam, sigma, seed=0, diagnose=True, evolve=None, ratio=True):
+def run(mask, qkv, n_steps, full_steps, period, lam, sigma, seed=0, diagnose=True, evolve=None, ratio=True,
+        qk_norm=None):
     """Drives n_steps denoising steps of one attention layer.
 
     qkv: device bf16 (q, k, v) of step 0.  Each later step's inputs come from
     ``evolve(prev, t)`` (default: + sigma * N(0,1) drawn on the device from a
     generator seeded with seed + t, rounded to bf16).  ratio=False runs the
     ablation without the statistical reshape (cache O_full - O_sparse, later
-    steps add it to the sparse output).  Returns a list of per-step records (and
+    steps add it to the sparse output).  qk_norm: (weight, bias) pairs of the layer
+    norms that each head's queries and keys pass through before attention, as
+    CogVideoX has them; what drifts are the rows before them.  Returns a list of per-step records (and
     the step outputs when ``diagnose`` is False, for callers that check them).
     """
     import torch
 
-    from . import StatCache, attn_cache, attn_sparse
+    from . import StatCache, attn_cache, attn_sparse, layer_norm
 
     if evolve is None:
         def evolve(prev, t):
@@ -61,6 +64,8 @@ def run(mask, qkv, n_steps, full_steps, period, lam, sigma, seed=0, diagnose=Tru
         if t > 0:
             cur = evolve(cur, t)
         q, k, v = cur
+        if qk_norm is not None:
+            q, k = (layer_norm(x, *wb, eps=1e-6) for x, wb in zip((q, k), qk_norm))
         caching = cache.is_caching_step(t) or cache.resid is None
         out = cache.attend(q, k, v, t)
         rec = {"t": t, "kind": ("full" if t < full_steps else "cache") if caching else "reshape"}
@@ -102,6 +107,8 @@ def main(argv=None):
     ap.add_argument("--seed", type=int, default=0)
     ap.add_argument("--no-ratio", action="store_true",
                     help="the ablation without the statistical reshape (residual O_full - O_sparse)")
+    ap.add_argument("--qk-norm", action="store_true",
+                    help="queries and keys pass through a layer norm of each head's rows (weight 1, bias 0)")
     args = ap.parse_args(argv)
 
     import numpy as np
@@ -118,8 +125,12 @@ def main(argv=None):
         mask = build_index(wl.T, wl.block, wl.kind, **kw)
     to_dev = lambda b: torch.from_numpy(np.ascontiguousarray(b).view(np.int16)).cuda().view(torch.bfloat16)
     qkv = tuple(to_dev(x) for x in synth.make_qkv(wl, 1, seed=args.seed))
+    norm = None
+    if args.qk_norm:
+        one, zero = torch.ones(wl.D, device="cuda"), torch.zeros(wl.D, device="cuda")
+        norm = ((one, zero), (one, zero))
     recs = run(mask, qkv, args.steps, args.full_steps, args.period, args.lam, args.sigma, seed=args.seed,
-               ratio=not args.no_ratio)
+               ratio=not args.no_ratio, qk_norm=norm)
     for r in recs:
         print(json.dumps(r), flush=True)
     rs = [r for r in recs if r["kind"] == "reshape"]
