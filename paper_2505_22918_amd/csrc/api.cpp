@@ -911,6 +911,7 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     a.col_idx = mask->col_idx;
     a.nnz = mask->nnz;
     a.t_col_idx = t->col_idx;
+    a.t_nnz = t->nnz;
     a.plan = t->col_idx + p.first;
     a.max_more = p.max_more;
     a.max_slots = p.max_slots;

@@ -200,7 +200,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(3, 3))) 
         const int rep = blockIdx.x / a.max_more, i = blockIdx.x - rep * a.max_more;
         item = a.n_masks * a.n_blk + i;
         const int row = plan[4 * item];
-        if (row < 0) return;
+        if (row < 0 || row >= a.n_masks * a.n_blk) return;
         m = row / a.n_blk;
         blk = row - m * a.n_blk;
         bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
@@ -220,13 +220,13 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(3, 3))) 
         e = e < b ? b : (e > a.nnz ? a.nnz : e);
         sparse_walk<D, false, W>(a, lds, bh, blk, a.col_idx + b, e - b, nullptr);
     } else if (plan[4 * item + 1] >= 0) {
+        // (clamped to their arrays, as the CSR is: whatever t holds, nothing else is read or written)
         const csr_ptr p = plan + 4 * item;
-        float* part = nullptr;
-        if (p[3] >= 0) {
-            const int rep = a.n_masks == 1 ? bh : (a.n_masks == a.heads ? bh / a.heads : 0);
-            part = a.part + ((size_t)rep * a.max_slots + p[3]) * (2 * 32 * W * D);
-        }
-        sparse_walk<D, true, W>(a, lds, bh, blk, a.t_col_idx + p[1], p[2], part);
+        const int first = p[1] < a.t_nnz ? p[1] : a.t_nnz, slot = p[3] < a.max_slots ? p[3] : -1;
+        const int count = p[2] < 0 ? 0 : (p[2] < a.t_nnz - first ? p[2] : a.t_nnz - first);
+        const int rep = a.n_masks == 1 ? bh : (a.n_masks == a.heads ? bh / a.heads : 0);
+        sparse_walk<D, true, W>(a, lds, bh, blk, a.t_col_idx + first, count,
+                                slot < 0 ? nullptr : a.part + ((size_t)rep * a.max_slots + slot) * (2 * 32 * W * D));
     } else {  // the transpose did not fit its array
         const size_t at = (size_t)bh * (size_t)a.T * D + (size_t)blk * 32 * W * D;
         const int left = a.T - blk * 32 * W, size = (left < 32 * W ? left : 32 * W) * D;
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256) void grad_join(GradArgs a) {
     const int rep = blockIdx.x / a.max_more, i = blockIdx.x - rep * a.max_more;
     const csr_ptr p = (csr_ptr)a.plan + 4 * (a.n_masks * a.n_blk + a.max_more + i);
     const int row = p[0];
-    if (row < 0) return;
+    if (row < 0 || row >= a.n_masks * a.n_blk || p[1] < 0 || p[2] < 1 || p[2] > a.max_slots - p[1]) return;
     const int m = row / a.n_blk, blk = row - m * a.n_blk, n = p[2];
     const int bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
     constexpr int SIZE = 32 * W * D;

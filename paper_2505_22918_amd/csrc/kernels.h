@@ -136,7 +136,7 @@ struct GradArgs {
     int32_t T64;        // T in whole 64
     float* part;        // workspace: fp32 dK and dV [slot][2][block][D] of split lists, max_slots for each use of a mask
     const int32_t* plan;  // of the transposed mask
-    int32_t max_more, max_slots;
+    int32_t t_nnz, max_more, max_slots;
     const int32_t* row_ptr;  // null: dense
     const int32_t* col_idx;
     const int32_t* t_col_idx;

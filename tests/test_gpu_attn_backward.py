@@ -268,3 +268,45 @@ def test_full_many_heads(gpu, D, T):
         a = (q[0, i], k[0, i], v[0, i], o[0, i], m[0, i], l[0, i], d_o[0, i])
         for name, g, r, t in zip(("dq", "dk", "dv"), out, og.head_backward(*a), og.head_tolerances(*a)):
             _check(sub(g)[0, i], r, t, f"{name} of head {pick[i]}")
+
+
+def test_largest_head(gpu):
+    """One head of the longest sequence whose offsets the kernels hold, block-diagonal: each block is an attention of its
+    own.  (131072 blocks: the transpose by searches; offsets of 2^30 bytes.)"""
+    import torch
+
+    T, D, block = 1 << 23, 64, 64
+    n = T // block
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, d_o = (torch.randn(1, 1, T, D, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    at = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    mask = rt.BlockMask(at, at[:n].clone(), block, n, n)
+    print("[sparse backward] largest head", flush=True)
+    o, m, l = rt.attn_sparse(q, k, v, mask)
+    out = rt.attn_sparse_backward(q, k, v, o, m, l, d_o, mask)
+    torch.cuda.synchronize()
+    for b in (0, 1, n // 2, n - 2, n - 1):
+        part = lambda t: to_np(t[0, 0, b * block:(b + 1) * block])  # noqa: E731
+        a = tuple(part(t) for t in (q, k, v, o, m, l, d_o))
+        for name, x, r, t in zip(("dq", "dk", "dv"), out, og.head_backward(*a), og.head_tolerances(*a)):
+            _check(part(x), r, t, f"{name} of block {b}")
+
+
+def test_a_transpose_of_anything_stays_in_its_arrays(gpu):
+    """The gradient call does not trust what the transpose holds: entries, parts and blocks out of range are left out."""
+    import torch
+
+    from paper_2505_22918_amd import _lib
+
+    T, n = 256, 4
+    dev, _ = _inputs(1, 2, T, 64, 15)
+    mask = rt.BlockMask.from_csr(np.arange(0, 2 * n + 1, 2), [0, 1, 0, 1, 2, 3, 2, 3], 64)
+    stats = rt.attn_sparse(*dev[:3], mask)
+    want = rt.attn_sparse_backward(*dev[:3], *stats, dev[3], mask)
+    t = mask.transposed()
+    for junk in (0, 7, 1 << 20, 0x7fffffff, -1, -0x80000000):
+        t.col_idx.fill_(junk)
+        dq, dk, dv = rt.attn_sparse_backward(*dev[:3], *stats, dev[3], mask)
+        torch.cuda.synchronize()
+        assert torch.equal(dq, want[0]) and dk.shape == dv.shape, junk
+    assert _lib.load().rt_last_error() == b""
