@@ -606,8 +606,9 @@ rt_status check_transposed(const rt_bsr* t, const rt_bsr* m) {
 }
 
 // How the lists of a transposed mask with room for `entries` are split over workgroups: after `seg` entries, four times
-// the mean list (and 32 at least), so that few are and none holds the others up; and what the plan and the parts
-// of split lists take at most.
+// the mean list and 96 at least, so that few are and none holds the others up; and what the plan and the parts of split
+// lists take at most.  CogVideoX-2B, whose four text blocks are kept by all 278 query blocks: parts of 36 entries
+// 630 us and 22 for their sums, of 96 595 and 9.5, of 128 593 and 9.
 struct Plan {
     int32_t seg, max_more, max_slots;
     int64_t first, values;  // the plan's place behind the entries, and the size of it all
@@ -615,7 +616,7 @@ struct Plan {
 
 rt_status plan_of(const rt_bsr* m, int32_t entries, Plan* out) {
     const int64_t rows = (int64_t)(m->n_masks > 1 ? m->n_masks : 1) * m->n_qblk;
-    const int64_t seg = std::max<int64_t>(32, 4 * ceil_div(entries, std::max<int64_t>(rows, 1)));
+    const int64_t seg = std::max<int64_t>(96, 4 * ceil_div(entries, std::max<int64_t>(rows, 1)));
     const int64_t splits = m->n_qblk > seg ? entries / seg : 0;
     if (rows + 2 * splits > INT32_MAX / 8) return fail(RT_EINVAL, "too many mask rows");
     out->seg = (int32_t)seg;

@@ -119,7 +119,7 @@ def test_sparse(gpu, D, block, T, masks, ratio):
 
 
 @pytest.mark.parametrize("D", [64, 72])
-@pytest.mark.parametrize("block,T,masks", [(32, 2300, 1), (32, 1500, 2), (32, 1111, 4), (64, 2700, 1), (64, 2139, 2)])
+@pytest.mark.parametrize("block,T,masks", [(32, 3300, 1), (32, 3211, 2), (32, 3130, 4), (64, 6211, 1)])
 def test_lists_that_are_split(gpu, D, block, T, masks):
     """A key block that every query block keeps: its list is walked in parts, which are joined."""
     print(f"[sparse backward, split] T={T} D={D} block={block} masks={masks}", flush=True)
@@ -235,6 +235,33 @@ def test_transposed_mask(gpu):
                 assert got_ci[at:at + len(ref)].tolist() == ref
                 at += len(ref)
             assert got_rp[m, n] == at
+
+
+@pytest.mark.parametrize("n,n_masks,keep", [(40, 2, 3), (97, 1, 2), (120, 3, 2), (300, 2, 60), (640, 1, 2), (700, 2, 3)])
+def test_the_plan_covers_every_list_once(gpu, n, n_masks, keep):
+    """Behind the entries: first parts, further parts, records of the split lists, whose parts are numbered in order."""
+    rp, ci = _masks(n, n_masks, keep, n, column=n // 3)
+    t = rt.BlockMask.from_csr(rp, ci, 64, n_masks=n_masks).transposed()
+    plan = t.col_idx[-(-len(ci) // 4) * 4:].cpu().numpy().reshape(-1, 4)
+    rows = t.row_ptr.cpu().numpy().reshape(n_masks, n + 1)
+    more = (len(plan) - n_masks * n) // 2
+    first, further, records = plan[:n_masks * n], plan[n_masks * n:n_masks * n + more], plan[n_masks * n + more:]
+    further = [tuple(x) for x in further if x[0] >= 0]
+    records = {x[0]: tuple(x[1:3]) for x in records if x[0] >= 0}
+    slots = []
+    for i, (row, at, count, slot) in enumerate(first):
+        b, e = rows[i // n, i % n], rows[i // n, i % n + 1]
+        parts = [(at, count, slot)] + [x[1:] for x in further if x[0] == i]
+        assert row == i and [x[0] for x in parts] == sorted(x[0] for x in parts)
+        assert b == at and sum(x[1] for x in parts) == e - b
+        assert all(x[0] + x[1] == y[0] for x, y in zip(parts, parts[1:]))
+        if len(parts) == 1:
+            assert slot == -1 and i not in records
+        else:
+            assert records[i] == (slot, len(parts)) and [x[2] for x in parts] == list(range(slot, slot + len(parts)))
+            slots += [x[2] for x in parts]
+    assert len(slots) == len(set(slots)) and all(0 <= x < 2 * more for x in slots)
+    assert len(records) == (n_masks if n > 96 and keep < 20 else 0) or keep >= 20
 
 
 def test_equal_calls_give_equal_bits(gpu):
