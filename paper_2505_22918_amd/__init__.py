@@ -224,24 +224,34 @@ class BlockMask:
     def transposed(self):
         """The mask's transpose as the gradient calls take it (rt_index_transpose): row kb lists the query
         blocks that keep key block kb.  Built on first use on the current stream and kept with the mask, so
-        that a mask of many steps is transposed once; under graph capture, unless it is known to be complete,
-        it is built anew as part of the graph and not kept.  n_masks > 1: masks that share entries of col_idx
-        (from_csr allows for them) do not fit and make the gradients dk and dv NaN."""
+        that a mask of many steps is transposed once.  It is built anew where torch's operators have written
+        the mask's arrays since, for a mask that a captured graph makes (its replays write another one), and,
+        as part of the graph, under capture before it is known to be complete.  A graph that takes a kept one
+        does not see later writes to the mask.  n_masks > 1: masks that share entries of col_idx (from_csr
+        allows for them) do not fit and make the gradients dk and dv NaN."""
         torch = _torch()
         kept = self.__dict__.get("_t")
-        if kept is not None and kept[1] is None:  # known to be complete
-            return kept[0]
+        raw, writes = _stream(self.row_ptr), self._writes()
+        if kept is not None:
+            if kept[3] != writes:
+                kept = None
+            elif kept[1] is None and kept[2] == raw:  # known to be complete, on the stream that its memory is of
+                return kept[0]
         with _on(self.row_ptr):
-            raw = _stream(self.row_ptr)
             capturing = torch.cuda.is_current_stream_capturing()
-            if kept is not None:
-                t, done, built_on = kept
-                if not capturing:
-                    if done.query():
-                        self.__dict__["_t"] = (t, None, None)
-                    elif raw != built_on:
-                        torch.cuda.current_stream().wait_event(done)
-                    return t
+            if kept is not None and not (capturing and kept[1] is not None):
+                t, done, built_on, _ = kept
+                if done is not None and done.query():
+                    done = None
+                    self.__dict__["_t"] = (t, None, built_on, writes)
+                if raw != built_on and not capturing:
+                    cur = torch.cuda.current_stream()
+                    if done is not None:
+                        cur.wait_event(done)
+                    # freed with the mask, its memory is not given out again before this stream's work has ended
+                    t.row_ptr.record_stream(cur)
+                    t.col_idx.record_stream(cur)
+                return t
             room = self.__dict__.get("_entries", self.nnz)
             row_ptr = torch.empty_like(self.row_ptr)
             lib, values = _lib.load(), ctypes.c_int64(0)
@@ -251,11 +261,24 @@ class BlockMask:
             t = BlockMask(row_ptr, col_idx, self.block, self.n_qblk, int(room), self.n_masks)
             _lib.check("rt_index_transpose", lib.rt_index_transpose(
                 ctypes.byref(self.c_struct()), self.n_qblk * self.block, ctypes.byref(t.c_struct()), raw))
-            if not capturing:
+            if not capturing and "_of_graph" not in self.__dict__:
                 done = torch.cuda.Event()
                 done.record()
-                self.__dict__["_t"] = (t, done, raw)
+                self.__dict__["_t"] = (t, done, raw, writes)
         return t
+
+    def _writes(self):
+        """How often torch's operators have written the mask's arrays."""
+        try:
+            return self.row_ptr._version, self.col_idx._version
+        except RuntimeError:  # inference tensors do not count
+            return None
+
+    def _made(self):
+        """The mask, marked if a graph capture under way writes its arrays (on the current device)."""
+        if _torch().cuda.is_current_stream_capturing():
+            self.__dict__["_of_graph"] = True
+        return self
 
     @classmethod
     def from_csr(cls, row_ptr, col_idx, block, device="cuda", n_masks=1):
@@ -331,10 +354,11 @@ def build_index(T, block, kind, device="cuda", host_mask=None, **pat) -> BlockMa
     with _on(row_ptr):
         _lib.check("rt_index_build", lib.rt_index_build(ctypes.byref(p), int(T), int(block), _ptr(row_ptr),
                                                         _ptr(col_idx), int(nnz), _stream(row_ptr)))
+        built = BlockMask(row_ptr, col_idx[:nnz] if nnz else col_idx[:0], int(block), n_blk, int(nnz), n_masks)._made()
     if dmask is not None:
         # keep the mask alive until the build has run on the stream
         torch.cuda.current_stream(row_ptr.device).synchronize()
-    return BlockMask(row_ptr, col_idx[:nnz] if nnz else col_idx[:0], int(block), n_blk, int(nnz), n_masks)
+    return built
 
 
 def dynamic_index(q, k, block, keep) -> BlockMask:
@@ -359,9 +383,9 @@ def dynamic_index(q, k, block, keep) -> BlockMask:
         _lib.check("rt_dynamic_index", lib.rt_dynamic_index(_ptr(q), _ptr(k), dims, int(block), int(keep),
                                                             _ptr(row_ptr), _ptr(col_idx), int(nnz), _ptr(work),
                                                             int(ws.value), _stream(q)))
-    # `work` returns to torch's stream-ordered cache here; a later reuse on this
-    # stream runs after the launch that reads it
-    return BlockMask(row_ptr, col_idx[:nnz], int(block), n_blk, int(nnz), B * H)
+        # `work` returns to torch's stream-ordered cache here; a later reuse on this
+        # stream runs after the launch that reads it
+        return BlockMask(row_ptr, col_idx[:nnz], int(block), n_blk, int(nnz), B * H)._made()
 
 
 def attn_full(q, k, v, block=64, stats=True, out=None):
