@@ -168,6 +168,7 @@ struct NormArgs {
     int32_t n1, n2;
     int32_t flat;        // rows of every tensor are s[2] apart throughout
     uint32_t rows_per_set, sets;
+    uint32_t turn0;      // forward: workgroups of earlier launches
     int32_t width, type;
     int32_t vec;         // rows start on 16 bytes and hold whole chunks of 8 elements
     int32_t weight_f32;

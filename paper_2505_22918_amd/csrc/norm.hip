@@ -175,7 +175,7 @@ __global__ __launch_bounds__(threads_of(LPR)) void norm_fwd(NormArgs a) {
     __shared__ float lds[LPR > 64 ? 2 * U * (LPR / 64) : 1];
     const int lane = threadIdx.x % LPR;
     const uint32_t first = a.rows_per_set * blockIdx.y, end = first + a.rows_per_set;
-    const uint32_t row0 = first + blockIdx.x * (RPW * U) + threadIdx.x / LPR;
+    const uint32_t row0 = first + (a.turn0 + blockIdx.x) * (RPW * U) + threadIdx.x / LPR;
     float x[U][NV][VEC];
     bool there[NV];
 #pragma unroll
@@ -425,17 +425,23 @@ __global__ __launch_bounds__(1024) void norm_join(const float* partial, int32_t 
 // full; longer ones take a wave with more chunks, and over 2048 (512) a workgroup, whose registers would else not
 // hold a row and its column sums.
 template <int TYPE, bool BWD, int VEC, int LPR, int NV>
-hipError_t launch(const NormArgs& a, uint32_t parts, hipStream_t stream) {
+hipError_t launch(NormArgs a, uint32_t parts, hipStream_t stream) {
     constexpr int NT = threads_of(LPR);
     constexpr uint32_t RPT = NT / LPR * (BWD ? bwd_rows(VEC, NV) : rows_at_once(VEC, NV));  // rows of a workgroup's turn
     const uint32_t turns = (a.rows_per_set + RPT - 1) / RPT;
-    if (BWD)
-        hipLaunchKernelGGL((norm_bwd<TYPE, VEC, LPR, NV>), dim3(turns < parts ? turns : parts, a.sets), dim3(NT), 0,
-                           stream, a);
-    else
-        hipLaunchKernelGGL((norm_fwd<TYPE, VEC, LPR, NV>), dim3(turns, a.sets), dim3(NT), 0, stream, a);
+    if (!BWD) {  // (a launch has less than 2^32 threads)
+        constexpr uint32_t MOST = (1u << 31) / NT;
+        for (a.turn0 = 0; a.turn0 < turns; a.turn0 += MOST) {
+            const uint32_t n = turns - a.turn0 < MOST ? turns - a.turn0 : MOST;
+            hipLaunchKernelGGL((norm_fwd<TYPE, VEC, LPR, NV>), dim3(n, a.sets), dim3(NT), 0, stream, a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+    hipLaunchKernelGGL((norm_bwd<TYPE, VEC, LPR, NV>), dim3(turns < parts ? turns : parts, a.sets), dim3(NT), 0, stream, a);
     hipError_t e = hipGetLastError();
-    if (BWD && e == hipSuccess && turns > 1 && parts > 1 && (a.dweight || a.dbias)) {
+    if (e == hipSuccess && turns > 1 && parts > 1 && (a.dweight || a.dbias)) {
         hipLaunchKernelGGL(norm_join, dim3((2 * a.width + 15) / 16, a.sets), dim3(1024), 0, stream, a.partial,
                            (int32_t)(turns < parts ? turns : parts), a.width, a.dweight, a.dbias);
         e = hipGetLastError();
