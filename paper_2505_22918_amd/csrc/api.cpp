@@ -618,7 +618,8 @@ rt_status plan_of(const rt_bsr* m, int32_t entries, Plan* out) {
     const int64_t rows = (int64_t)(m->n_masks > 1 ? m->n_masks : 1) * m->n_qblk;
     const int64_t seg = std::max<int64_t>(96, 4 * ceil_div(entries, std::max<int64_t>(rows, 1)));
     const int64_t splits = m->n_qblk > seg ? entries / seg : 0;
-    if (rows + 2 * splits > INT32_MAX / 8) return fail(RT_EINVAL, "too many mask rows");
+    // the plan's int32 places, and a wave for each row in a launch of less than 2^32 threads
+    if (rows + 2 * splits > INT32_MAX / 8 || rows >= (int64_t)1 << 26) return fail(RT_EINVAL, "too many mask rows");
     out->seg = (int32_t)seg;
     out->max_more = (int32_t)splits;
     out->max_slots = (int32_t)(2 * splits);
@@ -667,6 +668,8 @@ rt_status grad_args(const void* q, const void* k, const void* v, const void* o, 
     RT_TRY(check_tensor(workspace, "workspace"));
     if (workspace_bytes < need)
         return fail(RT_ECAPACITY, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+    if ((int64_t)d.B * d.H * whole64(d.T) >= (int64_t)1 << 29)  // 8 threads a row, in one launch
+        return fail(RT_EINVAL, "too many rows: B=%d H=%d T=%d", d.B, d.H, d.T);
     rt::GradArgs a{};
     a.q = static_cast<const uint16_t*>(q);
     a.k = static_cast<const uint16_t*>(k);
@@ -896,8 +899,8 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     RT_TRY(plan_of(mask, t->nnz, &p));
     const int64_t need = backward_workspace(dims, mask, p), bh = (int64_t)dims.B * dims.H;
     const int64_t uses = bh / (mask->n_masks > 1 ? mask->n_masks : 1);
-    if (uses * p.max_more + 2 * bh * mask->n_qblk + 32 > INT32_MAX)
-        return fail(RT_EINVAL, "too many key blocks");
+    if ((uses * p.max_more + 2 * bh * mask->n_qblk + 32) * 2 * mask->block >= (int64_t)1 << 32)
+        return fail(RT_EINVAL, "too many key blocks");  // 2 * block threads each, in one launch
     rt::GradArgs a{};
     RT_TRY(grad_args(q, k, v, o, row_max, row_sum, d_o, dims, dq, dk, dv, workspace, workspace_bytes, need, &a));
     const int64_t np = mask_ptr_bytes(mask), nc = (int64_t)mask->nnz * 4;
