@@ -189,9 +189,13 @@ __device__ __forceinline__ void sparse_walk(const GradArgs& a, lds_u8* lds, int 
 // W: waves of a block (32 rows each).  Workgroups: the further parts of split lists, dK and dV of every block, then dQ,
 // so that what takes longest begins first.  (A block's dK and dV next to its dQ, which reads the same rows, was no
 // faster at the CogVideoX shape and 20 % slower where the lists are random.)
+//
+// Three waves to a SIMD where two share a ring.  A lone wave's ring leaves room for two by LDS; in the registers of three
+// the 72-wide walk's sums go through the accumulator file (32 heads of 4096 tokens, 9 kept blocks of 32: 84 against 75
+// us with all 512 registers for two; 1024 tokens 30.5 against 26.2; 64-wide ones equal).
 template <int D, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(3, 3))) void grad_sparse(
-    GradArgs a, int more, int n_items, int per_xcd) {
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 1 ? 2 : 3, W == 1 ? 2 : 3))) void
+grad_sparse(GradArgs a, int more, int n_items, int per_xcd) {
     __shared__ __attribute__((aligned(1024))) unsigned char smem[GradRing<D, true, W, 32, kStages>::LDS];
     lds_u8* const lds = (lds_u8*)smem;
     const csr_ptr plan = (csr_ptr)a.plan;

@@ -14,11 +14,14 @@
 // 72-wide heads: the 8 dims past 64 take one k-step of the scores, half of it zeros in both operands, and one
 // 16x16x32 product for 16 own rows of the gradients.
 //
-// A wave takes 197 to 243 registers, so that two share a SIMD and one's products run under the other's exponentials.
-// Measured against one wave of 64 rows to a SIMD, half the LDS reads a product, whose tiles ran half a step apart as
-// in attn_tiles.h: CogVideoX dK and dV 10.1 -> 9.1 ms, dQ 7.2 -> 6.6 ms (that wave's 456 registers lie half in the
-// accumulator file, from where the vector unit has to copy every score); 72-wide heads did not fit it.  The same half
-// step within these waves: 8.9 and 6.6 ms, and spills for 72-wide heads; not kept.
+// 32 own rows, so that two or three waves share a SIMD and one's products run under another's exponentials.  Measured
+// against one wave of 64 rows to a SIMD, half the LDS reads a product, whose tiles ran half a step apart as in
+// attn_tiles.h (CogVideoX, two waves): dK and dV 10.1 -> 9.1 ms, dQ 7.2 -> 6.6 ms (that wave's 456 registers lie half in
+// the accumulator file, from where the vector unit has to copy every score); 72-wide heads did not fit it.  The same
+// half step within these waves: 8.9 and 6.6 ms, and spills for 72-wide heads; not kept.  64 queries a wave for dQ alone,
+// whose sums take half the registers: 6.5 ms in a launch of its own, no less than its share of the common one.  The
+// chunk's code once for chunks with rows past the end and once for the others: the compiler spills 49 registers of the
+// 168 (26 ms for 15).
 #pragma once
 
 #include "attn_common.h"
