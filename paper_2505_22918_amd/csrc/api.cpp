@@ -14,6 +14,7 @@
 
 #include "../../include/rettention.h"
 #include "kernels.h"
+#include "train.h"
 
 namespace {
 

@@ -15,7 +15,7 @@
 
 #include "attn_common.h"
 #include "attn_grad_tiles.h"
-#include "kernels.h"
+#include "train.h"
 
 namespace rt {
 namespace {

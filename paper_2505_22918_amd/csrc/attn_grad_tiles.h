@@ -25,7 +25,7 @@
 #pragma once
 
 #include "attn_common.h"
-#include "kernels.h"
+#include "train.h"
 
 namespace rt {
 namespace {

@@ -20,6 +20,7 @@
 #include <stdint.h>
 
 #include "kernels.h"
+#include "train.h"
 
 namespace rt {
 namespace {
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(kThreads) void row_fill(IndexArgs a) {
 // ---- transpose of a block mask -------------------------------------------------------------
 //
 // Row kb of the transposed mask lists the query blocks whose rows hold kb, ascending, and a plan says how the
-// gradients' call splits long rows (kernels.h).
+// gradients' call splits long rows (train.h).
 //
 // Up to kSmall blocks: one workgroup to a mask sets a bit for each entry in LDS, and a thread to a key block counts its
 // row of bits and writes it out in order.  Masks keep their places by what row_ptr says they hold.  More blocks: one

@@ -4,7 +4,7 @@
 #include <cstdio>
 #include <cstdlib>
 
-#include "kernels.h"
+#include "train.h"
 
 #define EXPECT(c)                                                                  \
     do {                                                                           \
