@@ -606,27 +606,43 @@ rt_status check_transposed(const rt_bsr* t, const rt_bsr* m) {
     return RT_OK;
 }
 
-// How the lists of a transposed mask with room for `entries` are split over workgroups: after `seg` entries, four times
-// the mean list and 96 at least, so that few are and none holds the others up; and what the plan and the parts of split
-// lists take at most.  CogVideoX-2B, whose four text blocks are kept by all 278 query blocks: parts of 36 entries
-// 630 us and 22 for their sums, of 96 595 and 9.5, of 128 593 and 9.
+// How the lists of a transposed mask with room for `entries` are split over workgroups, so that no long one (a text
+// block's, which all query blocks keep) holds a call up: after `seg` entries, twice the mean list and 16 at least, in
+// masks of more than 40 blocks; and what the plan and the parts of split lists take at most.  Where nothing is split,
+// that the plan could be costs a launch for the sums: 12 heads of 83 blocks with random lists 52.4 us without, 53.3 with;
+// of 55 blocks, four of them text's, 87 and 52.
 struct Plan {
-    int32_t seg, max_more, max_slots;
+    int32_t seg, max_more, max_base;  // entries of a part; parts beyond the first ones, and numbers of parts, at most
     int64_t first, values;  // the plan's place behind the entries, and the size of it all
+    int32_t fold = 1, max_slots = 0;  // of a gradient call
 };
 
 rt_status plan_of(const rt_bsr* m, int32_t entries, Plan* out) {
     const int64_t rows = (int64_t)(m->n_masks > 1 ? m->n_masks : 1) * m->n_qblk;
-    const int64_t seg = std::max<int64_t>(96, 4 * ceil_div(entries, std::max<int64_t>(rows, 1)));
+    const int64_t seg = m->n_qblk <= 40 ? std::max(m->n_qblk, 1)
+                                        : std::max<int64_t>(16, 2 * ceil_div(entries, std::max<int64_t>(rows, 1)));
     const int64_t splits = m->n_qblk > seg ? entries / seg : 0;
     // the plan's int32 places, and a wave for each row in a launch of less than 2^32 threads
     if (rows + 2 * splits > INT32_MAX / 8 || rows >= (int64_t)1 << 26) return fail(RT_EINVAL, "too many mask rows");
     out->seg = (int32_t)seg;
     out->max_more = (int32_t)splits;
-    out->max_slots = (int32_t)(2 * splits);
+    out->max_base = (int32_t)(2 * splits);
     out->first = ceil_div(entries, 4) * 4;
     out->values = out->first + 4 * (rows + 2 * splits);
     return RT_OK;
+}
+
+// How many parts a workgroup of the gradient call takes together: as many as keep a list's share below what each of
+// the workgroups that run at once (six to a CU) walks in the call.  Fewer cost more sums than they gain, more hold the
+// call up: CogVideoX-2B with two samples (four text blocks kept by all 278) 630 us and 22 for the sums with parts of 36
+// entries, 595 and 9.5 with 96; one head of it, all in all, 66 us in parts of 36, 53 in parts of 16 and 139 of 96.
+void fold_parts(const rt_dims& d, const rt_bsr* m, Plan* p) {
+    const int64_t kept = (int64_t)d.B * d.H / (m->n_masks > 1 ? m->n_masks : 1) * m->nnz;
+    p->fold = (int32_t)std::max<int64_t>(1, std::min(kept / 1536 / p->seg, ceil_div(m->n_qblk, p->seg)));
+    if ((int64_t)p->fold * p->seg >= m->n_qblk)  // no list is longer
+        p->max_more = p->max_slots = 0;
+    else
+        p->max_slots = p->fold > 1 ? 2 * p->max_base / p->fold : p->max_base;
 }
 
 int64_t mask_ptr_bytes(const rt_bsr* m) {
@@ -877,6 +893,7 @@ rt_status rt_attn_sparse_backward_workspace(rt_dims dims, const rt_bsr* mask, in
     if (entries < mask->nnz) return fail(RT_ECAPACITY, "room for %d entries, the mask has %d", entries, mask->nnz);
     Plan p{};
     RT_TRY(plan_of(mask, entries, &p));
+    fold_parts(dims, mask, &p);
     *bytes = backward_workspace(dims, mask, p);
     return ok();
 }
@@ -898,6 +915,7 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D;
     Plan p{};
     RT_TRY(plan_of(mask, t->nnz, &p));
+    fold_parts(dims, mask, &p);
     const int64_t need = backward_workspace(dims, mask, p), bh = (int64_t)dims.B * dims.H;
     const int64_t uses = bh / (mask->n_masks > 1 ? mask->n_masks : 1);
     if ((uses * p.max_more + 2 * bh * mask->n_qblk + 32) * 2 * mask->block >= (int64_t)1 << 32)
@@ -918,7 +936,11 @@ rt_status rt_attn_sparse_backward(const void* q, const void* k, const void* v, c
     a.t_col_idx = t->col_idx;
     a.t_nnz = t->nnz;
     a.plan = t->col_idx + p.first;
+    a.t_row_ptr = t->row_ptr;
+    a.seg = p.seg;
     a.max_more = p.max_more;
+    a.fold = p.fold;
+    a.max_base = p.max_base;
     a.max_slots = p.max_slots;
     a.part = a.row_vals + bh * 2 * a.T64;
     a.n_masks = mask->n_masks > 1 ? mask->n_masks : 1;

@@ -186,6 +186,13 @@ __device__ __forceinline__ void sparse_walk(const GradArgs& a, lds_u8* lds, int 
     t.store_all(a, head_off, row0, T);
 }
 
+// Where the parts of a list whose numbers in the plan begin with `base` lie.  Taken `fold` at a time, n of them (more
+// than fold) need n / fold places, rounded up: at most 2 n / fold, rounded down.
+__device__ __forceinline__ int part_place(const GradArgs& a, int base) {
+    base = base < a.max_base ? base : a.max_base;
+    return a.fold > 1 ? 2 * base / a.fold : base;
+}
+
 // W: waves of a block (32 rows each).  Workgroups: the further parts of split lists, dK and dV of every block, then dQ,
 // so that what takes longest begins first.  (A block's dK and dV next to its dQ, which reads the same rows, was no
 // faster at the CogVideoX shape and 20 % slower where the lists are random.)
@@ -201,10 +208,18 @@ grad_sparse(GradArgs a, int more, int n_items, int per_xcd) {
     const csr_ptr plan = (csr_ptr)a.plan;
     int bh, blk, m, item;
     if ((int)blockIdx.x < more) {
-        const int rep = blockIdx.x / a.max_more, i = blockIdx.x - rep * a.max_more;
-        item = a.n_masks * a.n_blk + i;
-        const int row = plan[4 * item];
-        if (row < 0 || row >= a.n_masks * a.n_blk) return;
+        // every fold-th part of a list is one to begin with, so that of `fold` items in a row at most one is
+        const int each = (a.max_more + a.fold - 1) / a.fold, rep = blockIdx.x / each;
+        const int i0 = (blockIdx.x - rep * each) * a.fold, i1 = i0 + a.fold < a.max_more ? i0 + a.fold : a.max_more;
+        int row = -1;
+        item = a.n_masks * a.n_blk + i0 - 1;
+        for (int i = i0; i < i1 && row < 0; ++i) {
+            row = plan[4 * ++item];
+            if (row < 0 || row >= a.n_masks * a.n_blk) return;  // no more items
+            const int nth = plan[4 * item + 3] - plan[4 * row + 3];
+            if (nth < 1 || nth % a.fold) row = -1;
+        }
+        if (row < 0) return;
         m = row / a.n_blk;
         blk = row - m * a.n_blk;
         bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
@@ -226,8 +241,18 @@ grad_sparse(GradArgs a, int more, int n_items, int per_xcd) {
     } else if (plan[4 * item + 1] >= 0) {
         // (clamped to their arrays, as the CSR is: whatever t holds, nothing else is read or written)
         const csr_ptr p = plan + 4 * item;
-        const int first = p[1] < a.t_nnz ? p[1] : a.t_nnz, slot = p[3] < a.max_slots ? p[3] : -1;
-        const int count = p[2] < 0 ? 0 : (p[2] < a.t_nnz - first ? p[2] : a.t_nnz - first);
+        const int first = p[1] < a.t_nnz ? p[1] : a.t_nnz, base = plan[4 * (m * a.n_blk + blk) + 3];
+        int slot = p[3] < 0 || base < 0 || p[3] < base ? -1 : part_place(a, base) + (p[3] - base) / a.fold, count = p[2];
+        if (slot >= 0 && a.fold > 1) {
+            const int left = a.t_row_ptr[m * (a.n_blk + 1) + blk + 1] - first;
+            count = a.seg * a.fold;
+            if (left <= count) {
+                count = left;
+                if (p[3] == base) slot = -1;  // all of the list
+            }
+        }
+        slot = slot < a.max_slots ? slot : -1;
+        count = count < 0 ? 0 : (count < a.t_nnz - first ? count : a.t_nnz - first);
         const int rep = a.n_masks == 1 ? bh : (a.n_masks == a.heads ? bh / a.heads : 0);
         sparse_walk<D, true, W>(a, lds, bh, blk, a.t_col_idx + first, count,
                                 slot < 0 ? nullptr : a.part + ((size_t)rep * a.max_slots + slot) * (2 * 32 * W * D));
@@ -240,15 +265,15 @@ grad_sparse(GradArgs a, int more, int n_items, int per_xcd) {
 
 // dK (blockIdx.y 0) or dV of one split key block: its parts in order
 template <int D, int W>
-__global__ __launch_bounds__(256) void grad_join(GradArgs a) {
-    const int rep = blockIdx.x / a.max_more, i = blockIdx.x - rep * a.max_more;
+__device__ __forceinline__ void join_list(const GradArgs& a, int rep, int i) {
     const csr_ptr p = (csr_ptr)a.plan + 4 * (a.n_masks * a.n_blk + a.max_more + i);
     const int row = p[0];
-    if (row < 0 || row >= a.n_masks * a.n_blk || p[1] < 0 || p[2] < 1 || p[2] > a.max_slots - p[1]) return;
-    const int m = row / a.n_blk, blk = row - m * a.n_blk, n = p[2];
+    if (row < 0 || row >= a.n_masks * a.n_blk || p[1] < 0 || p[2] <= a.fold || p[2] > a.max_base) return;
+    const int m = row / a.n_blk, blk = row - m * a.n_blk, first = part_place(a, p[1]), n = (p[2] + a.fold - 1) / a.fold;
+    if (n > a.max_slots - first) return;
     const int bh = a.n_masks == 1 ? rep : (a.n_masks == a.heads ? rep * a.heads + m : m);
     constexpr int SIZE = 32 * W * D;
-    const float* part = a.part + ((size_t)rep * a.max_slots + p[1]) * (2 * SIZE) + blockIdx.y * SIZE;
+    const float* part = a.part + ((size_t)rep * a.max_slots + first) * (2 * SIZE) + blockIdx.y * SIZE;
     uint16_t* out = (blockIdx.y ? a.dv : a.dk) + (size_t)bh * (size_t)a.T * D + (size_t)blk * SIZE;
     const int left = a.T - blk * 32 * W, size = (left < 32 * W ? left : 32 * W) * D;
     for (int j = threadIdx.x * 4; j < size; j += 1024) {
@@ -258,10 +283,15 @@ __global__ __launch_bounds__(256) void grad_join(GradArgs a) {
         reinterpret_cast<uint32_t*>(out + j)[1] = pack_bf16(s[2], s[3]);
     }
 }
+template <int D, int W>
+__global__ __launch_bounds__(256) void grad_join(GradArgs a) {
+    const int each = (a.max_more + a.fold - 1) / a.fold, rep = blockIdx.x / each;
+    for (int i = blockIdx.x - rep * each; i < a.max_more; i += each) join_list<D, W>(a, rep, i);
+}
 
 template <int D, int W>
 hipError_t launch_sparse(const GradArgs& a, hipStream_t stream) {
-    const int rep = a.n_bh / a.n_masks, more = rep * a.max_more, n = a.n_bh * a.n_blk, per = (n + 7) / 8;
+    const int rep = a.n_bh / a.n_masks, more = rep * ((a.max_more + a.fold - 1) / a.fold), n = a.n_bh * a.n_blk, per = (n + 7) / 8;
     hipLaunchKernelGGL((grad_sparse<D, W>), dim3(more + 16 * per), dim3(64 * W), 0, stream, a, more, n, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || more == 0) return e;

@@ -44,9 +44,12 @@ struct GradArgs {
     uint16_t* dv;
     float* row_vals;    // workspace [B,H][2][T64]: log2 of the denominator over the row's factor, and -dO . O
     int32_t T64;        // T in whole 64
-    float* part;        // workspace: fp32 dK and dV [slot][2][block][D] of split lists, max_slots for each use of a mask
+    float* part;        // workspace: fp32 dK and dV [place][2][block][D] of split lists, max_slots for each use of a mask
     const int32_t* plan;  // of the transposed mask
-    int32_t t_nnz, max_more, max_slots;
+    int32_t t_nnz, seg, max_more;
+    int32_t fold;       // parts of a split list that a workgroup takes together
+    int32_t max_base, max_slots;  // part numbers of the plan; places in `part`
+    const int32_t* t_row_ptr;
     const int32_t* row_ptr;  // null: dense
     const int32_t* col_idx;
     const int32_t* t_col_idx;

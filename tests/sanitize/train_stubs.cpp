@@ -19,7 +19,7 @@ namespace rt {
 hipError_t launch_index_transpose(const TransposeArgs& a, hipStream_t) {
     EXPECT(a.row_ptr && a.col_idx && a.t_row_ptr && a.t_col_idx);
     EXPECT(a.n_blk > 0 && a.n_masks > 0 && a.nnz > 0 && a.t_nnz >= a.nnz);
-    EXPECT(a.plan >= a.t_col_idx + a.t_nnz && a.seg >= 32 && a.max_more >= 0);
+    EXPECT(a.plan >= a.t_col_idx + a.t_nnz && a.seg >= 1 && a.max_more >= 0);
     return hipSuccess;
 }
 
@@ -32,7 +32,8 @@ hipError_t launch_attention_backward(const GradArgs& a, int D, hipStream_t) {
     if (a.row_ptr) {
         EXPECT(a.col_idx && a.t_col_idx && a.plan > a.t_col_idx && a.nnz > 0);
         EXPECT(a.n_blk == (a.T + a.block - 1) / a.block && a.n_bh % a.n_masks == 0);
-        EXPECT(a.max_slots == 2 * a.max_more);
+        EXPECT(a.fold >= 1 && a.seg >= 1 && a.t_row_ptr && a.max_slots <= a.max_base);
+        EXPECT(a.max_more ? a.max_slots >= 2 * a.max_more / a.fold : a.max_slots == 0);
         EXPECT((char*)a.part >= (char*)(a.row_vals + 2 * (size_t)a.n_bh * a.T64) && ((uintptr_t)a.part & 15) == 0);
         EXPECT((a.block == 32 || a.block == 64) && a.n_masks >= 1);
     }

@@ -264,6 +264,28 @@ def test_the_plan_covers_every_list_once(gpu, n, n_masks, keep):
     assert len(records) == (n_masks if n > 96 and keep < 20 else 0) or keep >= 20
 
 
+@pytest.mark.parametrize("D,block,n,H,masks", [(64, 32, 101, 160, 1), (72, 64, 101, 150, 1), (64, 64, 101, 96, 96),
+                                               (72, 32, 101, 100, 200), (64, 32, 41, 500, 1)])
+def test_parts_that_are_taken_together(gpu, D, block, n, H, masks):
+    """Many heads: a workgroup takes two and more parts of a list together, or a list whole.  Some heads of them against
+    the oracle."""
+    B = 2 if masks > 1 else 1
+    T = n * block - 5
+    rp, ci = _masks(n, masks, 3, D + H, column=n - 2)
+    kept = B * H * len(ci) // masks
+    assert kept // 1536 >= 2 * 16, "a call that folds its parts"
+    mask = rt.BlockMask.from_csr(rp, ci, block, n_masks=masks)
+    dev, host = _inputs(B, H, T, D, D + block)
+    stats = rt.attn_sparse(*dev[:3], mask)
+    out = rt.attn_sparse_backward(*dev[:3], *stats, dev[3], mask)
+    rows = rp.reshape(masks, n + 1)
+    for b, h in ((0, 0), (B - 1, H // 2), (B - 1, H - 1)):
+        one = lambda x: x[b:b + 1, h:h + 1]  # noqa: E731
+        row = rows[0 if masks == 1 else (h if masks == H else b * H + h)]
+        _compare([one(x) for x in host], [one(x) for x in stats], [one(x) for x in out],
+                 lambda *_: og.token_mask(row, ci, block, T))
+
+
 def test_equal_calls_give_equal_bits(gpu):
     import torch
 
