@@ -665,10 +665,22 @@ rt_status check_ranges(std::initializer_list<std::pair<range, const char*>> outs
 
 int32_t whole64(int32_t T) { return (int32_t)ceil_div(T, 64) * 64; }
 
-// Row values, and the parts of split lists.
+// Workgroups that share the walk of a tile of dense gradients.  Where there are few tiles, as many as fill the CUs once
+// (a tile has two walks; twice where they are 64 stages of 64 rows and more), each with 4 stages at least, if that takes
+// the time of 8 stages, about a microsecond each, off a walk: the sums are a launch of their own.  One head of 1175
+// tokens 26 -> 19 us, of 2734 50 -> 27 (30 with two workgroups to a CU), two of 8192 141 -> 127.
+int32_t dense_split(const rt_dims& d) {
+    const int64_t n = (int64_t)d.B * d.H * ceil_div(d.T, rt::kDenseRows), stages = ceil_div(d.T, 64);
+    const int64_t s = std::min((stages >= 64 ? 256 : 128) / std::max<int64_t>(n, 1), stages / 4);
+    return s > 1 && stages - ceil_div(stages, s) >= 8 ? (int32_t)s : 1;
+}
+
+// Row values, and the parts of split lists or walks.
 int64_t backward_workspace(const rt_dims& d, const rt_bsr* m, const Plan& p) {
-    const int64_t uses = m ? (int64_t)d.B * d.H / (m->n_masks > 1 ? m->n_masks : 1) : 0;
-    return (int64_t)d.B * d.H * whole64(d.T) * 8 + (m ? uses * p.max_slots * 2 * m->block * d.D * 4 : 0);
+    const int64_t bh = (int64_t)d.B * d.H, values = bh * whole64(d.T) * 8;
+    if (m) return values + bh / (m->n_masks > 1 ? m->n_masks : 1) * p.max_slots * 2 * m->block * d.D * 4;
+    const int64_t split = dense_split(d);
+    return values + (split > 1 ? split * bh * ceil_div(d.T, rt::kDenseRows) * 3 * rt::kDenseRows * d.D * 4 : 0);
 }
 
 // What the dense and the sparse gradient call check and set alike (rho and the mask aside).
@@ -878,6 +890,8 @@ rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, con
     const int64_t need = backward_workspace(dims, nullptr, Plan{});
     rt::GradArgs a{};
     RT_TRY(grad_args(q, k, v, o, row_max, row_sum, d_o, dims, dq, dk, dv, workspace, workspace_bytes, need, &a));
+    a.split = dense_split(dims);
+    a.part = a.row_vals + (int64_t)dims.B * dims.H * 2 * a.T64;
     RT_TRY(check_ranges({{{dq, nt}, "dq"}, {{dk, nt}, "dk"}, {{dv, nt}, "dv"}, {{workspace, need}, "workspace"}},
                         {{q, nt}, {k, nt}, {v, nt}, {o, nt}, {d_o, nt}, {row_max, ns}, {row_sum, ns}}));
     return hip_status(rt::launch_attention_backward(a, dims.D, static_cast<hipStream_t>(stream)),

@@ -5,6 +5,7 @@
 //   grad_dense   dK and dV of 128 keys, or dQ of 128 queries, to a workgroup of four waves
 //   grad_sparse  the same for one block, over the blocks its row of the (transposed) mask lists
 //   grad_join    sums of the parts of key blocks whose lists were split
+//   grad_sum     the same of dense tiles whose walks are shared, where there are few
 //
 // Seven products of T x T x D instead of the five that the gradients need: the scores and dP are formed for dK and dV
 // and again for dQ, so that every sum stays in one wave's registers: no atomics, equal bits from equal calls.
@@ -59,9 +60,10 @@ constexpr int kStages = 2;
 // which saves the launch of grad_rows.
 constexpr int kShort = 512;
 
-// dK and dV (KV) or dQ of 32 W rows of a head against all of the other side: stages 0, 1, .. of 64 rows.
-template <int D, bool KV, int W, bool SHORT>
-__device__ __forceinline__ void dense_walk(const GradArgs& a, lds_u8* lds, int item) {
+// dK and dV (KV) or dQ of 32 W rows of a head against all of the other side: stages 0, 1, .. of 64 rows.  SPLIT: against
+// one of a.split parts of it, whose fp32 sums grad_sum adds.
+template <int D, bool KV, int W, bool SHORT, bool SPLIT>
+__device__ __forceinline__ void dense_walk(const GradArgs& a, lds_u8* lds, int item, int part) {
     using R = GradRing<D, KV && !SHORT, W, 64, kStages>;
     const int T = a.T, n64 = (T + 63) >> 6, n_tile = (T + 32 * W - 1) / (32 * W);
     const int bh = item / n_tile;
@@ -70,7 +72,8 @@ __device__ __forceinline__ void dense_walk(const GradArgs& a, lds_u8* lds, int i
     R ring;
     ring.init(lds, (KV ? a.q : a.k) + head_off, (KV ? a.d_o : a.v) + head_off, a.row_vals + (size_t)bh * 2 * a.T64, T,
               a.T64);
-    ring.load(0, 0);
+    const int s0 = SPLIT ? n64 * part / a.split : 0, s1 = SPLIT ? n64 * (part + 1) / a.split : n64;
+    ring.load(0, s0 * 64);
     GradTile<D, KV, R::ZERO, R::TENSOR> t;
     t.init(lds, a.scale_log2);
     t.load_own(a, head_off, row0, T);
@@ -97,7 +100,7 @@ __device__ __forceinline__ void dense_walk(const GradArgs& a, lds_u8* lds, int i
             t.load_values(a, bh, row0, T);
     }
     int st = 0;  // LDS offset of the stage in use
-    for (int s = 0; s < n64; ++s) {
+    for (int s = s0; s < s1; ++s) {
         ring.turn();
         ring.load(R::STAGE - st, (s + 1) * 64);
 #pragma unroll
@@ -111,10 +114,16 @@ __device__ __forceinline__ void dense_walk(const GradArgs& a, lds_u8* lds, int i
         st = R::STAGE - st;
     }
     wait_vm<0>();  // nothing may land in LDS after the workgroup has ended
+    if (SPLIT) {
+        float* to = a.part + ((size_t)item * a.split + part) * (3 * 32 * W * D) + (threadIdx.x >> 6) * 32 * D;
+        t.store_part(0, to + (KV ? 0 : 2 * 32 * W * D), a.scale_nat);
+        if (KV) t.store_part(KV ? 1 : 0, to + 32 * W * D, 1.0f);
+        return;
+    }
     t.store_all(a, head_off, row0, T);
 }
 
-template <int D, int W, int WAVES, bool SHORT>
+template <int D, int W, int WAVES, bool SHORT, bool SPLIT>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(WAVES, WAVES))) void grad_dense(GradArgs a,
                                                                                                       int n_items,
                                                                                                       int per_xcd) {
@@ -123,12 +132,38 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(WAVES, W
     // the first half of the workgroups, which has more to do, takes dK and dV
     const bool kv = (int)blockIdx.x < 8 * per_xcd;
     const int g = kv ? blockIdx.x : blockIdx.x - 8 * per_xcd;
-    const int item = (g & 7) * per_xcd + (g >> 3);
+    int item = (g & 7) * per_xcd + (g >> 3), part = 0;
     if (item >= n_items) return;
+    if (SPLIT) {
+        part = item % a.split;
+        item /= a.split;
+    }
     if (kv)
-        dense_walk<D, true, W, SHORT>(a, (lds_u8*)smem, item);
+        dense_walk<D, true, W, SHORT, SPLIT>(a, (lds_u8*)smem, item, part);
     else
-        dense_walk<D, false, W, SHORT>(a, (lds_u8*)smem, item);
+        dense_walk<D, false, W, SHORT, SPLIT>(a, (lds_u8*)smem, item, part);
+}
+
+// out[j .. j + 3], below size, from n parts STRIDE apart, in order; four of them asked for at a time
+template <int STRIDE>
+__device__ __forceinline__ void sum_parts(const float* part, int n, uint16_t* out, int j, int size) {
+    if (j >= size) return;
+    f32x4 s = {};
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) s += *reinterpret_cast<const f32x4*>(part + (size_t)k * STRIDE + j);
+    reinterpret_cast<uint32_t*>(out + j)[0] = pack_bf16(s[0], s[1]);
+    reinterpret_cast<uint32_t*>(out + j)[1] = pack_bf16(s[2], s[3]);
+}
+
+// dK, dV or dQ (blockIdx.y) of 32 W rows, 1024 values of them (blockIdx.z)
+template <int D, int W>
+__global__ __launch_bounds__(256) void grad_sum(GradArgs a) {
+    constexpr int SIZE = 32 * W * D;
+    const int n_tile = (a.T + 32 * W - 1) / (32 * W), bh = blockIdx.x / n_tile, row0 = (blockIdx.x - bh * n_tile) * 32 * W;
+    const float* part = a.part + (size_t)blockIdx.x * a.split * (3 * SIZE) + blockIdx.y * SIZE;
+    uint16_t* out = (blockIdx.y == 0 ? a.dk : blockIdx.y == 1 ? a.dv : a.dq) + ((size_t)bh * a.T + row0) * D;
+    const int left = a.T - row0, size = (left < 32 * W ? left : 32 * W) * D;
+    sum_parts<3 * SIZE>(part, a.split, out, blockIdx.z * 1024 + threadIdx.x * 4, size);
 }
 
 // ---- sparse --------------------------------------------------------------------------------
@@ -276,15 +311,10 @@ __device__ __forceinline__ void join_list(const GradArgs& a, int rep, int i) {
     const float* part = a.part + ((size_t)rep * a.max_slots + first) * (2 * SIZE) + blockIdx.y * SIZE;
     uint16_t* out = (blockIdx.y ? a.dv : a.dk) + (size_t)bh * (size_t)a.T * D + (size_t)blk * SIZE;
     const int left = a.T - blk * 32 * W, size = (left < 32 * W ? left : 32 * W) * D;
-    for (int j = threadIdx.x * 4; j < size; j += 1024) {
-        f32x4 s = *reinterpret_cast<const f32x4*>(part + j);
-        for (int k = 1; k < n; ++k) s += *reinterpret_cast<const f32x4*>(part + (size_t)k * 2 * SIZE + j);
-        reinterpret_cast<uint32_t*>(out + j)[0] = pack_bf16(s[0], s[1]);
-        reinterpret_cast<uint32_t*>(out + j)[1] = pack_bf16(s[2], s[3]);
-    }
+    for (int j = threadIdx.x * 4; j < size; j += 2048) sum_parts<2 * SIZE>(part, n, out, j, size);
 }
 template <int D, int W>
-__global__ __launch_bounds__(256) void grad_join(GradArgs a) {
+__global__ __launch_bounds__(512) void grad_join(GradArgs a) {
     const int each = (a.max_more + a.fold - 1) / a.fold, rep = blockIdx.x / each;
     for (int i = blockIdx.x - rep * each; i < a.max_more; i += each) join_list<D, W>(a, rep, i);
 }
@@ -295,13 +325,13 @@ hipError_t launch_sparse(const GradArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((grad_sparse<D, W>), dim3(more + 16 * per), dim3(64 * W), 0, stream, a, more, n, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || more == 0) return e;
-    hipLaunchKernelGGL((grad_join<D, W>), dim3(more, 2), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((grad_join<D, W>), dim3(more, 2), dim3(512), 0, stream, a);
     return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const GradArgs& a, hipStream_t stream) {
-    constexpr int W = 4;
+    constexpr int W = kDenseRows / 32;
     const int n = a.n_bh * ((a.T + 32 * W - 1) / (32 * W)), per = (n + 7) / 8;
     const bool few = n < 256;  // 2 n workgroups over 256 CUs
     if (a.row_ptr || a.T > kShort || !few) {
@@ -315,11 +345,17 @@ hipError_t launch_d(const GradArgs& a, hipStream_t stream) {
     // tokens).  64-wide heads fit three waves to a SIMD, which pays where there are as many (14.5 against 14.8 ms; 9.0
     // against 7.9 us where there are not: a wave with fewer registers waits more); 72-wide ones spill (819 against 533).
     if (!few)
-        hipLaunchKernelGGL((grad_dense<D, W, D == 64 ? 3 : 2, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
-    else if (a.T > kShort)
-        hipLaunchKernelGGL((grad_dense<D, W, 2, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
+        hipLaunchKernelGGL((grad_dense<D, W, D == 64 ? 3 : 2, false, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
+    else if (a.split > 1) {
+        const int all = n * a.split, each = (all + 7) / 8;
+        hipLaunchKernelGGL((grad_dense<D, W, 2, false, true>), dim3(16 * each), dim3(64 * W), 0, stream, a, all, each);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((grad_sum<D, W>), dim3(n, 3, kDenseRows * D / 1024), dim3(256), 0, stream, a);
+    } else if (a.T > kShort)
+        hipLaunchKernelGGL((grad_dense<D, W, 2, false, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
     else
-        hipLaunchKernelGGL((grad_dense<D, W, 2, true>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
+        hipLaunchKernelGGL((grad_dense<D, W, 2, true, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
     return hipGetLastError();
 }
 

@@ -28,6 +28,7 @@ struct TransposeArgs {
 __attribute__((weak)) hipError_t launch_index_transpose(const TransposeArgs& a, hipStream_t stream);
 
 // Gradients of attention (attn_grad.hip).
+constexpr int kDenseRows = 128;  // rows of a dense tile
 struct GradArgs {
     const uint16_t* q;  // bf16 [B,H,T,D]
     const uint16_t* k;
@@ -44,6 +45,7 @@ struct GradArgs {
     uint16_t* dv;
     float* row_vals;    // workspace [B,H][2][T64]: log2 of the denominator over the row's factor, and -dO . O
     int32_t T64;        // T in whole 64
+    int32_t split;      // dense: workgroups that share a tile's walk; more than 1: part is [tile][split][dK, dV, dQ][rows][D]
     float* part;        // workspace: fp32 dK and dV [place][2][block][D] of split lists, max_slots for each use of a mask
     const int32_t* plan;  // of the transposed mask
     int32_t t_nnz, seg, max_more;

@@ -29,6 +29,7 @@ hipError_t launch_attention_backward(const GradArgs& a, int D, hipStream_t) {
     EXPECT(a.row_vals && a.T64 >= a.T && a.T64 < a.T + 64 && a.T64 % 64 == 0);
     EXPECT(a.T > 0 && a.n_bh > 0 && (long long)a.T * D * 2 <= (1LL << 30));
     EXPECT(!a.d_rho || a.rho);
+    if (!a.row_ptr) EXPECT(a.split >= 1 && a.split <= a.T64 / 64 && a.part >= a.row_vals + 2 * (size_t)a.n_bh * a.T64);
     if (a.row_ptr) {
         EXPECT(a.col_idx && a.t_col_idx && a.plan > a.t_col_idx && a.nnz > 0);
         EXPECT(a.n_blk == (a.T + a.block - 1) / a.block && a.n_bh % a.n_masks == 0);

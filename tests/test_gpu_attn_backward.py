@@ -83,6 +83,16 @@ def test_full_long(gpu):
     _compare(host, stats, rt.attn_full_backward(*dev[:3], *stats, dev[3]))
 
 
+@pytest.mark.parametrize("H,T,D", [(1, 705, 64), (1, 1027, 72), (2, 1500, 64), (3, 1290, 72), (2, 2003, 72)])
+def test_full_few_heads(gpu, H, T, D):
+    """Few tiles: workgroups share a tile's walk, and the parts are added in order."""
+    dev, host = _inputs(1, H, T, D, T)
+    stats = rt.attn_full(*dev[:3])
+    out = rt.attn_full_backward(*dev[:3], *stats, dev[3])
+    _compare(host, stats, out)
+    assert all((x == y).all() for x, y in zip(out, rt.attn_full_backward(*dev[:3], *stats, dev[3])))
+
+
 @pytest.mark.parametrize("D", [64, 72])
 @pytest.mark.parametrize("block", [32, 64])
 @pytest.mark.parametrize("T,masks,ratio", [(1, 1, False), (33, 1, True), (64, 1, False), (65, "H", True),
