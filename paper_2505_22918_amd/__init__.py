@@ -225,29 +225,20 @@ class BlockMask:
         """The mask's transpose as the gradient calls take it (rt_index_transpose): row kb lists the query
         blocks that keep key block kb.  Built on first use on the current stream and kept with the mask, so
         that a mask of many steps is transposed once.  It is built anew where torch's operators have written
-        the mask's arrays since, for a mask that a captured graph makes (its replays write another one), and,
-        as part of the graph, under capture before it is known to be complete.  A graph that takes a kept one
-        does not see later writes to the mask.  n_masks > 1: masks that share entries of col_idx (from_csr
-        allows for them) do not fit and make the gradients dk and dv NaN."""
+        the mask's arrays since, for a mask that a captured graph makes (its replays write another one), and
+        in every capture, as part of the graph: a graph holds what it reads, and its replays follow the mask's
+        arrays as they are then.  n_masks > 1: masks that share entries of col_idx (from_csr allows for them)
+        do not fit and make the gradients dk and dv NaN."""
         torch = _torch()
-        kept = self.__dict__.get("_t")
         raw, writes = _stream(self.row_ptr), self._writes()
-        if kept is not None:
-            if kept[3] != writes:
-                kept = None
-            elif kept[1] is None and kept[2] == raw:  # known to be complete, on the stream that its memory is of
-                return kept[0]
         with _on(self.row_ptr):
             capturing = torch.cuda.is_current_stream_capturing()
-            if kept is not None and not (capturing and kept[1] is not None):
+            kept = None if capturing else self.__dict__.get("_t")
+            if kept is not None and kept[3] == writes:
                 t, done, built_on, _ = kept
-                if done is not None and done.query():
-                    done = None
-                    self.__dict__["_t"] = (t, None, built_on, writes)
-                if raw != built_on and not capturing:
+                if raw != built_on:
                     cur = torch.cuda.current_stream()
-                    if done is not None:
-                        cur.wait_event(done)
+                    cur.wait_event(done)
                     # freed with the mask, its memory is not given out again before this stream's work has ended
                     t.row_ptr.record_stream(cur)
                     t.col_idx.record_stream(cur)

@@ -1,0 +1,89 @@
+"""When a BlockMask keeps its transpose and when it builds another, with stand-ins for the device: no GPU needed."""
+
+import ctypes
+
+import pytest
+
+import paper_2505_22918_amd as rt
+
+
+class _Device:
+    """What the binding asks of the device: the current stream, whether it is captured, and the launches it was given."""
+
+    def __init__(self):
+        self.stream, self.capturing, self.idle = 1, False, False  # idle: all work has ended
+        self.built, self.waits, self.held = [], [], []
+
+    # the library
+    def rt_index_transpose_size(self, mask, room, values):
+        ctypes.cast(values, ctypes.POINTER(ctypes.c_int64))[0] = room + 64
+        return 0
+
+    def rt_index_transpose(self, mask, T, t, stream):
+        self.built.append((stream, self.capturing))
+        return 0
+
+
+@pytest.fixture
+def device(monkeypatch):
+    import contextlib
+
+    import torch
+
+    dev = _Device()
+
+    class Stream:
+        def wait_event(self, event):
+            dev.waits.append((dev.stream, event.at))
+
+    class Event:
+        def record(self, stream=None):
+            self.at = dev.stream
+
+        def query(self):
+            return dev.idle
+
+    monkeypatch.setattr(rt, "_stream", lambda t: dev.stream)
+    monkeypatch.setattr(rt, "_on", lambda t: contextlib.nullcontext())
+    monkeypatch.setattr(rt._lib, "load", lambda: dev)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: dev.capturing)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream())
+    monkeypatch.setattr(torch.cuda, "Event", Event)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: dev.held.append(t.data_ptr()))
+    return dev
+
+
+def _mask():
+    import torch
+
+    return rt.BlockMask(torch.arange(5, dtype=torch.int32), torch.arange(4, dtype=torch.int32), 64, 4, 4)
+
+
+def test_a_mask_of_many_steps_is_transposed_once(device):
+    mask = _mask()
+    t = mask.transposed()
+    assert mask.transposed() is t and device.built == [(1, False)] and not device.waits
+
+
+def test_another_stream_waits_and_holds_the_memory(device):
+    mask = _mask()
+    t = mask.transposed()
+    device.stream = 2
+    assert mask.transposed() is t and device.waits == [(2, 1)]
+    assert set(device.held) == {t.row_ptr.data_ptr(), t.col_idx.data_ptr()}
+
+
+def test_a_capture_builds_its_own(device):
+    """A graph keeps the addresses that its capture saw, a mask may replace the transpose it keeps: what a capture uses
+    is built by the graph, in the graph's memory."""
+    mask = _mask()
+    kept = mask.transposed()
+    device.idle, device.stream = True, 2
+    mask.transposed()
+    for stream in (1, 2):
+        device.stream, device.capturing = stream, True
+        t = mask.transposed()
+        assert t is not kept and t.col_idx.data_ptr() != kept.col_idx.data_ptr()
+        assert device.built[-1] == (stream, True)
+    device.stream, device.capturing = 1, False
+    assert mask.transposed() is kept and len(device.built) == 3
