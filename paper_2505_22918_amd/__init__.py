@@ -225,7 +225,7 @@ class BlockMask:
         """The mask's transpose as the gradient calls take it (rt_index_transpose): row kb lists the query
         blocks that keep key block kb.  Built on first use on the current stream and kept with the mask, so
         that a mask of many steps is transposed once.  It is built anew where torch's operators have written
-        the mask's arrays since, for a mask that a captured graph makes (its replays write another one), and
+        the mask's arrays since, where they do not count that (inference tensors), for a mask that a captured graph makes (its replays write another one), and
         in every capture, as part of the graph: a graph holds what it reads, and its replays follow the mask's
         arrays as they are then.  n_masks > 1: masks that share entries of col_idx (from_csr allows for them)
         do not fit and make the gradients dk and dv NaN."""
@@ -252,7 +252,7 @@ class BlockMask:
             t = BlockMask(row_ptr, col_idx, self.block, self.n_qblk, int(room), self.n_masks)
             _lib.check("rt_index_transpose", lib.rt_index_transpose(
                 ctypes.byref(self.c_struct()), self.n_qblk * self.block, ctypes.byref(t.c_struct()), raw))
-            if not capturing and "_of_graph" not in self.__dict__:
+            if not capturing and writes is not None and "_of_graph" not in self.__dict__:
                 done = torch.cuda.Event()
                 done.record()
                 self.__dict__["_t"] = (t, done, raw, writes)

@@ -87,3 +87,15 @@ def test_a_capture_builds_its_own(device):
         assert device.built[-1] == (stream, True)
     device.stream, device.capturing = 1, False
     assert mask.transposed() is kept and len(device.built) == 3
+
+
+def test_arrays_whose_writes_are_not_counted(device):
+    """Inference tensors have no version: nothing is kept that a write could leave behind."""
+    import torch
+
+    with torch.inference_mode():
+        mask = _mask()
+    first = mask.transposed()
+    with torch.inference_mode():
+        mask.col_idx.add_(0)
+    assert mask.transposed() is not first and len(device.built) == 2
