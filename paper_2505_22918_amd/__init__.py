@@ -112,6 +112,12 @@ class _on(object):
         return False
 
 
+def _capturing(t):
+    """Whether the current stream of t's device is being captured."""
+    with _on(t):
+        return _torch().cuda.is_current_stream_capturing()
+
+
 def _ptr(t):
     """Device address of t, or NULL for None (ctypes takes ints for void*)."""
     return t.data_ptr() if t is not None else None
@@ -212,6 +218,11 @@ class BlockMask:
     nnz: int
     n_masks: int = 1
 
+    def __post_init__(self):
+        # made under a capture: replays of the graph write the arrays
+        on_gpu = isinstance(self.row_ptr, _torch().Tensor) and self.row_ptr.is_cuda
+        self.__dict__["_of_graph"] = on_gpu and _capturing(self.row_ptr)
+
     def c_struct(self):
         """The rt_bsr view of this mask (built once: a mask is not modified after it is made)."""
         c = self.__dict__.get("_c")
@@ -223,19 +234,20 @@ class BlockMask:
 
     def transposed(self):
         """The mask's transpose as the gradient calls take it (rt_index_transpose): row kb lists the query
-        blocks that keep key block kb.  Built on first use on the current stream and kept with the mask, so
-        that a mask of many steps is transposed once.  It is built anew where torch's operators have written
-        the mask's arrays since, where they do not count that (inference tensors), for a mask that a captured graph makes (its replays write another one), and
-        in every capture, as part of the graph: a graph holds what it reads, and its replays follow the mask's
-        arrays as they are then.  n_masks > 1: masks that share entries of col_idx (from_csr allows for them)
-        do not fit and make the gradients dk and dv NaN."""
+        blocks that keep key block kb.  Built on the current stream.  It is kept with the mask, so that a mask of
+        many steps is transposed once, as long as no operator of torch has written the mask's arrays in place
+        (their version counters are 0): an operator in a captured graph counts once and writes at every replay.
+        Else, for a mask made under a capture, and for inference tensors, which have no counters, each call
+        builds another.  So does each capture, as part of the graph: a graph holds what it reads, and its replays
+        follow the mask's arrays as they are then.  n_masks > 1: masks that share entries of col_idx (from_csr
+        allows for them) do not fit and make the gradients dk and dv NaN."""
         torch = _torch()
-        raw, writes = _stream(self.row_ptr), self._writes()
+        raw, unwritten = _stream(self.row_ptr), self._unwritten()
         with _on(self.row_ptr):
             capturing = torch.cuda.is_current_stream_capturing()
-            kept = None if capturing else self.__dict__.get("_t")
-            if kept is not None and kept[3] == writes:
-                t, done, built_on, _ = kept
+            kept = self.__dict__.get("_t") if unwritten and not capturing else None
+            if kept is not None:
+                t, done, built_on = kept
                 if raw != built_on:
                     cur = torch.cuda.current_stream()
                     cur.wait_event(done)
@@ -252,24 +264,21 @@ class BlockMask:
             t = BlockMask(row_ptr, col_idx, self.block, self.n_qblk, int(room), self.n_masks)
             _lib.check("rt_index_transpose", lib.rt_index_transpose(
                 ctypes.byref(self.c_struct()), self.n_qblk * self.block, ctypes.byref(t.c_struct()), raw))
-            if not capturing and writes is not None and "_of_graph" not in self.__dict__:
+            if unwritten and not capturing:
                 done = torch.cuda.Event()
                 done.record()
-                self.__dict__["_t"] = (t, done, raw, writes)
+                self.__dict__["_t"] = (t, done, raw)
         return t
 
-    def _writes(self):
-        """How often torch's operators have written the mask's arrays."""
+    def _unwritten(self):
+        """Nothing has written the mask's arrays since they were allocated, as far as torch counts, nor does a graph
+        that made them."""
+        if self.__dict__["_of_graph"]:
+            return False
         try:
-            return self.row_ptr._version, self.col_idx._version
+            return self.row_ptr._version == 0 and self.col_idx._version == 0
         except RuntimeError:  # inference tensors do not count
-            return None
-
-    def _made(self):
-        """The mask, marked if a graph capture under way writes its arrays (on the current device)."""
-        if _torch().cuda.is_current_stream_capturing():
-            self.__dict__["_of_graph"] = True
-        return self
+            return False
 
     @classmethod
     def from_csr(cls, row_ptr, col_idx, block, device="cuda", n_masks=1):
@@ -345,11 +354,10 @@ def build_index(T, block, kind, device="cuda", host_mask=None, **pat) -> BlockMa
     with _on(row_ptr):
         _lib.check("rt_index_build", lib.rt_index_build(ctypes.byref(p), int(T), int(block), _ptr(row_ptr),
                                                         _ptr(col_idx), int(nnz), _stream(row_ptr)))
-        built = BlockMask(row_ptr, col_idx[:nnz] if nnz else col_idx[:0], int(block), n_blk, int(nnz), n_masks)._made()
     if dmask is not None:
         # keep the mask alive until the build has run on the stream
         torch.cuda.current_stream(row_ptr.device).synchronize()
-    return built
+    return BlockMask(row_ptr, col_idx[:nnz] if nnz else col_idx[:0], int(block), n_blk, int(nnz), n_masks)
 
 
 def dynamic_index(q, k, block, keep) -> BlockMask:
@@ -374,9 +382,9 @@ def dynamic_index(q, k, block, keep) -> BlockMask:
         _lib.check("rt_dynamic_index", lib.rt_dynamic_index(_ptr(q), _ptr(k), dims, int(block), int(keep),
                                                             _ptr(row_ptr), _ptr(col_idx), int(nnz), _ptr(work),
                                                             int(ws.value), _stream(q)))
-        # `work` returns to torch's stream-ordered cache here; a later reuse on this
-        # stream runs after the launch that reads it
-        return BlockMask(row_ptr, col_idx[:nnz], int(block), n_blk, int(nnz), B * H)._made()
+    # `work` returns to torch's stream-ordered cache here; a later reuse on this
+    # stream runs after the launch that reads it
+    return BlockMask(row_ptr, col_idx[:nnz], int(block), n_blk, int(nnz), B * H)
 
 
 def attn_full(q, k, v, block=64, stats=True, out=None):

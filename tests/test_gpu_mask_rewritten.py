@@ -57,3 +57,54 @@ def test_a_mask_rewritten_in_inference_mode(x, inside):
         with torch.inference_mode():
             mask.col_idx.copy_(_col(16, 4, seed))
             assert _same(_grads(x, mask), x, 16, 4, seed)
+
+
+def _static(n, keep, made):
+    """A mask over buffers that a graph fills from another buffer, and the graph: the mask made before or after the
+    capture, or by from_csr."""
+    import torch
+
+    rp, ci = (torch.tensor(a, dtype=torch.int32).cuda() for a in _csr(n, keep, 0))
+    mask = None
+    if made == "csr":
+        mask = rt.BlockMask.from_csr(*_csr(n, keep, 0), 64)
+        rp, ci = mask.row_ptr, mask.col_idx
+    elif made == "before":
+        mask = rt.BlockMask(rp, ci, 64, n, n * keep)
+    source = ci.clone()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        ci.copy_(source)
+    return mask or rt.BlockMask(rp, ci, 64, n, n * keep), source, g
+
+
+@pytest.mark.parametrize("early", [True, False])
+@pytest.mark.parametrize("made", ["csr", "before", "after"])
+def test_a_graph_that_writes_the_arrays_of_a_mask(x, made, early):
+    """Eager calls between the replays, with and without one before the capture."""
+    mask, source, g = _static(16, 4, made)
+    if early:
+        assert _same(_grads(x, mask), x, 16, 4, 0)
+    for seed in (1, 2, 3):
+        source.copy_(_col(16, 4, seed))
+        g.replay()
+        for _ in range(2):
+            assert _same(_grads(x, mask), x, 16, 4, seed), seed
+
+
+def test_a_mask_made_by_hand_in_a_capture(x):
+    """Its arrays are the graph's own, which every replay writes."""
+    import torch
+
+    source = _col(16, 4, 0)
+    rp = torch.tensor(_csr(16, 4, 0)[0], dtype=torch.int32).cuda()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        mask = rt.BlockMask(rp, source + 0, 64, 16, 64)
+    for seed in (1, 2, 3):
+        source.copy_(_col(16, 4, seed))
+        g.replay()
+        for _ in range(2):
+            assert _same(_grads(x, mask), x, 16, 4, seed), seed

@@ -99,3 +99,36 @@ def test_arrays_whose_writes_are_not_counted(device):
     with torch.inference_mode():
         mask.col_idx.add_(0)
     assert mask.transposed() is not first and len(device.built) == 2
+
+
+def test_a_write_in_a_capture_counts_once_and_happens_at_every_replay(device):
+    mask = _mask()
+    mask.transposed()
+    device.capturing = True
+    mask.col_idx.add_(0)
+    device.capturing = False
+    seen = [mask.transposed() for _ in range(3)]
+    assert len({id(t) for t in seen}) == 3 and len(device.built) == 4
+
+
+@pytest.mark.parametrize("written", ["row_ptr", "col_idx"])
+def test_arrays_written_before_the_mask_is_made(device, written):
+    """Static buffers that a graph fills: the capture may have come first."""
+    import torch
+
+    arrays = {"row_ptr": torch.arange(5, dtype=torch.int32), "col_idx": torch.arange(4, dtype=torch.int32)}
+    arrays[written].copy_(arrays[written].clone())
+    mask = rt.BlockMask(arrays["row_ptr"], arrays["col_idx"], 64, 4, 4)
+    assert mask.transposed() is not mask.transposed()
+
+
+def test_a_mask_made_under_a_capture(device, monkeypatch):
+    """By the framework or by hand."""
+    import torch
+
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True, raising=False)
+    device.capturing = True
+    mask = _mask()
+    device.capturing = False
+    assert mask.transposed() is not mask.transposed()
+    assert _mask().transposed() is not None
