@@ -232,7 +232,7 @@ class BlockMask:
             self.__dict__["_c"] = c
         return c
 
-    def transposed(self):
+    def transposed(self, anew=False):
         """The mask's transpose as the gradient calls take it (rt_index_transpose): row kb lists the query
         blocks that keep key block kb.  Built on the current stream.  It is kept with the mask, so that a mask of
         many steps is transposed once, as long as no operator of torch has written the mask's arrays in place
@@ -240,12 +240,17 @@ class BlockMask:
         Else, for a mask made under a capture, and for inference tensors, which have no counters, each call
         builds another.  So does each capture, as part of the graph: a graph holds what it reads, and its replays
         follow the mask's arrays as they are then.  n_masks > 1: masks that share entries of col_idx (from_csr
-        allows for them) do not fit and make the gradients dk and dv NaN."""
+        allows for them) do not fit and make the gradients dk and dv NaN.
+
+        anew: built now in any case, and kept by the same rule.  Writes that torch does not count (by another
+        library, through .data, by a graph to arrays of its own over which the mask was made later) need it.  A
+        caller who holds a transpose hands it to attn_sparse_backward: captured calls over one static mask then
+        share it."""
         torch = _torch()
         raw, unwritten = _stream(self.row_ptr), self._unwritten()
         with _on(self.row_ptr):
             capturing = torch.cuda.is_current_stream_capturing()
-            kept = self.__dict__.get("_t") if unwritten and not capturing else None
+            kept = self.__dict__.get("_t") if unwritten and not capturing and not anew else None
             if kept is not None:
                 t, done, built_on = kept
                 if raw != built_on:
@@ -255,13 +260,11 @@ class BlockMask:
                     t.row_ptr.record_stream(cur)
                     t.col_idx.record_stream(cur)
                 return t
-            room = self.__dict__.get("_entries", self.nnz)
+            lib, room = _lib.load(), int(self.__dict__.get("_entries", self.nnz))
             row_ptr = torch.empty_like(self.row_ptr)
-            lib, values = _lib.load(), ctypes.c_int64(0)
-            _lib.check("rt_index_transpose_size",
-                       lib.rt_index_transpose_size(ctypes.byref(self.c_struct()), int(room), ctypes.byref(values)))
-            col_idx = torch.empty(values.value, dtype=torch.int32, device=row_ptr.device)
-            t = BlockMask(row_ptr, col_idx, self.block, self.n_qblk, int(room), self.n_masks)
+            col_idx = torch.empty(_transpose_values(self.block, self.n_qblk, self.nnz, self.n_masks, room),
+                                  dtype=torch.int32, device=row_ptr.device)
+            t = BlockMask(row_ptr, col_idx, self.block, self.n_qblk, room, self.n_masks)
             _lib.check("rt_index_transpose", lib.rt_index_transpose(
                 ctypes.byref(self.c_struct()), self.n_qblk * self.block, ctypes.byref(t.c_struct()), raw))
             if unwritten and not capturing:
@@ -305,6 +308,15 @@ class BlockMask:
         rows = hrp.reshape(n_masks, n_qblk + 1).astype(np.int64)
         mask.__dict__["_entries"] = max(int((rows[:, -1] - rows[:, 0]).sum()), int(hci.size))  # masks may share entries
         return mask
+
+
+def _transpose_values(block, n_qblk, nnz, n_masks, room):
+    """int32 values of the transpose of such a mask, with room for `room` entries."""
+    values = ctypes.c_int64(0)
+    _lib.check("rt_index_transpose_size",
+               _lib.load().rt_index_transpose_size(ctypes.byref(_lib.RtBsr(None, None, block, n_qblk, nnz, n_masks)),
+                                                   room, ctypes.byref(values)))
+    return values.value
 
 
 def _pattern(kind, grid_h=0, grid_w=0, frames=0, n_text=0, keep=0, mask=None, host_mask=None, n_masks=1):
@@ -586,11 +598,29 @@ def attn_full_backward(q, k, v, o, row_max, row_sum, d_o, out=None):
     return dq, dk, dv
 
 
-def attn_sparse_backward(q, k, v, o, row_max, row_sum, d_o, mask: BlockMask, rho=None, rho_delta=0.0, out=None):
+def _check_transposed(t, mask, q):
+    """t holds what the gradient call reads of a transpose of such a mask."""
+    torch = _torch()
+    if not isinstance(t, BlockMask):
+        raise ValueError("transposed must be a mask's transposed()")
+    _mask_on(t, q)
+    for name, a in (("row_ptr", t.row_ptr), ("col_idx", t.col_idx)):
+        if a.dtype is not torch.int32 or not a.is_contiguous():
+            raise ValueError(f"transposed.{name} must be a contiguous int32 tensor")
+    if (t.block, t.n_qblk, t.n_masks) != (mask.block, mask.n_qblk, mask.n_masks) or t.nnz < mask.nnz:
+        raise ValueError("transposed is not of such a mask")
+    values = _transpose_values(mask.block, mask.n_qblk, mask.nnz, mask.n_masks, t.nnz)
+    if t.row_ptr.numel() != mask.row_ptr.numel() or t.col_idx.numel() < values:
+        raise ValueError("transposed must be a mask's transposed()")
+
+
+def attn_sparse_backward(q, k, v, o, row_max, row_sum, d_o, mask: BlockMask, rho=None, rho_delta=0.0, out=None,
+                         transposed=None):
     """Gradients (dq, dk, dv) of sparse attention (Eq.5), or with rho (dq, dk, dv, d_rho) of its reshaped output
     min(1, rho + rho_delta) * SparseAttn + R, for the output's gradient d_o (which is R's gradient too).  o,
     row_max and row_sum are attn_sparse's for these q, k, v and mask: the sparse output, not the reshaped one.
-    out: three tensors to write dq, dk, dv into instead of new ones."""
+    out: three tensors to write dq, dk, dv into instead of new ones.  transposed: mask.transposed() as the caller
+    holds it, taken as it is (None: the mask's own)."""
     torch = _torch()
     lib = _lib.load()
     dims = _check_qkv(q, k, v)
@@ -601,7 +631,11 @@ def attn_sparse_backward(q, k, v, o, row_max, row_sum, d_o, mask: BlockMask, rho
     dq, dk, dv = _grads(out, q)
     if q.numel() == 0:
         return (dq, dk, dv) if rho is None else (dq, dk, dv, torch.empty_like(rho))
-    t = mask.transposed()
+    if transposed is None:
+        t = mask.transposed()
+    else:
+        t = transposed
+        _check_transposed(t, mask, q)
     bsr = mask.c_struct()
     need = _backward_bytes(tuple(q.shape), (mask.block, mask.n_qblk, mask.nnz, mask.n_masks, t.nnz))
     d_rho = torch.empty_like(rho) if rho is not None else None

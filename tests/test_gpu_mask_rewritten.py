@@ -108,3 +108,51 @@ def test_a_mask_made_by_hand_in_a_capture(x):
         g.replay()
         for _ in range(2):
             assert _same(_grads(x, mask), x, 16, 4, seed), seed
+
+
+def test_uncounted_writes_and_a_transpose_asked_for(x):
+    """Writes through .data leave torch's counters as they are."""
+    mask = rt.BlockMask.from_csr(*_csr(16, 4, 0), 64)
+    assert _same(_grads(x, mask), x, 16, 4, 0)
+    for seed in (1, 2):
+        mask.col_idx.data.copy_(_col(16, 4, seed))
+        t = mask.transposed(anew=True)
+        assert _same(_grads(x, mask), x, 16, 4, seed)
+        assert _same(_grads(x, mask, transposed=t), x, 16, 4, seed)
+
+
+def test_captured_calls_over_a_transpose_that_the_caller_holds(x):
+    import torch
+
+    q, k, v, d_o = x
+    mask = rt.BlockMask.from_csr(*_csr(16, 4, 0), 64)
+    t = mask.transposed()
+    stats = rt.attn_sparse(q, k, v, mask)
+    outs = [torch.empty_like(q) for _ in range(3)]
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rt.attn_sparse_backward(q, k, v, *stats, d_o, mask, out=outs, transposed=t)
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        want = rt.attn_sparse_backward(q, k, v, *stats, d_o, mask)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_what_is_no_transpose_of_the_mask_is_refused(x):
+    import torch
+
+    mask = rt.BlockMask.from_csr(*_csr(16, 4, 0), 64)
+    t = mask.transposed()
+    cut = lambda **kw: rt.BlockMask(**{**{f: getattr(t, f) for f in t.__dataclass_fields__}, **kw})  # noqa: E731
+    assert _same(_grads(x, mask, transposed=cut()), x, 16, 4, 0)
+    bad = [mask, t.col_idx, rt.BlockMask.from_csr(*_csr(16, 3, 0), 64).transposed(), rt.BlockMask.from_csr(*_csr(32, 4, 0), 32).transposed(),
+           cut(row_ptr=t.row_ptr[:-1]), cut(col_idx=t.col_idx[:-1]), cut(col_idx=t.col_idx.long()), cut(nnz=t.nnz + 4096),
+           cut(n_masks=2), cut(row_ptr=t.row_ptr.cpu()), cut(col_idx=torch.stack([t.col_idx] * 2, 1)[:, 0])]
+    for i, b in enumerate(bad):
+        with pytest.raises(ValueError):
+            _grads(x, mask, transposed=b)
+            print("accepted:", i)

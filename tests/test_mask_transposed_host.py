@@ -132,3 +132,10 @@ def test_a_mask_made_under_a_capture(device, monkeypatch):
     device.capturing = False
     assert mask.transposed() is not mask.transposed()
     assert _mask().transposed() is not None
+
+
+def test_anew_replaces_the_kept_one(device):
+    mask = _mask()
+    first = mask.transposed()
+    second = mask.transposed(anew=True)
+    assert second is not first and mask.transposed() is second and len(device.built) == 2
