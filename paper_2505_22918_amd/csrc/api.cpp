@@ -607,12 +607,13 @@ rt_status check_transposed(const rt_bsr* t, const rt_bsr* m) {
 }
 
 // How the lists of a transposed mask with room for `entries` are split over workgroups, so that no long one (a text
-// block's, which all query blocks keep) holds a call up: after `seg` entries, twice the mean list and 16 at least, in
-// masks of more than 40 blocks, 96 where each head has its own; and what the plan and the parts of split lists take at
-// most.  Where nothing is split, that the plan could be costs a launch for the sums: 12 heads of 83 blocks with random
-// lists 52.4 us without, 53.3 with; of 55 blocks, four of them text's, 87 and 52.  Masks of their own come with the
-// step's inputs, are transposed for one call, and seldom hold such a block (12 random ones of 83 blocks, transposed in
-// each call: 64.9 us, 59.8 unsplit).
+// block's, which all query blocks keep, or one that all score well) holds a call up: after `seg` entries, twice the mean
+// list and 16 at least, in masks of more than 40 blocks; and what the plan and the parts of split lists take at most.
+// Where nothing turns out to be split, that the plan could be costs a launch for the sums.  Gradients of 12 heads, each
+// with a mask of its own, new in each call, unsplit and by this rule: 83 blocks with random lists 58.1 and 63.2 us, with
+// one block that all queries keep 142 and 72, dynamic masks 159 and 77; 55 blocks 39.9 and 42.5, 94 and 51.  Up to 40
+// blocks splitting would cost 2 us without such a block (32 blocks 21.1 and 23.0) and gain up to 20 with one (59 and
+// 38; 24 blocks 38 and 32); the masks of images of that size hold none.
 struct Plan {
     int32_t seg, max_more, max_base;  // entries of a part; parts beyond the first ones, and numbers of parts, at most
     int64_t first, values;  // the plan's place behind the entries, and the size of it all
@@ -621,9 +622,8 @@ struct Plan {
 
 rt_status plan_of(const rt_bsr* m, int32_t entries, Plan* out) {
     const int64_t rows = (int64_t)(m->n_masks > 1 ? m->n_masks : 1) * m->n_qblk;
-    const int64_t seg = m->n_qblk <= (m->n_masks > 1 ? 96 : 40)
-                            ? std::max(m->n_qblk, 1)
-                            : std::max<int64_t>(16, 2 * ceil_div(entries, std::max<int64_t>(rows, 1)));
+    const int64_t seg = m->n_qblk <= 40 ? std::max(m->n_qblk, 1)
+                                        : std::max<int64_t>(16, 2 * ceil_div(entries, std::max<int64_t>(rows, 1)));
     const int64_t splits = m->n_qblk > seg ? entries / seg : 0;
     // the plan's int32 places, and a wave for each row in a launch of less than 2^32 threads
     if (rows + 2 * splits > INT32_MAX / 8 || rows >= (int64_t)1 << 26) return fail(RT_EINVAL, "too many mask rows");
