@@ -742,8 +742,9 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None):
 def layer_norm_backward(d_y, x, mean, rstd, weight=None, bias=True, out=None):
     """Gradients (dx, d_weight, d_bias) of layer_norm for the gradient d_y of its output; mean and rstd are the
     forward call's.  dx has x's type, in a new contiguous tensor or `out` (any row strides); d_weight and d_bias
-    are fp32 of the weight's shape, summed over the rows of each set.  Without a weight both are None; bias=False
-    leaves d_bias out."""
+    are fp32 of the weight's shape, summed over the rows of each set.  bias: the forward call's, for d_bias where
+    there is no weight; True gives d_bias with a weight's gradient, False leaves it out.  What there is no vector
+    for is None."""
     torch = _torch()
     lib = _lib.load()
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
@@ -751,7 +752,8 @@ def layer_norm_backward(d_y, x, mean, rstd, weight=None, bias=True, out=None):
     shape = tuple(x.shape)
     xs = _norm_strides(shape, x.stride(), x.dtype, "x")
     dys = _norm_like(d_y, "d_y", x)
-    dims, need = _norm_dims(shape, x.dtype, _norm_weight(weight, "weight", x), None)
+    given = None if bias is None or isinstance(bias, bool) else bias
+    dims, need = _norm_dims(shape, x.dtype, _norm_weight(weight, "weight", x), _norm_weight(given, "bias", x))
     for name, t in (("mean", mean), ("rstd", rstd)):
         if not _same(t, torch.float32, shape[:-1], x):
             _stat(t, shape[:-1], name, x.device)
@@ -763,7 +765,9 @@ def layer_norm_backward(d_y, x, mean, rstd, weight=None, bias=True, out=None):
     d_weight = d_bias = None
     if weight is not None:
         d_weight = torch.empty(weight.shape, dtype=torch.float32, device=x.device)
-        d_bias = torch.empty_like(d_weight) if bias else None
+    like = given if given is not None else (weight if bias else None)
+    if like is not None:
+        d_bias = torch.empty(like.shape, dtype=torch.float32, device=x.device)
     work = _workspace(need, x)
     with _on(x):
         _lib.check("rt_layer_norm_backward",
