@@ -705,7 +705,9 @@ def _norm_like(t, name, x):
 def _norm_weight(t, name, x):
     if t is None:
         return None
-    if not (t.is_cuda and t.get_device() == x.get_device() and t.is_contiguous()):
+    if not (isinstance(t, _torch().Tensor) and t.is_cuda):
+        _on_device(t, name, None)
+    if not (t.get_device() == x.get_device() and t.is_contiguous()):
         _on_device(t, name, x.device)
         raise ValueError(f"{name} must be contiguous")
     return tuple(t.shape), t.dtype
