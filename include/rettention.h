@@ -291,8 +291,8 @@ rt_status rt_index_transpose(const rt_bsr* mask, int32_t T, const rt_bsr* t, voi
  * rounded to bf16 for the matrix products, whose sums are fp32.  Equal calls give equal
  * bits.  workspace: device memory, 16-byte aligned, of at least the bytes that
  * rt_attn_full_backward_workspace reports (RT_ECAPACITY below), overwritten; it, and the
- * outputs, must not overlap each other or an input.  B*H times T in whole 64 is below 2^29
- * (RT_EINVAL). */
+ * outputs, must not overlap each other or an input.  B*H times T in whole 64 is below 2^29,
+ * and B*H times ceil(T / 128) is at most 2^23 - 8 in this call (RT_EINVAL). */
 rt_status rt_attn_full_backward_workspace(rt_dims dims, int64_t* bytes);
 rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, const void* o,
                                 const float* row_max, const float* row_sum, const void* d_o, rt_dims dims,

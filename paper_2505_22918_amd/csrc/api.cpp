@@ -889,6 +889,9 @@ rt_status rt_attn_full_backward(const void* q, const void* k, const void* v, con
     RT_TRY(check_dims(dims, &empty));
     if (empty) return ok();
     RT_TRY(check_items(dims, 32));
+    // two workgroups of 256 threads for each tile, in whole eights, in one launch
+    if (16 * ceil_div((int64_t)dims.B * dims.H * ceil_div(dims.T, rt::kDenseRows), 8) * 256 >= (int64_t)1 << 32)
+        return fail(RT_EINVAL, "too many rows: B=%d H=%d T=%d", dims.B, dims.H, dims.T);
     const int64_t nt = tensor_bytes(dims, 2), ns = tensor_bytes(dims, 4) / dims.D;
     const int64_t need = backward_workspace(dims, nullptr, Plan{});
     rt::GradArgs a{};
