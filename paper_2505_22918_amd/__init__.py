@@ -3,6 +3,8 @@
 Python face of librettention.so.  Functions take torch CUDA tensors for device
 memory and launch on torch's current stream; all computation runs in the HIP
 library (the binding only marshals pointers and sizes).
+Results carry no gradient function, also where inputs require gradients: the
+*_backward functions are called for them.
 
   build_index           block CSR of the static mask (Sec.3, App. A.4)
   dynamic_index         per-(batch, head) mask chosen from the step's Q and K

@@ -232,7 +232,7 @@ __device__ __forceinline__ int part_place(const GradArgs& a, int base) {
 // so that what takes longest begins first.  (A block's dK and dV next to its dQ, which reads the same rows, was no
 // faster at the CogVideoX shape and 20 % slower where the lists are random.)
 //
-// Three waves to a SIMD where two share a ring.  A lone wave's ring leaves room for two by LDS; in the registers of three
+// Three waves to a SIMD where two share a ring (72 wide: 3 registers spilled, none read inside the walk).  A lone wave's ring leaves room for two by LDS; in the registers of three
 // the 72-wide walk's sums go through the accumulator file (32 heads of 4096 tokens, 9 kept blocks of 32: 84 against 75
 // us with all 512 registers for two; 1024 tokens 30.5 against 26.2; 64-wide ones equal).
 template <int D, int W>
@@ -342,8 +342,9 @@ hipError_t launch_d(const GradArgs& a, hipStream_t stream) {
     }
     if (a.row_ptr) return a.block == 64 ? launch_sparse<D, 2>(a, stream) : launch_sparse<D, 1>(a, stream);
     // Workgroups of four waves (eight: 15.6 against 15.4 ms at the CogVideoX shape, 11.4 against 8.4 us at 2 heads of 256
-    // tokens).  64-wide heads fit three waves to a SIMD, which pays where there are as many (14.5 against 14.8 ms; 9.0
-    // against 7.9 us where there are not: a wave with fewer registers waits more); 72-wide ones spill (819 against 533).
+    // tokens).  64-wide heads run three waves to a SIMD where there are as many (14.5 against 14.8 ms, though the
+    // compiler spills 6 registers, 4 of them read again at each stage of dK and dV; 9.0 against 7.9 us where there are
+    // not: a wave with fewer registers waits more); 72-wide ones spill far more (819 against 533).
     if (!few)
         hipLaunchKernelGGL((grad_dense<D, W, D == 64 ? 3 : 2, false, false>), dim3(16 * per), dim3(64 * W), 0, stream, a, n, per);
     else if (a.split > 1) {

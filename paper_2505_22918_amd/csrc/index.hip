@@ -212,7 +212,10 @@ __global__ __launch_bounds__(kThreads) void row_fill(IndexArgs a) {
 // wave to a (mask, kb) looks at 64 rows at a time, each lane with a binary search of its row (rows are ascending),
 // once to count and once, after a scan of the counts, to write; ballots keep the order.
 //
-// Latency: 12 masks of 83 blocks 16 us in three launches, 9 in one.
+// Latency: 12 masks of 83 blocks 16 us in three launches, 9 in one (its kernel alone 6.6).  In one launch 32 blocks take
+// 5 us, 256 15, 640 33.  The searches are of every row for every key block, so their time grows with the square of the
+// blocks: 641 29 us (30 masks of them 267), 1024 44, 2048 107, 4096 340 to 730, 16384 4.7 ms, 131072 (the longest head)
+// 240 ms.
 
 constexpr int kSmall = 640;  // its bits take 51 KB
 

@@ -421,6 +421,9 @@ __global__ __launch_bounds__(1024) void norm_join(const float* partial, int32_t 
     }
 }
 
+// The gradients of rows in 1024 lanes spill (128 registers to a lane): 16 to 46 of them in chunks of 8, 52 to 133 one by
+// one.
+//
 // Lanes and chunks of a row.  Rows of up to 512 elements (64 one by one) share a wave, so that its accesses stay
 // full; longer ones take a wave with more chunks, and over 2048 (512) a workgroup, whose registers would else not
 // hold a row and its column sums.
