@@ -278,7 +278,7 @@ class BlockMask:
     def _unwritten(self):
         """Nothing has written the mask's arrays since they were allocated, as far as torch counts, nor does a graph
         that made them."""
-        if self.__dict__["_of_graph"]:
+        if self.__dict__.get("_of_graph"):
             return False
         try:
             return self.row_ptr._version == 0 and self.col_idx._version == 0
@@ -756,7 +756,7 @@ def layer_norm_backward(d_y, x, mean, rstd, weight=None, bias=True, out=None):
     shape = tuple(x.shape)
     xs = _norm_strides(shape, x.stride(), x.dtype, "x")
     dys = _norm_like(d_y, "d_y", x)
-    given = None if bias is None or isinstance(bias, bool) else bias
+    given = bias if isinstance(bias, torch.Tensor) else None
     dims, need = _norm_dims(shape, x.dtype, _norm_weight(weight, "weight", x), _norm_weight(given, "bias", x))
     for name, t in (("mean", mean), ("rstd", rstd)):
         if not _same(t, torch.float32, shape[:-1], x):

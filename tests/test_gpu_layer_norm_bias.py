@@ -34,7 +34,9 @@ def test_bias_of_the_forward_call_beside_a_weight(gpu):
     want = rt.layer_norm_backward(dy, x, mean, rstd, w)
     got = rt.layer_norm_backward(dy, x, mean, rstd, w, bias=b)
     assert all((a == c).all() for a, c in zip(got, want))
-    assert rt.layer_norm_backward(dy, x, mean, rstd, w, bias=False)[2] is None
+    for no in (False, None, 0):
+        assert rt.layer_norm_backward(dy, x, mean, rstd, w, bias=no)[2] is None
+    assert (rt.layer_norm_backward(dy, x, mean, rstd, w, bias=1)[2] == want[2]).all()
     assert rt.layer_norm_backward(dy, x, mean, rstd)[1:] == (None, None)
     for bad in (b[:71], b.half(), b.cpu(), _tensor((5, 72), "fp32", 5)):
         with pytest.raises(ValueError):
