@@ -139,3 +139,11 @@ def test_anew_replaces_the_kept_one(device):
     first = mask.transposed()
     second = mask.transposed(anew=True)
     assert second is not first and mask.transposed() is second and len(device.built) == 2
+
+
+def test_a_mask_restored_from_its_fields_alone(device):
+    """As copies of masks that were stored earlier come back: without what their making notes."""
+    whole = _mask()
+    mask = object.__new__(rt.BlockMask)
+    mask.__dict__.update({f: getattr(whole, f) for f in rt.BlockMask.__dataclass_fields__})
+    assert mask.transposed() is mask.transposed()
