@@ -356,6 +356,73 @@ rt_status rt_layer_norm_backward(const void* dy, const int64_t dy_stride[3], con
                                  float* d_weight, float* d_bias, void* workspace, int64_t workspace_bytes,
                                  void* stream);
 
+/* ---- Rotary positions, and differential attention ---------------------------------- */
+
+/* Rotary positions: of each row's first `rotated` elements, pair p is turned by the angle
+ *   theta = position * freq[p],  (a, b) -> amplitude (a cos - b sin, a sin + b cos)
+ * in 32 bits (the angle in 64); elements past them are copied.  RT_ROPE_INTERLEAVED: pair p is
+ * the elements 2 p and 2 p + 1; RT_ROPE_HALF: p and p + rotated / 2.  Rows are counted by sample,
+ * head and token (B, H, T), D consecutive elements each; stride[3] gives the elements from one
+ * row to the next in each index, as for rt_layer_norm.  positions: device [T][axes], or
+ * [B][T][axes] with per_sample, contiguous; pair p takes the coordinate axis[p] of its token.
+ * freq: device, rotated / 2 radians a position; axis: device, the same number of values from 0 to
+ * axes - 1, or NULL where axes is 1.  y may be x with x's strides (in place); else no element of
+ * y may share memory with another, with x or with another input.  2 <= D <= 16384, T D < 2^32;
+ * at most 2^24 - 1 workgroups of 256 threads, each with an 8th of a row's elements or less. */
+enum { RT_ROPE_INTERLEAVED = 0, RT_ROPE_HALF = 1 };
+enum { RT_POS_I32 = 0, RT_POS_I64 = 1, RT_POS_F32 = 2 };
+typedef struct {
+    int32_t B, H, T, D;
+    int32_t type;          /* of x and y: RT_BF16, RT_F16 or RT_F32 */
+    int32_t rotated;       /* even, 2 to D                          */
+    int32_t layout;        /* RT_ROPE_*                             */
+    int32_t axes;          /* coordinates of a token, 1 to 16       */
+    int32_t position_type; /* RT_POS_*                              */
+    int32_t per_sample;    /* not 0: each sample has its positions  */
+} rt_rope_dims;
+rt_status rt_rope(const void* x, const int64_t x_stride[3], const void* positions, const double* freq,
+                  const int32_t* axis, float amplitude, rt_rope_dims dims, void* y, const int64_t y_stride[3],
+                  void* stream);
+
+/* Its gradient: dy turned by -theta, times amplitude.  dx may be dy with its strides. */
+rt_status rt_rope_backward(const void* dy, const int64_t dy_stride[3], const void* positions, const double* freq,
+                           const int32_t* axis, float amplitude, rt_rope_dims dims, void* dx,
+                           const int64_t dx_stride[3], void* stream);
+
+/* Differential attention: two softmax maps to a head, one subtracted with a learned weight.
+ *   P_i = softmax(Q_i K_i^T / sqrt(D)), i = 1, 2;  O_i = P_i V;  O = O_1 - lam_h O_2
+ * q: device bf16 [B][2 H][Tq][D], k: [B][2 H][Tk][D], the maps of head h at 2 h and 2 h + 1;
+ * v: [B][H][Tk][2 D]; lam: device fp32, n_lam values: one for each head (H) or for all (1).
+ * k_lens: device int32 [B], the keys that each sample has (its first ones; taken as 0 to Tk), or
+ * NULL: Tk.  Keys and values past them are not used, whatever they hold; without keys O is 0.
+ * o: device bf16 [B][H][Tq][2 D] (written).  o2, row_max, row_sum: written together, or all NULL:
+ * O_2, bf16 as o, and fp32 [B][2 H][Tq] the largest score m (divided by sqrt(D)) of each map's row
+ * and its sum of exp(score - m); without keys -inf and 0.  P is rounded to bf16 for the matrix
+ * products, whose sums are fp32.  Equal calls give equal bits.  workspace: device, 16-byte
+ * aligned, of the bytes that rt_attn_diff_workspace reports, overwritten (parts of the keys where
+ * there are few rows).  Outputs and workspace must not overlap each other or an input.
+ * D is 64 or 72; B H < 2^23, 4 T D <= 2^30 and B H T (in whole 64) < 2^28 for T = Tq and Tk. */
+typedef struct {
+    int32_t B, H, Tq, Tk, D;
+} rt_diff_dims;
+rt_status rt_attn_diff_workspace(rt_diff_dims dims, int64_t* bytes);
+rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float* lam, int32_t n_lam,
+                       const int32_t* k_lens, rt_diff_dims dims, void* o, void* o2, float* row_max, float* row_sum,
+                       void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Gradients of rt_attn_diff for Q, K, V and lam, the probabilities recomputed from its statistics:
+ *   dA = dO V^T;  delta_2 = dO . O_2, delta_1 = dO . O + lam delta_2
+ *   dS_1 = P_1 (dA - delta_1), dS_2 = -lam P_2 (dA - delta_2);  dV = (P_1 - lam P_2)^T dO
+ *   dQ_i = dS_i K_i / sqrt(D), dK_i = dS_i^T Q_i / sqrt(D);  dlam = -sum of delta_2 over the
+ * rows of each head, or of all.  o, o2, row_max, row_sum: of rt_attn_diff for these inputs; d_o:
+ * as o; dq, dk, dv: as q, k, v (written; rows past k_lens 0); d_lam: device fp32 [n_lam]
+ * (written).  Sums are fp32, dlam's 64-bit, in a fixed order: equal calls give equal bits. */
+rt_status rt_attn_diff_backward_workspace(rt_diff_dims dims, int64_t* bytes);
+rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, const float* lam, int32_t n_lam,
+                                const int32_t* k_lens, const void* o, const void* o2, const float* row_max,
+                                const float* row_sum, const void* d_o, rt_diff_dims dims, void* dq, void* dk,
+                                void* dv, float* d_lam, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Static description of a status code. */
 const char* rt_status_str(rt_status status);
 

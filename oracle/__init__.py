@@ -15,6 +15,8 @@ block_index  The static block mask M / kept set S (Sec.3) as CSR lists of kept
 dynamic_mask The run-time block mask (future work of Sec.6 and App. A.2): per
              (batch, head), each query block keeps itself and the top-scoring
              key blocks of the block-pooled Q K^T described in Sec.2.
+heads        Rotary positions, and differential attention with its gradients,
+             with the tolerances of bf16 operands and fp32 sums.
 schedule     The denoising-step schedule of Sec.5 composed from the attention
              definitions, with the ramp of Sec.4.2.
 

@@ -20,6 +20,11 @@ Results carry no gradient function, also where inputs require gradients: the
   attn_sparse_backward  gradients of sparse attention, or of its reshaped output, for Q, K, V (and rho)
   layer_norm            layer norm of rows, of any row strides, with row statistics
   layer_norm_backward   its gradients, the weight's and bias's among them
+  rope_plan             frequencies, axes and layout of rotary positions (RopePlan)
+  rope                  rotary positions of heads' rows, of any row strides
+  rope_backward         their gradient
+  attn_diff             differential attention: two softmax maps to a head, one subtracted with a learned weight
+  attn_diff_backward    its gradients for Q, K, V and the weight
   StatCache             per-layer cache of rho and R with the step schedule of Sec.5
 """
 
@@ -50,6 +55,12 @@ __all__ = [
     "attn_sparse_backward",
     "layer_norm",
     "layer_norm_backward",
+    "RopePlan",
+    "rope_plan",
+    "rope",
+    "rope_backward",
+    "attn_diff",
+    "attn_diff_backward",
     "StatCache",
     "PAT_EXPLICIT",
     "PAT_LOCAL2D",
@@ -779,6 +790,230 @@ def layer_norm_backward(d_y, x, mean, rstd, weight=None, bias=True, out=None):
                                               _ptr(dx), dxs, _ptr(d_weight), _ptr(d_bias), _ptr(work), need,
                                               _stream(x)))
     return dx, d_weight, d_bias
+
+
+@dataclass(frozen=True)
+class RopePlan:
+    """How rows are rotated by their positions: freq, fp64 radians a position of each pair, and axis, int32 the
+    coordinate of the position that each pair goes by (None where there is one), both contiguous on the device; the
+    number of coordinates; the pairs' layout ("interleaved": elements 2 p and 2 p + 1, or "half": p and p + half of the
+    rotated part); a factor of cosines and sines.  rope_plan makes the usual ones."""
+
+    freq: object
+    axis: object = None
+    axes: int = 1
+    layout: str = "interleaved"
+    amplitude: float = 1.0
+
+    @property
+    def rotated(self):
+        """Elements of a row that are rotated, its first ones."""
+        return 2 * self.freq.numel()
+
+
+def rope_plan(rotated, base=10000.0, widths=None, layout="interleaved", scaling=None, factor=1.0, original=None,
+              device="cuda") -> RopePlan:
+    """Rotary positions of a row's first `rotated` elements: pair i of an axis of w elements turns by
+    base^(-2 i / w) radians a position.
+
+    widths: the elements of each axis, in order, where positions have several coordinates (a video's frames, rows and
+    columns); their sum is `rotated`.  scaling stretches them for contexts `factor` times longer: "linear" divides all
+    frequencies by it; "ntk" raises the base, to base * factor^(w / (w - 2)), which leaves an axis' first pair as it is
+    and divides its last one; "yarn" divides the frequencies of pairs that turn less than once over the `original`
+    positions, leaves those that turn more than 32 times, blends in between, and multiplies cosines and sines by
+    0.1 ln(factor) + 1.  The plan is made on the host, to be kept; it holds two small arrays on the device."""
+    import math
+
+    torch = _torch()
+    rotated = int(rotated)
+    widths = [rotated] if widths is None else [int(w) for w in widths]
+    if rotated < 2 or rotated % 2 or sum(widths) != rotated or any(w < 2 or w % 2 for w in widths) or len(widths) > 16:
+        raise ValueError(f"rotated={rotated} widths={widths}: need even numbers of 2 and more that add up, 16 at most")
+    base, factor = float(base), float(factor)
+    if not (math.isfinite(base) and base > 0 and math.isfinite(factor) and factor > 0):
+        raise ValueError(f"base={base} factor={factor} (need positive numbers)")
+    if layout not in _ROPE_LAYOUTS:
+        raise ValueError(f"layout={layout!r} (need one of {sorted(_ROPE_LAYOUTS)})")
+    if scaling not in (None, "linear", "ntk", "yarn"):
+        raise ValueError(f"scaling={scaling!r} (need None, 'linear', 'ntk' or 'yarn')")
+    if scaling == "yarn" and (original is None or not original > 0):
+        raise ValueError("scaling='yarn' needs original, the positions that the frequencies were made for")
+    freq, axis = [], []
+    for i, w in enumerate(widths):
+        b = base * factor ** (w / (w - 2)) if scaling == "ntk" and w > 2 else base
+        for p in range(w // 2):
+            f = b ** (-2 * p / w)
+            if scaling == "linear":
+                f /= factor
+            elif scaling == "yarn":
+                g = min(max((original * f / (2 * math.pi) - 1) / 31, 0.0), 1.0)
+                f = g * f + (1 - g) * f / factor
+            freq.append(f)
+            axis.append(i)
+    return RopePlan(torch.tensor(freq, dtype=torch.float64, device=device),
+                    torch.tensor(axis, dtype=torch.int32, device=device) if len(widths) > 1 else None, len(widths),
+                    layout, 0.1 * math.log(factor) + 1 if scaling == "yarn" else 1.0)
+
+
+_ROPE_LAYOUTS = {"interleaved": _lib.RT_ROPE_INTERLEAVED, "half": _lib.RT_ROPE_HALF}
+
+
+def _rope_positions(positions, plan, x):
+    """Checks a plan and positions against x; the positions' C type and whether each sample has its own."""
+    torch = _torch()
+    if not isinstance(plan, RopePlan):
+        raise ValueError("plan must be a RopePlan")
+    if plan.layout not in _ROPE_LAYOUTS:
+        raise ValueError(f"layout={plan.layout!r} (need one of {sorted(_ROPE_LAYOUTS)})")
+    _on_device(plan.freq, "plan.freq", x.device)
+    if plan.freq.dtype is not torch.float64 or plan.freq.dim() != 1 or not plan.freq.is_contiguous():
+        raise ValueError("plan.freq must be a contiguous fp64 vector")
+    if plan.axis is None:
+        if plan.axes != 1:
+            raise ValueError("plan.axis is needed where there are several axes")
+    else:
+        _on_device(plan.axis, "plan.axis", x.device)
+        if plan.axis.dtype is not torch.int32 or plan.axis.shape != plan.freq.shape or not plan.axis.is_contiguous():
+            raise ValueError("plan.axis must be a contiguous int32 vector of plan.freq's length")
+    _on_device(positions, "positions", x.device)
+    kind = {torch.int32: _lib.RT_POS_I32, torch.int64: _lib.RT_POS_I64, torch.float32: _lib.RT_POS_F32}.get(positions.dtype)
+    B, T = x.shape[0], x.shape[2]
+    last = () if plan.axes == 1 else (plan.axes,)
+    shape = tuple(positions.shape)
+    if kind is None or shape not in ((T,) + last, (B, T) + last) or not positions.is_contiguous():
+        raise ValueError(f"positions must be a contiguous int32, int64 or fp32 tensor of shape {(T,) + last} or {(B, T) + last}")
+    return kind, shape != (T,) + last
+
+
+def _rope(fn, name, x, positions, plan, out):
+    torch = _torch()
+    lib = _lib.load()
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        _on_device(x, name, None)
+    shape = tuple(x.shape)
+    if len(shape) != 4:
+        raise ValueError(f"{name} must be a [B,H,T,D] tensor")
+    xs = _norm_strides(shape, x.stride(), x.dtype, name)
+    kind, per_sample = _rope_positions(positions, plan, x)
+    if out is None:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device)
+        ys = _norm_strides(shape, y.stride(), x.dtype, "out")
+    else:
+        _on_device(out, "out", x.device)
+        if out.dtype is not x.dtype or out.shape != x.shape:
+            raise ValueError(f"out must have the type and shape of {name}")
+        y, ys = out, _norm_strides(shape, out.stride(), x.dtype, "out")
+    dims = _lib.RtRopeDims(*shape, _norm_types()[x.dtype], plan.rotated, _ROPE_LAYOUTS[plan.layout], plan.axes, kind,
+                           per_sample)
+    with _on(x):
+        _lib.check(fn, getattr(lib, fn)(_ptr(x), xs, _ptr(positions), _ptr(plan.freq), _ptr(plan.axis),
+                                        float(plan.amplitude), dims, _ptr(y), ys, _stream(x)))
+    return y
+
+
+def rope(x, positions, plan: RopePlan, out=None):
+    """Rotary positions: each pair of the first plan.rotated elements of x's rows is turned by the angle of its token's
+    position; the other elements are copied.
+
+    x: bf16, fp16 or fp32 [B,H,T,D] with any row strides (queries and keys of a packed projection [B,T,3,H,D] in one
+    call: qkv[:, :, :2].flatten(2, 3).transpose(1, 2)).  positions: int32, int64 or fp32 [T], or [B,T] for each
+    sample's own, with a last dimension of coordinates where the plan has several axes; at position 0 rows stay as they
+    are (times the plan's amplitude).  Returns a new contiguous tensor or `out`: any row strides, x itself to rotate
+    in place."""
+    return _rope("rt_rope", "x", x, positions, plan, out)
+
+
+def rope_backward(d_y, positions, plan: RopePlan, out=None):
+    """Gradient of rope's x for the gradient d_y of its output: d_y turned back (times the plan's amplitude).  As rope
+    otherwise."""
+    return _rope("rt_rope_backward", "d_y", d_y, positions, plan, out)
+
+
+@functools.lru_cache(maxsize=1024)
+def _diff_bytes(fn, dims):
+    """Workspace of a differential attention call of these (B, H, Tq, Tk, D)."""
+    need = ctypes.c_int64(0)
+    _lib.check(fn, getattr(_lib.load(), fn)(_lib.RtDiffDims(*dims), ctypes.byref(need)))
+    return need.value
+
+
+def _diff_inputs(q, k, v, lam, k_lens):
+    """Checks the inputs of differential attention; (B, H, Tq, Tk, D)."""
+    torch = _torch()
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != q.get_device():
+            _on_device(t, name, None if t is q else q.device)
+        if t.dtype is not torch.bfloat16 or t.dim() != 4 or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous bf16 tensor of 4 dimensions")
+    B, H2, Tq, D = q.shape
+    H, Tk = H2 // 2, k.shape[2]
+    if H2 % 2 or tuple(k.shape) != (B, H2, Tk, D) or tuple(v.shape) != (B, H, Tk, 2 * D):
+        raise ValueError("need q [B,2H,Tq,D], k [B,2H,Tk,D] and v [B,H,Tk,2D]")
+    if not (isinstance(lam, torch.Tensor) and lam.is_cuda and lam.get_device() == q.get_device()):
+        _on_device(lam, "lam", q.device)
+    if lam.dtype is not torch.float32 or tuple(lam.shape) not in ((), (1,), (H,)) or not lam.is_contiguous():
+        raise ValueError(f"lam must be a contiguous fp32 tensor of shape (), (1,) or ({H},)")
+    if k_lens is not None:
+        _on_device(k_lens, "k_lens", q.device)
+        if k_lens.dtype is not torch.int32 or tuple(k_lens.shape) != (B,) or not k_lens.is_contiguous():
+            raise ValueError(f"k_lens must be a contiguous int32 tensor of shape ({B},)")
+    return B, H, Tq, Tk, D
+
+
+def attn_diff(q, k, v, lam, k_lens=None, stats=True, out=None):
+    """Differential attention: (softmax(Q_1 K_1^T / sqrt(D)) - lam softmax(Q_2 K_2^T / sqrt(D))) V for each head.
+
+    q: bf16 [B,2H,Tq,D], k: [B,2H,Tk,D], the two maps of head h at 2 h and 2 h + 1; v: [B,H,Tk,2D]; lam: fp32, one value
+    or [H].  k_lens: int32 [B] on the device, the keys that each sample has, its first ones (a padded batch, or a cache
+    with room for more); without keys the output is 0.  Returns o [B,H,Tq,2D], with stats (o, o2, row_max, row_sum) as
+    attn_diff_backward takes them: the second map's output, and of both maps' rows the largest score and the sum of
+    exponentials against it, fp32 [B,2H,Tq]."""
+    torch = _torch()
+    lib = _lib.load()
+    B, H, Tq, Tk, D = dims = _diff_inputs(q, k, v, lam, k_lens)
+    shape = (B, H, Tq, 2 * D)
+    o = torch.empty(shape, dtype=q.dtype, device=q.device) if out is None else _bf16(out, shape, "out", q.device)
+    o2 = m = l = None
+    if stats:
+        o2 = torch.empty_like(o)
+        m = torch.empty((B, 2 * H, Tq), dtype=torch.float32, device=q.device)
+        l = torch.empty_like(m)
+    need = _diff_bytes("rt_attn_diff_workspace", dims)
+    work = _workspace(need, q)
+    with _on(q):
+        _lib.check("rt_attn_diff",
+                   lib.rt_attn_diff(_ptr(q), _ptr(k), _ptr(v), _ptr(lam), lam.numel(), _ptr(k_lens), _lib.RtDiffDims(*dims),
+                                    _ptr(o), _ptr(o2), _ptr(m), _ptr(l), _ptr(work), need, _stream(q)))
+    return (o, o2, m, l) if stats else o
+
+
+def attn_diff_backward(q, k, v, o, o2, row_max, row_sum, d_o, lam, k_lens=None, out=None):
+    """Gradients (dq, dk, dv, d_lam) of differential attention for the gradient d_o of its output: o, o2, row_max and
+    row_sum are attn_diff's for these q, k, v, lam and k_lens.  d_lam is fp32 of lam's shape, summed over the rows of
+    each head, or of all; dk and dv are 0 past a sample's keys.  out: three tensors to write dq, dk, dv into instead
+    of new ones."""
+    torch = _torch()
+    lib = _lib.load()
+    B, H, Tq, Tk, D = dims = _diff_inputs(q, k, v, lam, k_lens)
+    for name, t in (("o", o), ("o2", o2), ("d_o", d_o)):
+        _bf16(t, (B, H, Tq, 2 * D), name, q.device)
+    for name, t in (("row_max", row_max), ("row_sum", row_sum)):
+        _stat(t, (B, 2 * H, Tq), name, q.device)
+    if out is None:
+        dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
+    else:
+        if len(out) != 3:
+            raise ValueError("out must hold dq, dk and dv")
+        dq, dk, dv = (_bf16(t, like.shape, name, q.device) for t, like, name in zip(out, (q, k, v), ("dq", "dk", "dv")))
+    d_lam = torch.empty_like(lam)
+    need = _diff_bytes("rt_attn_diff_backward_workspace", dims)
+    work = _workspace(need, q)
+    with _on(q):
+        _lib.check("rt_attn_diff_backward",
+                   lib.rt_attn_diff_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(lam), lam.numel(), _ptr(k_lens), _ptr(o),
+                                             _ptr(o2), _ptr(row_max), _ptr(row_sum), _ptr(d_o), _lib.RtDiffDims(*dims),
+                                             _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_lam), _ptr(work), need, _stream(q)))
+    return dq, dk, dv, d_lam
 
 
 class StatCache:

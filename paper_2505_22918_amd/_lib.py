@@ -65,7 +65,18 @@ class RtNormDims(ctypes.Structure):
     ]
 
 
+class RtRopeDims(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("B", "H", "T", "D", "type", "rotated", "layout", "axes", "position_type",
+                                       "per_sample")]
+
+
+class RtDiffDims(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("B", "H", "Tq", "Tk", "D")]
+
+
 RT_BF16, RT_F16, RT_F32 = range(3)
+RT_ROPE_INTERLEAVED, RT_ROPE_HALF = range(2)
+RT_POS_I32, RT_POS_I64, RT_POS_F32 = range(3)
 c_int64 = ctypes.c_int64
 Strides = c_int64 * 3
 
@@ -106,6 +117,15 @@ _SIGS = {
     "rt_layer_norm_backward": (c_int32, [c_void_p, Strides, c_void_p, Strides, c_void_p, c_void_p, c_void_p,
                                          RtNormDims, c_void_p, Strides, c_void_p, c_void_p, c_void_p, c_int64,
                                          c_void_p]),
+    "rt_rope": (c_int32, [c_void_p, Strides, c_void_p, c_void_p, c_void_p, c_float, RtRopeDims, c_void_p, Strides,
+                          c_void_p]),
+    "rt_rope_backward": (c_int32, [c_void_p, Strides, c_void_p, c_void_p, c_void_p, c_float, RtRopeDims, c_void_p,
+                                   Strides, c_void_p]),
+    "rt_attn_diff_workspace": (c_int32, [RtDiffDims, ctypes.POINTER(c_int64)]),
+    "rt_attn_diff": (c_int32, [c_void_p] * 4 + [c_int32, c_void_p, RtDiffDims] + [c_void_p] * 5 + [c_int64, c_void_p]),
+    "rt_attn_diff_backward_workspace": (c_int32, [RtDiffDims, ctypes.POINTER(c_int64)]),
+    "rt_attn_diff_backward": (c_int32, [c_void_p] * 4 + [c_int32] + [c_void_p] * 6 + [RtDiffDims] + [c_void_p] * 5
+                              + [c_int64, c_void_p]),
     "rt_status_str": (ctypes.c_char_p, [c_int32]),
     "rt_last_error": (ctypes.c_char_p, []),
     "rt_version": (c_int32, []),

@@ -18,8 +18,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librettention.so")
-SOURCES = ["attn.hip", "attn_dense.hip", "elementwise.hip", "index.hip", "dynamic.hip", "norm.hip", "api.cpp"]
-GRAD_SOURCES = ["attn_grad.hip"]  # beside them: LDS DMAs of its own
+SOURCES = ["attn.hip", "attn_dense.hip", "elementwise.hip", "index.hip", "dynamic.hip", "norm.hip", "rope.hip", "api.cpp"]
+GRAD_SOURCES = ["attn_grad.hip", "attn_diff.hip"]  # beside them: LDS DMAs of its own
 ARCH = "gfx950"
 
 

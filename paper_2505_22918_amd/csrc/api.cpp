@@ -13,6 +13,7 @@
 #include <utility>
 
 #include "../../include/rettention.h"
+#include "heads.h"
 #include "kernels.h"
 #include "train.h"
 
@@ -1052,6 +1053,299 @@ rt_status rt_layer_norm_backward(const void* dy, const int64_t dy_stride[3], con
     a.partial = static_cast<float*>(workspace);
     return hip_status(rt::launch_norm_backward(a, norm_parts(dims), static_cast<hipStream_t>(stream)),
                       "layer norm gradient launch");
+}
+
+// ---- rotary positions ----------------------------------------------------------------------
+
+namespace {
+
+// How a thread's pieces and heads are chosen: the widest piece that all rows start on and hold whole numbers of, and as
+// many heads as leave 16 waves to a CU (a token's angles are formed once for them all).
+void set_rope(rt::RopeArgs& a, std::initializer_list<std::pair<const void*, const int64_t*>> ts) {
+    const int64_t size = type_bytes(a.type), n[3] = {a.B, a.H, a.T};
+    a.vec = 1;
+    for (int v : {8, 4}) {
+        if (v * size > 16 || a.D % v || (a.half && a.pairs % v)) continue;
+        bool fits = true;
+        for (const auto& t : ts) {
+            fits = fits && reinterpret_cast<uintptr_t>(t.first) % (uintptr_t)(v * size) == 0;
+            for (int i = 0; i < 3; ++i) fits = fits && (n[i] < 2 || t.second[i] % v == 0);
+        }
+        if (fits) {
+            a.vec = v;
+            break;
+        }
+    }
+    const int64_t one = std::max<int64_t>(1, (int64_t)a.B * a.T * rt::rope_places(a)), want = 256 * 16 * 64;
+    const int64_t groups = std::min(ceil_div(want, one), ceil_div(a.H, rt::kRopeAhead));
+    a.each = (int32_t)(ceil_div(ceil_div(a.H, groups), rt::kRopeAhead) * rt::kRopeAhead);
+    a.groups = (int32_t)ceil_div(a.H, a.each);
+}
+
+rt_status rope(const void* x, const int64_t* x_stride, const void* positions, const double* freq, const int32_t* axis,
+               float amplitude, const rt_rope_dims& d, bool inverse, void* y, const int64_t* y_stride, void* stream) {
+    if (d.B < 0 || d.H < 0 || d.T < 0) return fail(RT_EINVAL, "negative dims B=%d H=%d T=%d", d.B, d.H, d.T);
+    if (d.type != RT_BF16 && d.type != RT_F16 && d.type != RT_F32) return fail(RT_EUNSUPPORTED, "type=%d", d.type);
+    if (d.position_type != RT_POS_I32 && d.position_type != RT_POS_I64 && d.position_type != RT_POS_F32)
+        return fail(RT_EUNSUPPORTED, "position_type=%d", d.position_type);
+    if (d.layout != RT_ROPE_INTERLEAVED && d.layout != RT_ROPE_HALF) return fail(RT_EUNSUPPORTED, "layout=%d", d.layout);
+    if (d.D < 2) return fail(RT_EINVAL, "width D=%d (need >= 2)", d.D);
+    if (d.D > 16384) return fail(RT_EUNSUPPORTED, "width D=%d (supported: up to 16384)", d.D);
+    if (d.rotated < 2 || d.rotated > d.D || d.rotated % 2)
+        return fail(RT_EINVAL, "rotated=%d (need an even number of 2 to D=%d elements)", d.rotated, d.D);
+    if (d.axes < 1) return fail(RT_EINVAL, "axes=%d (need >= 1)", d.axes);
+    if (d.axes > 16) return fail(RT_EUNSUPPORTED, "axes=%d (supported: up to 16)", d.axes);
+    if (!std::isfinite(amplitude)) return fail(RT_EINVAL, "amplitude is not finite");
+    if (d.B == 0 || d.H == 0 || d.T == 0) return ok();
+    if ((int64_t)d.T * d.D >= (int64_t)1 << 32 || (int64_t)d.B * d.H > INT32_MAX ||
+        (int64_t)d.B * d.H >= ((int64_t)1 << 48) / d.T)
+        return fail(RT_EINVAL, "tensor too large");
+    const rt_norm_dims rows{d.B, d.H, d.T, d.D, d.type, d.type, 1};
+    int64_t x_span = 0, y_span = 0;
+    RT_TRY(check_rows(x, x_stride, rows, false, "x", &x_span));
+    RT_TRY(check_rows(y, y_stride, rows, true, "y", &y_span));
+    const int64_t pos_size = d.position_type == RT_POS_I64 ? 8 : 4, sets = d.per_sample ? d.B : 1;
+    if (!positions) return fail(RT_EINVAL, "positions is NULL");
+    if (reinterpret_cast<uintptr_t>(positions) % (uintptr_t)pos_size) return fail(RT_EINVAL, "positions is not aligned to its elements");
+    if (!freq) return fail(RT_EINVAL, "freq is NULL");
+    if (reinterpret_cast<uintptr_t>(freq) % 8) return fail(RT_EINVAL, "freq is not 8-byte aligned");
+    if (d.axes > 1) RT_TRY(check_stat(axis, "axis"));
+    bool same = x == y;  // in place: every thread reads its elements before it writes them
+    const int64_t n[3] = {d.B, d.H, d.T};
+    for (int i = 0; i < 3; ++i) same = same && (n[i] < 2 || x_stride[i] == y_stride[i]);
+    const int64_t np = sets * d.T * d.axes * pos_size, nf = (int64_t)d.rotated / 2 * 8;
+    RT_TRY(check_no_overlap(y, y_span, "y", {{positions, np}, {freq, nf}, {d.axes > 1 ? axis : nullptr, nf / 2}}, "an input"));
+    if (!same) RT_TRY(check_no_overlap(y, y_span, "y", {{x, x_span}}, "x"));
+    rt::RopeArgs a{};
+    a.x = x;
+    a.y = y;
+    a.positions = positions;
+    a.freq = freq;
+    a.axis = axis;
+    for (int i = 0; i < 3; ++i) {
+        a.xs[i] = n[i] > 1 ? x_stride[i] : 0;
+        a.ys[i] = n[i] > 1 ? y_stride[i] : 0;
+    }
+    a.B = d.B;
+    a.H = d.H;
+    a.T = d.T;
+    a.D = d.D;
+    a.pairs = d.rotated / 2;
+    a.axes = d.axes;
+    a.type = d.type;
+    a.pos_type = d.position_type;
+    a.half = d.layout == RT_ROPE_HALF;
+    a.per_sample = d.per_sample != 0;
+    a.inverse = inverse;
+    a.amplitude = amplitude;
+    set_rope(a, {{x, x_stride}, {y, y_stride}});
+    if (rt::rope_blocks(a) >= (int64_t)1 << 24) return fail(RT_EINVAL, "tensor too large");  // 256 threads each, in one launch
+    return hip_status(rt::launch_rope(a, static_cast<hipStream_t>(stream)), "rotary position launch");
+}
+
+}  // namespace
+
+rt_status rt_rope(const void* x, const int64_t x_stride[3], const void* positions, const double* freq, const int32_t* axis,
+                  float amplitude, rt_rope_dims dims, void* y, const int64_t y_stride[3], void* stream) {
+    return rope(x, x_stride, positions, freq, axis, amplitude, dims, false, y, y_stride, stream);
+}
+
+rt_status rt_rope_backward(const void* dy, const int64_t dy_stride[3], const void* positions, const double* freq,
+                           const int32_t* axis, float amplitude, rt_rope_dims dims, void* dx, const int64_t dx_stride[3],
+                           void* stream) {
+    return rope(dy, dy_stride, positions, freq, axis, amplitude, dims, true, dx, dx_stride, stream);
+}
+
+// ---- differential attention ----------------------------------------------------------------
+
+namespace {
+
+rt_status check_diff(const rt_diff_dims& d) {
+    if (d.B < 0 || d.H < 0 || d.Tq < 0 || d.Tk < 0)
+        return fail(RT_EINVAL, "negative dims B=%d H=%d Tq=%d Tk=%d", d.B, d.H, d.Tq, d.Tk);
+    if (d.D != 64 && d.D != 72) return fail(RT_EUNSUPPORTED, "head width D=%d (supported: 64, 72)", d.D);
+    const int64_t bh = (int64_t)d.B * d.H, t = std::max(d.Tq, d.Tk);
+    if (bh >= (int64_t)1 << 23) return fail(RT_EINVAL, "B*H too large");
+    // buffer record counts and offsets within one head are 32-bit, as in the other attention calls; values are 2 D wide
+    if (t * d.D * 4 > (int64_t)1 << 30) return fail(RT_EINVAL, "Tq=%d Tk=%d too long for one head", d.Tq, d.Tk);
+    if (bh * t * d.D * 2 >= (int64_t)1 << 40) return fail(RT_EINVAL, "tensor too large");
+    // threads of a launch: 256 for every tile of 128 rows, and 16 for each row in whole 64
+    if (bh * whole64((int32_t)t) >= (int64_t)1 << 28) return fail(RT_EINVAL, "too many rows: B=%d H=%d Tq=%d Tk=%d", d.B, d.H, d.Tq, d.Tk);
+    return RT_OK;
+}
+
+// Bytes of the calls' tensors
+struct DiffBytes {
+    int64_t q, k, v, o, stat, lam, lens;
+};
+DiffBytes diff_bytes(const rt_diff_dims& d, int32_t n_lam) {
+    const int64_t bh = (int64_t)d.B * d.H;
+    return {bh * d.Tq * d.D * 4, bh * d.Tk * d.D * 4, bh * d.Tk * d.D * 4, bh * d.Tq * d.D * 4, bh * d.Tq * 8, (int64_t)n_lam * 4,
+            (int64_t)d.B * 4};
+}
+
+// Forward: waves of a workgroup, and workgroups that share a tile's keys where there are few tiles.
+int32_t diff_waves(const rt_diff_dims& d) { return d.Tq <= 32 ? 1 : 4; }
+int32_t diff_split(const rt_diff_dims& d) {
+    const int64_t w = diff_waves(d), n = (int64_t)d.B * d.H * ceil_div(d.Tq, 32 * w), stages = ceil_div(d.Tk, w == 1 ? 32 : 64);
+    const int64_t s = std::min((w == 1 ? 1024 : 512) / std::max<int64_t>(n, 1), stages / 4);
+    return s > 1 ? (int32_t)s : 1;
+}
+int64_t diff_workspace(const rt_diff_dims& d) {
+    const int64_t s = diff_split(d);
+    return std::max<int64_t>(16, s > 1 ? (int64_t)d.B * d.H * s * 2 * d.Tq * (2 * d.D + 3) * 4 : 0);
+}
+
+// Backward: the same for tiles of keys and of queries.
+void diff_back_split(const rt_diff_dims& d, int32_t* k, int32_t* q) {
+    const int64_t bh = (int64_t)d.B * d.H, sk = ceil_div(d.Tq, 64), sq = ceil_div(d.Tk, 64);  // stages of their walks
+    const int64_t n = bh * (ceil_div(d.Tk, rt::kDiffRows) + ceil_div(d.Tq, rt::kDiffRows));
+    const int64_t s = 512 / std::max<int64_t>(n, 1);
+    *k = (int32_t)std::max<int64_t>(1, std::min(s, sk / 4));
+    *q = (int32_t)std::max<int64_t>(1, std::min(s, sq / 4));
+    if (std::max(sk - ceil_div(sk, *k), sq - ceil_div(sq, *q)) < 8) *k = *q = 1;
+}
+int64_t diff_vals(const rt_diff_dims& d) { return (int64_t)d.B * d.H * 4 * whole64(d.Tq); }
+int64_t diff_part_k(const rt_diff_dims& d, int64_t split) {
+    return (int64_t)d.B * d.H * ceil_div(d.Tk, rt::kDiffRows) * split * 4 * rt::kDiffRows * d.D;
+}
+int64_t diff_part_q(const rt_diff_dims& d, int64_t split) {
+    return (int64_t)d.B * d.H * ceil_div(d.Tq, rt::kDiffRows) * split * 2 * rt::kDiffRows * d.D;
+}
+int64_t diff_back_workspace(const rt_diff_dims& d) {
+    int32_t k = 1, q = 1;
+    diff_back_split(d, &k, &q);
+    const int64_t parts = k > 1 || q > 1 ? diff_part_k(d, k) + diff_part_q(d, q) : 0;
+    return std::max<int64_t>(16, (diff_vals(d) + parts) * 4);
+}
+
+// What both calls check and set alike.
+rt_status diff_args(const void* q, const void* k, const void* v, const float* lam, int32_t n_lam, const int32_t* k_lens,
+                    const rt_diff_dims& d, rt::DiffArgs* out) {
+    if (n_lam != 1 && n_lam != d.H) return fail(RT_EINVAL, "n_lam=%d (need 1 or H=%d)", n_lam, d.H);
+    if (d.Tq > 0 && d.B > 0 && d.H > 0) RT_TRY(check_tensor(q, "q"));
+    if (d.Tk > 0 && d.B > 0 && d.H > 0) {
+        RT_TRY(check_tensor(k, "k"));
+        RT_TRY(check_tensor(v, "v"));
+    }
+    if (n_lam > 0) RT_TRY(check_stat(lam, "lam"));
+    if (k_lens) RT_TRY(check_stat(k_lens, "k_lens"));
+    rt::DiffArgs a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.lam = lam;
+    a.lam_step = n_lam == d.H && d.H > 1 ? 1 : 0;
+    a.k_lens = k_lens;
+    a.H = d.H;
+    a.Tq = d.Tq;
+    a.Tk = d.Tk;
+    a.n_bh = d.B * d.H;
+    a.scale_nat = (float)(1.0 / std::sqrt((double)d.D));
+    a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d.D));
+    *out = a;
+    return RT_OK;
+}
+
+}  // namespace
+
+rt_status rt_attn_diff_workspace(rt_diff_dims dims, int64_t* bytes) {
+    if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
+    RT_TRY(check_diff(dims));
+    *bytes = diff_workspace(dims);
+    return ok();
+}
+
+rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float* lam, int32_t n_lam, const int32_t* k_lens,
+                       rt_diff_dims dims, void* o, void* o2, float* row_max, float* row_sum, void* workspace,
+                       int64_t workspace_bytes, void* stream) {
+    RT_TRY(check_diff(dims));
+    rt::DiffArgs a{};
+    if (dims.B == 0 || dims.H == 0 || dims.Tq == 0) return ok();
+    RT_TRY(diff_args(q, k, v, lam, n_lam, k_lens, dims, &a));
+    RT_TRY(check_tensor(o, "o"));
+    const int given = (o2 != nullptr) + (row_max != nullptr) + (row_sum != nullptr);
+    if (given % 3) return fail(RT_EINVAL, "o2, row_max and row_sum are written together or not at all");
+    if (given) {
+        RT_TRY(check_tensor(o2, "o2"));
+        RT_TRY(check_stat(row_max, "row_max"));
+        RT_TRY(check_stat(row_sum, "row_sum"));
+    }
+    const int64_t need = diff_workspace(dims);
+    a.split = diff_split(dims);
+    const void* ws = a.split > 1 ? workspace : nullptr;
+    if (a.split > 1) {
+        RT_TRY(check_tensor(workspace, "workspace"));
+        if (workspace_bytes < need)
+            return fail(RT_ECAPACITY, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+    }
+    const DiffBytes n = diff_bytes(dims, n_lam);
+    RT_TRY(check_ranges({{{o, n.o}, "o"}, {{o2, n.o}, "o2"}, {{row_max, n.stat}, "row_max"}, {{row_sum, n.stat}, "row_sum"},
+                         {{ws, need}, "workspace"}},
+                        {{q, n.q}, {k, n.k}, {v, n.v}, {lam, n.lam}, {k_lens, n.lens}}));
+    a.o = static_cast<uint16_t*>(o);
+    a.o2 = static_cast<uint16_t*>(o2);
+    a.row_max = row_max;
+    a.row_sum = row_sum;
+    a.waves = diff_waves(dims);
+    a.part = static_cast<float*>(workspace);
+    return hip_status(rt::launch_diff(a, dims.D, static_cast<hipStream_t>(stream)), "differential attention launch");
+}
+
+rt_status rt_attn_diff_backward_workspace(rt_diff_dims dims, int64_t* bytes) {
+    if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
+    RT_TRY(check_diff(dims));
+    *bytes = diff_back_workspace(dims);
+    return ok();
+}
+
+rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, const float* lam, int32_t n_lam,
+                                const int32_t* k_lens, const void* o, const void* o2, const float* row_max,
+                                const float* row_sum, const void* d_o, rt_diff_dims dims, void* dq, void* dk, void* dv,
+                                float* d_lam, void* workspace, int64_t workspace_bytes, void* stream) {
+    RT_TRY(check_diff(dims));
+    rt::DiffArgs a{};
+    RT_TRY(diff_args(q, k, v, lam, n_lam, k_lens, dims, &a));
+    if (n_lam > 0) RT_TRY(check_stat(d_lam, "d_lam"));
+    const bool rows = a.n_bh > 0 && dims.Tq > 0, cols = a.n_bh > 0 && dims.Tk > 0;
+    if (rows) {
+        RT_TRY(check_tensor(o, "o"));
+        RT_TRY(check_tensor(o2, "o2"));
+        RT_TRY(check_stat(row_max, "row_max"));
+        RT_TRY(check_stat(row_sum, "row_sum"));
+        RT_TRY(check_tensor(d_o, "d_o"));
+        RT_TRY(check_tensor(dq, "dq"));
+        RT_TRY(check_tensor(workspace, "workspace"));
+    }
+    if (cols) {
+        RT_TRY(check_tensor(dk, "dk"));
+        RT_TRY(check_tensor(dv, "dv"));
+    }
+    const int64_t need = diff_back_workspace(dims);
+    if (rows && workspace_bytes < need)
+        return fail(RT_ECAPACITY, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
+    const DiffBytes n = diff_bytes(dims, n_lam);
+    RT_TRY(check_ranges({{{rows ? dq : nullptr, n.q}, "dq"}, {{cols ? dk : nullptr, n.k}, "dk"}, {{cols ? dv : nullptr, n.v}, "dv"},
+                         {{n_lam ? d_lam : nullptr, n.lam}, "d_lam"}, {{rows ? workspace : nullptr, need}, "workspace"}},
+                        {{q, n.q}, {k, n.k}, {v, n.v}, {lam, n.lam}, {k_lens, n.lens}, {o, n.o}, {o2, n.o}, {row_max, n.stat},
+                         {row_sum, n.stat}, {d_o, n.o}}));
+    a.o = static_cast<uint16_t*>(const_cast<void*>(o));
+    a.o2 = static_cast<uint16_t*>(const_cast<void*>(o2));
+    a.row_max = const_cast<float*>(row_max);
+    a.row_sum = const_cast<float*>(row_sum);
+    a.d_o = static_cast<const uint16_t*>(d_o);
+    a.dq = static_cast<uint16_t*>(dq);
+    a.dk = static_cast<uint16_t*>(dk);
+    a.dv = static_cast<uint16_t*>(dv);
+    a.d_lam = d_lam;
+    a.T64 = whole64(dims.Tq);
+    a.row_vals = static_cast<float*>(workspace);
+    diff_back_split(dims, &a.split_k, &a.split_q);
+    a.part_k = a.row_vals + diff_vals(dims);
+    a.part_q = a.part_k + diff_part_k(dims, a.split_k);
+    if (n_lam == 0) return ok();  // no heads
+    return hip_status(rt::launch_diff_backward(a, dims.D, static_cast<hipStream_t>(stream)),
+                      "differential attention gradient launch");
 }
 
 }  // extern "C"

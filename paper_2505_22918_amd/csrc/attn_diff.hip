@@ -1,0 +1,818 @@
+// Differential attention and its gradients (gfx950, CDNA4).
+//
+//   P_i = softmax(Q_i K_i^T / sqrt(D)), i = 1, 2, over the keys that a sample has;  O = P_1 V - lam P_2 V
+//
+//   dA = dO V^T,  delta_i = dO . (P_i V),  dS_1 = P_1 (dA - delta_1),  dS_2 = -lam P_2 (dA - delta_2)
+//   dV = (P_1 - lam P_2)^T dO,  dQ_i = dS_i K_i / sqrt(D),  dK_i = dS_i^T Q_i / sqrt(D),  dlam = -sum of delta_2
+//
+//   diff_fwd    32 queries of both maps to a wave: one pass over the keys, V read once for both
+//   diff_join   the parts of split walks
+//   diff_rows   per query row: log2 of both denominators, -delta_2, delta_2 - delta_1
+//   diff_bwd    dK_1, dK_2 and dV of 128 keys, or dQ_1 and dQ_2 of 128 queries, to a workgroup of four waves; dlam
+//   diff_sum    the parts of split walks
+//
+// The maps share V, dA and the product that forms dV: with D-wide maps and 2 D-wide values the gradient executes 28 D
+// multiplications and additions a pair of query and key (scores and dA are formed for dK, dV and again for dQ, so that
+// every sum stays in one wave's registers: no atomics, equal bits from equal calls); two calls of plain attention's
+// gradients over 2 D-wide values would execute 40 D.
+//
+// The products are transposed as in attn_grad_tiles.h: a 32x32x16 accumulator hands each lane 16 rows of the side
+// read from LDS for one own row, which is what the B operand of the next product takes, so that P and dS never leave
+// registers; they are rounded to bf16 there, as the matrix products take them.  Scores, statistics and sums are fp32.
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_common.h"
+#include "attn_grad_tiles.h"
+#include "heads.h"
+
+namespace rt {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---- rows in LDS ---------------------------------------------------------------------------
+
+// 256-byte rows' 16 slots are swizzled by the row, so that 16 rows of a row read (one slot) and the four rows of half a
+// transposed one (four slots) fall on different banks.
+template <int D>
+__device__ __forceinline__ int wide_swz(int r) {
+    return Geo<D>::SWZ ? ((r & 3) << 2) | ((r >> 2) & 3) : 0;
+}
+
+// A wave's reads of narrow rows (queries or keys, D wide) and of wide ones (values or output gradients, 2 D wide).
+// 72-wide heads: narrow rows' last 8 elements are half a k-step of the scores and a 16x16x32 product of the gradients,
+// of which they fill half; wide rows' last 16 fill both.
+template <int D>
+struct Reads {
+    static constexpr int NB = 2 * D, WB = 4 * D;   // bytes of a row
+    static constexpr int WS = 2 * D / 16;          // k-steps of a wide row
+    static constexpr bool TAIL = D == 72, SWZ = Geo<D>::SWZ;
+
+    lds_u8* lds;
+    int lane, l32, hi;
+    int n_rd, n_tr, n_t, w_rd, w_tr, w_t;
+
+    __device__ __forceinline__ void init(lds_u8* smem) {
+        lds = smem;
+        lane = threadIdx.x & 63;
+        l32 = lane & 31;
+        hi = lane >> 5;
+        // as in attn_grad_tiles.h: row l32, slot hi; transposed rows 4 hi + L / 4 (+ 8), which puts elements
+        // 32 dt + 16 hi .. + 15 on a lane's 16 accumulators
+        const int G4 = lane >> 4, L = lane & 15;
+        const int r = 4 * hi + (L >> 2), d = 16 * (L & 1) + 8 * (G4 & 1) + 4 * ((L >> 1) & 1);
+        n_rd = l32 * NB + ((hi ^ swz<D>(l32)) * 16);
+        n_tr = r * NB + (((d >> 3) ^ swz<D>(r)) * 16) + (d & 7) * 2;
+        w_rd = l32 * WB + ((hi ^ wide_swz<D>(l32)) * 16);
+        w_tr = r * WB + (((d >> 3) ^ wide_swz<D>(r)) * 16) + (d & 7) * 2;
+        const int tr = 16 * (G4 & 1) + 4 * (G4 >> 1) + (L >> 2);
+        n_t = tr * NB + (64 + 4 * (L & 1)) * 2;
+        w_t = tr * WB + (128 + 4 * (L & 3)) * 2;
+    }
+    __device__ __forceinline__ bf16x8 n_row(int base, int s) const {
+        return *(const lds_bf16x8*)(lds + (SWZ ? (n_rd ^ (32 * s)) + base : n_rd + base + 32 * s));
+    }
+    __device__ __forceinline__ bf16x8 n_row_tail(int base, int zero) const {
+        return *(const lds_bf16x8*)(lds + (hi ? zero : n_rd + base + 128));
+    }
+    __device__ __forceinline__ bf16x8 w_row(int base, int s) const {
+        return *(const lds_bf16x8*)(lds + (SWZ ? (w_rd ^ (32 * s)) + base : w_rd + base + 32 * s));
+    }
+    static __device__ __forceinline__ bf16x8 tr_read(const lds_u8* p, const lds_u8* p8) {
+        const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p);
+        const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)p8);
+        return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    __device__ __forceinline__ bf16x8 n_col(int base, int dt, int ks) const {
+        const lds_u8* p = lds + base + 16 * ks * NB;
+        return SWZ ? tr_read(p + (n_tr ^ (64 * dt)), p + 8 * NB + (n_tr ^ (64 * dt) ^ 32))
+                   : tr_read(p + n_tr + 64 * dt, p + 8 * NB + n_tr + 64 * dt);
+    }
+    __device__ __forceinline__ bf16x8 w_col(int base, int dt, int ks) const {
+        const lds_u8* p = lds + base + 16 * ks * WB;
+        return SWZ ? tr_read(p + (w_tr ^ (64 * dt)), p + 8 * WB + (w_tr ^ (64 * dt) ^ 32))
+                   : tr_read(p + w_tr + 64 * dt, p + 8 * WB + w_tr + 64 * dt);
+    }
+    __device__ __forceinline__ bf16x8 n_col_tail(int base) const { return tr_read(lds + base + n_t, lds + base + n_t + 8 * NB); }
+    __device__ __forceinline__ bf16x8 w_col_tail(int base) const { return tr_read(lds + base + w_t, lds + base + w_t + 8 * WB); }
+
+    // rows row0 .. + 31 of x (zeros from row `end` on): lane holds row l32, elements 16 s + 8 hi ..
+    template <int S>
+    __device__ __forceinline__ void own_rows(const uint16_t* x, int bytes, int row0, int end, bf16x8 (&to)[S],
+                                             bf16x8* tail) const {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)x, (short)0, end * bytes, 0x00020000);
+        const int off = (row0 + l32) * bytes;
+        auto load = [&](int o) { return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, o, 0, 0)); };
+#pragma unroll
+        for (int s = 0; s < S; ++s) to[s] = load(off + 32 * s + 16 * hi);
+        if (tail) *tail = load(hi ? kOob : off + 128);
+    }
+};
+
+__device__ __forceinline__ bf16x8 op(const uint32_t (&p)[8], int ks) {
+    return __builtin_bit_cast(bf16x8, u32x4{p[4 * ks], p[4 * ks + 1], p[4 * ks + 2], p[4 * ks + 3]});
+}
+// the two operands of 16 contraction rows become two of 32 for the halves of the own rows (attn_tiles.h)
+__device__ __forceinline__ void halves(const uint32_t (&p)[8], uint32_t (&y)[8]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        auto s = __builtin_amdgcn_permlane16_swap(p[r], p[4 + r], false, false);
+        y[r] = s[0];
+        y[4 + r] = s[1];
+    }
+}
+__device__ __forceinline__ f32x4 mma16(const bf16x8& x, const bf16x8& y, const f32x4& z) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0);
+}
+
+// Two stages of BS rows of both maps' narrow rows and of the wide ones (and, VALS, of four values a row), filled and
+// read by W waves: the stage after the one in use is asked for when all waves are through the one before it.  Rows past
+// the end read as zeros.
+template <int D, int W, int BS, bool VALS>
+struct DiffRing {
+    static constexpr int NB = 2 * D, WB = 4 * D, NT = BS * NB, WT = BS * WB;
+    static constexpr int WIDE = 2 * NT, VAL = WIDE + WT, STAGE = VAL + (VALS ? BS * 16 : 0);
+    static constexpr int ZERO = 2 * STAGE, LDS = ZERO + 64;
+    static_assert(!VALS || BS * 16 % 512 == 0, "values in one load");
+
+    uint32_t lds0;
+    int lane, w;
+    int from_n[2], from_w, from_v;
+    i32x4 rs[3], vs;
+
+    __device__ __forceinline__ void init(lds_u8* lds, const uint16_t* x1, const uint16_t* x2, const uint16_t* y, int rows) {
+        lds0 = (uint32_t)(uintptr_t)lds;
+        lane = threadIdx.x & 63;
+        w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        rs[0] = buffer_rsrc(x1, rows * NB);
+        rs[1] = buffer_rsrc(x2, rows * NB);
+        rs[2] = buffer_rsrc(y, rows * WB);
+        // a lane's source offset in a kilobyte (8 narrow rows, odd and even ones; 4 wide ones, see wide_of)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+            from_n[p] = Geo<D>::SWZ ? (lane >> 3) * NB + (((lane & 7) ^ swz<D>((lane >> 3) | (p << 3))) * 16) : lane * 16;
+        from_w = Geo<D>::SWZ ? (lane >> 4) * WB + (((lane & 15) ^ wide_swz<D>(lane >> 4)) * 16) : lane * 16;
+        if (threadIdx.x < 4) *(lds_u32x4*)(lds + ZERO + 16 * threadIdx.x) = u32x4{};
+    }
+    __device__ __forceinline__ void init_values(const float* vals, int T64) {
+        vs = buffer_rsrc(vals, T64 * 16);
+        from_v = (lane / (BS / 4)) * T64 * 4 + (lane % (BS / 4)) * 16;
+    }
+    __device__ __forceinline__ int narrow_of(int kb) const { return kb & 1 ? from_n[1] : from_n[0]; }
+    __device__ __forceinline__ int wide_of(int kb) const { return Geo<D>::SWZ ? from_w ^ ((kb & 3) * 16) : from_w; }
+    template <int SIZE, bool WD>
+    __device__ __forceinline__ void fill(uint32_t dst, int at, const i32x4& r) const {
+        constexpr int FULL = SIZE / (1024 * W), REST = (SIZE - FULL * 1024 * W) / (16 * W);
+        static_assert(FULL * 1024 * W + REST * 16 * W == SIZE && (REST == 0 || !Geo<D>::SWZ), "even shares");
+#pragma unroll
+        for (int n = 0; n < FULL; ++n) {
+            const int kb = n * W + w;
+            dma16(__builtin_amdgcn_readfirstlane(dst + kb * 1024), (WD ? wide_of(kb) : narrow_of(kb)) + at + kb * 1024, r);
+        }
+        if (REST) {
+            const int b = FULL * W * 1024 + w * REST * 16;
+            if (lane < REST) dma16(__builtin_amdgcn_readfirstlane(dst + b), lane * 16 + at + b, r);
+        }
+    }
+    __device__ __forceinline__ void load(int to, int row0) const {
+        const uint32_t dst = lds0 + to;
+        fill<NT, false>(dst, row0 * NB, rs[0]);
+        fill<NT, false>(dst + NT, row0 * NB, rs[1]);
+        fill<WT, true>(dst + WIDE, row0 * WB, rs[2]);
+        if (VALS && w == 0 && lane < BS) dma16(__builtin_amdgcn_readfirstlane(dst + VAL), from_v + row0 * 4, vs);
+    }
+    // the stage asked for has landed, and every wave is through the one before it
+    __device__ __forceinline__ void turn() const {
+        wait_vm<0>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (W > 1) __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+};
+
+__device__ __forceinline__ int keys_of(const DiffArgs& a, int b) {
+    if (!a.k_lens) return a.Tk;
+    const int n = a.k_lens[b];
+    return n < 0 ? 0 : (n > a.Tk ? a.Tk : n);
+}
+
+// ---- forward -------------------------------------------------------------------------------
+
+constexpr float kMove = 24.0f;  // the running max moves when a probability against it passes 2^kMove
+
+// Workgroups of W waves, 32 queries each.  SPLIT: a part of the keys, whose sums against their own running max go to
+// a.part ([tile's head][part][map][query][2 D], then [..][3] of the max in score units, the sum and the true max).
+template <int D, int W, bool STATS, bool SPLIT>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 1 ? 1 : 2, W == 1 ? 1 : 2))) void
+diff_fwd(DiffArgs a, int n_items, int per_xcd) {
+    constexpr int BS = W == 1 ? 32 : 64;
+    using R = DiffRing<D, W, BS, false>;
+    constexpr int NB = R::NB, WB = R::WB;
+    constexpr bool TAIL = D == 72;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[R::LDS];
+    lds_u8* const lds = (lds_u8*)smem;
+
+    int item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), part = 0;
+    if (item >= n_items) return;
+    if (SPLIT) {
+        part = item % a.split;
+        item /= a.split;
+    }
+    const int n_tile = (a.Tq + 32 * W - 1) / (32 * W), bh = item / n_tile, b = bh / a.H;
+    const int row0 = ((item - bh * n_tile) * W + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 32;
+    const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
+    const int s0 = SPLIT ? (int)((int64_t)n_st * part / a.split) : 0, s1 = SPLIT ? (int)((int64_t)n_st * (part + 1) / a.split) : n_st;
+
+    R ring;
+    ring.init(lds, a.k + (size_t)(2 * bh) * a.Tk * D, a.k + (size_t)(2 * bh + 1) * a.Tk * D, a.v + (size_t)bh * a.Tk * (2 * D), keys);
+    ring.load(0, s0 * BS);
+    Reads<D> rd;
+    rd.init(lds);
+    bf16x8 q[2][4], q_tail[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        rd.own_rows(a.q + (size_t)(2 * bh + i) * a.Tq * D, NB, row0, a.Tq, q[i], TAIL ? &q_tail[i] : nullptr);
+
+    f32x16 acc[2][4];
+    f32x4 tacc[2][2];
+    float m_run[2], m_top[2], l_run[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) acc[i][d] = f32x16{};
+        tacc[i][0] = tacc[i][1] = f32x4{};
+        m_run[i] = -1e30f;  // finite: a chunk without keys gives p = 0, not NaN
+        m_top[i] = -INFINITY;
+        l_run[i] = 0.f;
+    }
+    // a value of each query as the tails' accumulators hold them: query 16 h + lane % 16
+    auto tail_bcast = [&](float x, int h) {
+        return __int_as_float(__builtin_amdgcn_ds_bpermute((16 * h + (rd.lane & 15)) << 2, __float_as_int(x)));
+    };
+    const float c2 = a.scale_log2;
+    int st = 0;
+    for (int s = s0; s < s1; ++s) {
+        ring.turn();
+        ring.load(R::STAGE - st, (s + 1) * BS);
+        if (row0 < a.Tq) {
+#pragma unroll
+            for (int h = 0; h < BS / 32; ++h) {
+                const int first = s * BS + 32 * h, cv = st + R::WIDE + 32 * h * WB;
+                uint32_t pk[2][8];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int cx = st + i * R::NT + 32 * h * NB;
+                    f32x16 sc = {};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sc = mma(rd.n_row(cx, k), q[i][k], sc);
+                    if (TAIL) sc = mma(rd.n_row_tail(cx, R::ZERO), q_tail[i], sc);
+                    if (first + 32 > keys) {
+                        const int lim = keys - first - 4 * rd.hi;
+#pragma unroll
+                        for (int x = 0; x < 16; ++x)
+                            if (8 * (x >> 2) + (x & 3) >= lim) sc[x] = -INFINITY;
+                    }
+                    float top = fmaxf(fmaxf(sc[0], sc[1]), sc[2]);
+#pragma unroll
+                    for (int x = 3; x < 15; x += 2) top = fmaxf(fmaxf(top, sc[x]), sc[x + 1]);
+                    top = fmaxf(top, sc[15]);
+                    if (STATS) m_top[i] = fmaxf(m_top[i], top);
+                    if (__builtin_amdgcn_ballot_w64((top - m_run[i]) * c2 > kMove)) {
+                        const float to = fmaxf(m_run[i], pair_max(top));
+                        const float alpha = __builtin_amdgcn_exp2f((m_run[i] - to) * c2);
+                        m_run[i] = to;
+                        l_run[i] *= alpha;
+#pragma unroll
+                        for (int d = 0; d < 4; ++d) acc[i][d] *= alpha;
+                        if (TAIL) {
+                            tacc[i][0] *= tail_bcast(alpha, 0);
+                            tacc[i][1] *= tail_bcast(alpha, 1);
+                        }
+                    }
+                    const float mc = m_run[i] * c2;
+                    float sum[2] = {0.f, 0.f};
+#pragma unroll
+                    for (int x = 0; x < 16; x += 2) {
+                        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -mc));
+                        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -mc));
+                        sum[(x >> 1) & 1] += e0 + e1;
+                        pk[i][x / 2] = pack_bf16(e0, e1);
+                    }
+                    l_run[i] += sum[0] + sum[1];
+                }
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const bf16x8 v = rd.w_col(cv, d, ks);
+                        acc[0][d] = mma(v, op(pk[0], ks), acc[0][d]);
+                        acc[1][d] = mma(v, op(pk[1], ks), acc[1][d]);
+                    }
+                if (TAIL) {
+                    const bf16x8 v = rd.w_col_tail(cv);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t y[8];
+                        halves(pk[i], y);
+                        tacc[i][0] = mma16(v, op(y, 0), tacc[i][0]);
+                        tacc[i][1] = mma16(v, op(y, 1), tacc[i][1]);
+                    }
+                }
+            }
+        }
+        st = R::STAGE - st;
+    }
+    wait_vm<0>();  // nothing may land in LDS after the workgroup has ended
+    if (row0 >= a.Tq) return;
+    const int row = row0 + rd.l32;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        l_run[i] = pair_sum(l_run[i]);
+        if (STATS) m_top[i] = pair_max(m_top[i]);
+    }
+    if (SPLIT) {
+        const size_t n_part = (size_t)a.n_bh * a.split, at = (size_t)bh * a.split + part;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float* o = a.part + (at * 2 + i) * a.Tq * (2 * D);
+            if (row < a.Tq) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        *reinterpret_cast<f32x4*>(o + (size_t)row * (2 * D) + 32 * d + 16 * rd.hi + 4 * u) =
+                            f32x4{acc[i][d][4 * u], acc[i][d][4 * u + 1], acc[i][d][4 * u + 2], acc[i][d][4 * u + 3]};
+                if (rd.hi == 0) {
+                    float* x = a.part + n_part * 2 * a.Tq * (2 * D) + ((at * 2 + i) * a.Tq + row) * 3;
+                    x[0] = m_run[i];
+                    x[1] = l_run[i];
+                    x[2] = STATS ? m_top[i] : 0.f;
+                }
+            }
+            if (TAIL) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int r = row0 + 16 * h + (rd.lane & 15);
+                    if (r < a.Tq) *reinterpret_cast<f32x4*>(o + (size_t)r * (2 * D) + 128 + 4 * (rd.lane >> 4)) = tacc[i][h];
+                }
+            }
+        }
+        return;
+    }
+    float inv[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        inv[i] = l_run[i] == 0.f ? 0.f : 1.0f / l_run[i];  // no keys: 0
+        if (STATS && rd.hi == 0 && row < a.Tq) {
+            const size_t at = (size_t)(2 * bh + i) * a.Tq + row;
+            a.row_max[at] = m_top[i] * a.scale_nat;
+            a.row_sum[at] = l_run[i] == 0.f ? 0.f : l_run[i] * __builtin_amdgcn_exp2f((m_run[i] - m_top[i]) * c2);
+        }
+    }
+    const float lam = a.lam[(bh - b * a.H) * a.lam_step];
+    uint16_t* const o = a.o + (size_t)bh * a.Tq * (2 * D);
+    uint16_t* const o2 = STATS ? a.o2 + (size_t)bh * a.Tq * (2 * D) : nullptr;
+    if (row < a.Tq) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint32_t x[4], y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int j = 8 * u + 2 * e;
+                    const float b0 = acc[1][d][j] * inv[1], b1 = acc[1][d][j + 1] * inv[1];
+                    x[e] = pack_bf16(__builtin_fmaf(-lam, b0, acc[0][d][j] * inv[0]), __builtin_fmaf(-lam, b1, acc[0][d][j + 1] * inv[0]));
+                    y[e] = pack_bf16(b0, b1);
+                }
+                const size_t at = (size_t)row * (2 * D) + 32 * d + 16 * rd.hi + 8 * u;
+                *reinterpret_cast<u32x4*>(o + at) = u32x4{x[0], x[1], x[2], x[3]};
+                if (STATS) *reinterpret_cast<u32x4*>(o2 + at) = u32x4{y[0], y[1], y[2], y[3]};
+            }
+    }
+    if (TAIL) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float i0 = tail_bcast(inv[0], h), i1 = tail_bcast(inv[1], h);
+            const int r = row0 + 16 * h + (rd.lane & 15);
+            if (r < a.Tq) {
+                const size_t at = (size_t)r * (2 * D) + 128 + 4 * (rd.lane >> 4);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float b0 = tacc[1][h][2 * e] * i1, b1 = tacc[1][h][2 * e + 1] * i1;
+                    reinterpret_cast<uint32_t*>(o + at)[e] = pack_bf16(__builtin_fmaf(-lam, b0, tacc[0][h][2 * e] * i0), __builtin_fmaf(-lam, b1, tacc[0][h][2 * e + 1] * i0));
+                    if (STATS) reinterpret_cast<uint32_t*>(o2 + at)[e] = pack_bf16(b0, b1);
+                }
+            }
+        }
+    }
+}
+
+// A query row of split walks: D / 2 threads, 4 elements of both maps each
+template <int D>
+__global__ __launch_bounds__(256) void diff_join(DiffArgs a, int64_t rows) {
+    constexpr int LANES = D / 2, EACH = 256 / LANES;
+    const int g = threadIdx.x / LANES, j = (threadIdx.x - g * LANES) * 4;
+    const int64_t i = (int64_t)blockIdx.x * EACH + g;
+    if (g >= EACH || i >= rows) return;
+    const int64_t bh = i / a.Tq, row = i - bh * a.Tq;
+    const float* stats = a.part + (size_t)a.n_bh * a.split * 2 * a.Tq * (2 * D);
+    f32x4 o[2];
+#pragma unroll
+    for (int map = 0; map < 2; ++map) {
+        auto at = [&](int p) { return ((bh * a.split + p) * 2 + map) * (size_t)a.Tq + row; };
+        float m = -INFINITY, top = -INFINITY, l = 0.f;
+        for (int p = 0; p < a.split; ++p) {
+            m = fmaxf(m, stats[at(p) * 3]);
+            top = fmaxf(top, stats[at(p) * 3 + 2]);
+        }
+        f32x4 s = {};
+#pragma unroll 4
+        for (int p = 0; p < a.split; ++p) {
+            const float f = __builtin_amdgcn_exp2f((stats[at(p) * 3] - m) * a.scale_log2);
+            l = __builtin_fmaf(f, stats[at(p) * 3 + 1], l);
+            s += *reinterpret_cast<const f32x4*>(a.part + at(p) * (2 * D) + j) * f;
+        }
+        o[map] = s * (l == 0.f ? 0.f : 1.0f / l);
+        if (a.row_max && j == 0) {
+            const size_t to = (size_t)(2 * bh + map) * a.Tq + row;
+            a.row_max[to] = top * a.scale_nat;
+            a.row_sum[to] = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
+        }
+    }
+    const f32x4 d = o[0] - o[1] * a.lam[(bh % a.H) * a.lam_step];
+    const size_t to = (size_t)i * (2 * D) + j;
+    reinterpret_cast<uint32_t*>(a.o + to)[0] = pack_bf16(d[0], d[1]);
+    reinterpret_cast<uint32_t*>(a.o + to)[1] = pack_bf16(d[2], d[3]);
+    if (a.o2) {
+        reinterpret_cast<uint32_t*>(a.o2 + to)[0] = pack_bf16(o[1][0], o[1][1]);
+        reinterpret_cast<uint32_t*>(a.o2 + to)[1] = pack_bf16(o[1][2], o[1][3]);
+    }
+}
+
+template <int D, int W, bool STATS, bool SPLIT>
+hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream) {
+    const int n = a.n_bh * ((a.Tq + 32 * W - 1) / (32 * W)) * (SPLIT ? a.split : 1), per = (n + 7) / 8;
+    hipLaunchKernelGGL((diff_fwd<D, W, STATS, SPLIT>), dim3(8 * per), dim3(64 * W), 0, stream, a, n, per);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !SPLIT) return e;
+    constexpr int EACH = 256 / (D / 2);
+    const int64_t rows = (int64_t)a.n_bh * a.Tq;
+    hipLaunchKernelGGL((diff_join<D>), dim3((uint32_t)((rows + EACH - 1) / EACH)), dim3(256), 0, stream, a, rows);
+    return hipGetLastError();
+}
+template <int D, int W>
+hipError_t launch_fwd_w(const DiffArgs& a, hipStream_t stream) {
+    if (a.split > 1) return a.o2 ? launch_fwd<D, W, true, true>(a, stream) : launch_fwd<D, W, false, true>(a, stream);
+    return a.o2 ? launch_fwd<D, W, true, false>(a, stream) : launch_fwd<D, W, false, false>(a, stream);
+}
+template <int D>
+hipError_t launch_fwd_d(const DiffArgs& a, hipStream_t stream) {
+    return a.waves == 1 ? launch_fwd_w<D, 1>(a, stream) : launch_fwd_w<D, 4>(a, stream);
+}
+
+// ---- backward ------------------------------------------------------------------------------
+
+// 16 lanes a row (the first two of them take a 72-wide head's last chunks too); rows are counted with each head's padded
+// to whole 64, whose values are zeros
+template <int D>
+__global__ __launch_bounds__(256) void diff_rows(DiffArgs a, int64_t rows) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const int c = threadIdx.x & 15;
+    if (i >= rows) return;
+    const int64_t bh = i / a.T64;
+    const int t = (int)(i - bh * a.T64);
+    float* vals = a.row_vals + bh * 4 * a.T64 + t;
+    if (t >= a.Tq) {
+        if (c < 4) vals[(size_t)c * a.T64] = 0.f;
+        return;
+    }
+    const int64_t row = bh * a.Tq + t;
+    float s = 0.f, s2 = 0.f;
+    auto add = [&](int ch) {
+        const size_t at = row * (2 * D) + 8 * ch;
+        const u32x4 x = *reinterpret_cast<const u32x4*>(a.o + at), x2 = *reinterpret_cast<const u32x4*>(a.o2 + at),
+                    y = *reinterpret_cast<const u32x4*>(a.d_o + at);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            s = __builtin_fmaf(lo_f(x[w]), lo_f(y[w]), s);
+            s = __builtin_fmaf(hi_f(x[w]), hi_f(y[w]), s);
+            s2 = __builtin_fmaf(lo_f(x2[w]), lo_f(y[w]), s2);
+            s2 = __builtin_fmaf(hi_f(x2[w]), hi_f(y[w]), s2);
+        }
+    };
+    add(c);
+    if (D == 72 && c < 2) add(16 + c);
+    s += dpp<0xB1>(s);
+    s2 += dpp<0xB1>(s2);
+    s += dpp<0x4E>(s);
+    s2 += dpp<0x4E>(s2);
+    s += dpp<0x141>(s);
+    s2 += dpp<0x141>(s2);
+    s += dpp<0x140>(s);
+    s2 += dpp<0x140>(s2);
+    if (c < 2) {
+        const size_t at = (size_t)(2 * bh + c) * a.Tq + t;
+        const float l = a.row_sum[at];
+        vals[(size_t)c * a.T64] = l == 0.f ? INFINITY : __builtin_fmaf(a.row_max[at], kLog2e, log2f(l));
+    }
+    // delta_1 = dO . O + lam delta_2
+    if (c == 2) vals[(size_t)2 * a.T64] = -s2;
+    if (c == 3) vals[(size_t)3 * a.T64] = s2 - __builtin_fmaf(a.lam[(bh % a.H) * a.lam_step], s2, s);
+}
+
+// dlam of head h (all heads where they share it): the sum of -delta_2, in 64 bits
+__device__ __forceinline__ void sum_lam(const DiffArgs& a, double* lds, int h) {
+    double s = 0.0;
+    const int step = a.lam_step ? a.H : 1;
+    for (int bh = h; bh < a.n_bh; bh += step) {
+        const float* x = a.row_vals + ((size_t)bh * 4 + 2) * a.T64;
+#pragma unroll 4
+        for (int t = threadIdx.x; t < a.T64; t += 256) s += x[t];
+    }
+    lds[threadIdx.x] = s;
+    for (int n = 128; n; n /= 2) {
+        __syncthreads();
+        if ((int)threadIdx.x < n) lds[threadIdx.x] += lds[threadIdx.x + n];
+    }
+    if (threadIdx.x == 0) a.d_lam[h] = (float)lds[0];
+}
+
+// Own rows K_1, K_2, V (KV) against X = Q_1, Q_2 and Y = dO of the queries, or own Q_1, Q_2, dO against K_1, K_2, V:
+// 32 own rows to a wave, 32 W to a workgroup.  SPLIT: against a part of the other side.
+template <int D, bool KV, int W, int BS, bool SPLIT>
+__device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int item, int part) {
+    using R = DiffRing<D, W, BS, KV>;
+    using Rd = Reads<D>;
+    constexpr int NB = R::NB, WB = R::WB, NW = KV ? 4 : 1;
+    constexpr bool TAIL = D == 72;
+    const int T = KV ? a.Tk : a.Tq, Tx = KV ? a.Tq : a.Tk;  // rows of the own side and of the other
+    const int n_tile = (T + 32 * W - 1) / (32 * W), bh = item / n_tile, b = bh / a.H;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = ((item - bh * n_tile) * W + wave) * 32;
+    const int keys = keys_of(a, b);
+    const int own_end = KV ? keys : T, x_end = KV ? Tx : keys;
+    const int tile0 = row0 - 32 * wave;
+    int n_st = (x_end + BS - 1) / BS;
+    if (KV && tile0 >= keys) n_st = 0;  // keys that the sample does not have
+    const int split = KV ? a.split_k : a.split_q;
+    const int s0 = SPLIT ? (int)((int64_t)n_st * part / split) : 0, s1 = SPLIT ? (int)((int64_t)n_st * (part + 1) / split) : n_st;
+
+    const size_t n_x = (size_t)(2 * bh) * Tx * D, n_own = (size_t)(2 * bh) * T * D;
+    const size_t w_x = (size_t)bh * Tx * (2 * D), w_own = (size_t)bh * T * (2 * D);
+    const uint16_t* x = (KV ? a.q : a.k) + n_x;
+    const uint16_t* own = (KV ? a.k : a.q) + n_own;
+    R ring;
+    ring.init(lds, x, x + (size_t)Tx * D, (KV ? a.d_o : a.v) + w_x, x_end);
+    const float* vals = a.row_vals + (size_t)bh * 4 * a.T64;
+    if (KV) ring.init_values(vals, a.T64);
+    ring.load(0, s0 * BS);
+    Rd rd;
+    rd.init(lds);
+    bf16x8 n_op[2][4], n_tail[2], w_op[Rd::WS];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rd.own_rows(own + (size_t)i * T * D, NB, row0, own_end, n_op[i], TAIL ? &n_tail[i] : nullptr);
+    rd.own_rows((KV ? a.v : a.d_o) + w_own, WB, row0, own_end, w_op, nullptr);
+    float log[2] = {INFINITY, INFINITY}, minus = 0.f, more = 0.f;  // of the own query
+    if (!KV && row0 + rd.l32 < T) {
+        log[0] = vals[row0 + rd.l32];
+        log[1] = vals[a.T64 + row0 + rd.l32];
+        minus = vals[2 * a.T64 + row0 + rd.l32];
+        more = vals[3 * a.T64 + row0 + rd.l32];
+    }
+    const float c2 = a.scale_log2, lam = a.lam[(bh - b * a.H) * a.lam_step];
+
+    f32x16 acc[2][2], wacc[NW];  // dK or dQ of each map; dV
+    f32x4 tacc[2][2], wtacc[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        acc[i][0] = acc[i][1] = f32x16{};
+        tacc[i][0] = tacc[i][1] = wtacc[i] = f32x4{};
+    }
+#pragma unroll
+    for (int d = 0; d < NW; ++d) wacc[d] = f32x16{};
+
+    int st = 0;
+    for (int s = s0; s < s1; ++s) {
+        ring.turn();
+        ring.load(R::STAGE - st, (s + 1) * BS);
+        if (row0 < own_end) {
+#pragma unroll
+            for (int h = 0; h < BS / 32; ++h) {
+                const int cw = st + R::WIDE + 32 * h * WB, first = s * BS + 32 * h;
+                // four values of a chunk's rows 8 j + 4 hi ..
+                auto value = [&](int n, int j) {
+                    return __builtin_bit_cast(f32x4, *(const lds_u32x4*)(lds + st + R::VAL + n * BS * 4 + (32 * h + 8 * j + 4 * rd.hi) * 4));
+                };
+                f32x16 dp;  // dA - delta_2
+                if (KV) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const f32x4 v = value(2, j);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) dp[4 * j + e] = v[e];
+                    }
+                } else {
+                    dp = f32x16{} + minus;
+                }
+#pragma unroll
+                for (int k = 0; k < Rd::WS; ++k) dp = mma(rd.w_row(cw, k), w_op[k], dp);
+                f32x16 p1;  // map 1's probabilities (KV)
+                uint32_t pk[8], ds[8];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int cx = st + i * R::NT + 32 * h * NB;
+                    f32x16 sc = {};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sc = mma(rd.n_row(cx, k), n_op[i][k], sc);
+                    if (TAIL) sc = mma(rd.n_row_tail(cx, R::ZERO), n_tail[i], sc);
+                    if (!KV && first + 32 > keys) {
+                        const int lim = keys - first - 4 * rd.hi;
+#pragma unroll
+                        for (int x = 0; x < 16; ++x)
+                            if (8 * (x >> 2) + (x & 3) >= lim) sc[x] = -INFINITY;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        f32x4 lg = {log[i], log[i], log[i], log[i]}, mo = {more, more, more, more};
+                        if (KV) lg = value(i, j);
+                        if (KV && i == 0) mo = value(3, j);
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            const int x = 4 * j + e;
+                            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -lg[e]));
+                            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -lg[e + 1]));
+                            if (i == 0) {
+                                ds[x / 2] = pack_bf16(e0 * (dp[x] + mo[e]), e1 * (dp[x + 1] + mo[e + 1]));
+                                p1[x] = e0;
+                                p1[x + 1] = e1;
+                            } else {
+                                ds[x / 2] = pack_bf16(e0 * dp[x], e1 * dp[x + 1]);
+                                if (KV) pk[x / 2] = pack_bf16(__builtin_fmaf(-lam, e0, p1[x]), __builtin_fmaf(-lam, e1, p1[x + 1]));
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[i][k & 1] = mma(rd.n_col(cx, k & 1, k >> 1), op(ds, k >> 1), acc[i][k & 1]);
+                    if (TAIL) {
+                        const bf16x8 c = rd.n_col_tail(cx);
+                        uint32_t y[8];
+                        halves(ds, y);
+                        tacc[i][0] = mma16(c, op(y, 0), tacc[i][0]);
+                        tacc[i][1] = mma16(c, op(y, 1), tacc[i][1]);
+                    }
+                }
+                if (KV) {
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                        for (int d = 0; d < NW; ++d) wacc[d] = mma(rd.w_col(cw, d, ks), op(pk, ks), wacc[d]);
+                    if (TAIL) {
+                        const bf16x8 c = rd.w_col_tail(cw);
+                        uint32_t y[8];
+                        halves(pk, y);
+                        wtacc[0] = mma16(c, op(y, 0), wtacc[0]);
+                        wtacc[1] = mma16(c, op(y, 1), wtacc[1]);
+                    }
+                }
+            }
+        }
+        st = R::STAGE - st;
+    }
+    wait_vm<0>();  // nothing may land in LDS after the workgroup has ended
+
+    // rows of a tile as fp32 [32][width] of a part, or rounded into the output (rows past the keys as zeros)
+    auto store = [&](const f32x16* c, int tiles, const f32x4* t, int t_n, int width, float f, float* to, uint16_t* out) {
+        const int row = row0 + rd.l32;
+        auto put = [&](int r, int col, float x0, float x1, float x2, float x3) {
+            if (SPLIT) {
+                *reinterpret_cast<f32x4*>(to + (r - row0) * width + col) = f32x4{x0, x1, x2, x3};
+            } else if (r < T) {
+                uint32_t* p = reinterpret_cast<uint32_t*>(out + (size_t)r * width + col);
+                p[0] = pack_bf16(x0, x1);
+                p[1] = pack_bf16(x2, x3);
+            }
+        };
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            if (d >= tiles) break;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                auto v = [&](int e) { return row >= own_end ? 0.f : c[d][4 * u + e] * f; };
+                put(row, 32 * d + 16 * rd.hi + 4 * u, v(0), v(1), v(2), v(3));
+            }
+        }
+        if (TAIL && 4 * (rd.lane >> 4) < t_n) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = row0 + 16 * h + (rd.lane & 15);
+                auto v = [&](int e) { return r >= own_end ? 0.f : t[h][e] * f; };
+                put(r, width - t_n + 4 * (rd.lane >> 4), v(0), v(1), v(2), v(3));
+            }
+        }
+    };
+    const float f2 = -lam * a.scale_nat;
+    constexpr int TILE = 32 * W * D;  // of one map
+    float* to = SPLIT ? (KV ? a.part_k : a.part_q) + ((size_t)item * split + part) * ((KV ? 4 : 2) * TILE) : nullptr;
+    uint16_t* const out = (KV ? a.dk : a.dq) + n_own;
+    store(acc[0], 2, tacc[0], 8, D, a.scale_nat, to + 32 * wave * D, out);
+    store(acc[1], 2, tacc[1], 8, D, f2, to + TILE + 32 * wave * D, out + (size_t)T * D);
+    if (KV) store(wacc, 4, wtacc, 16, 2 * D, 1.0f, to + 2 * TILE + 32 * wave * (2 * D), a.dv + w_own);
+}
+
+template <int D, bool SPLIT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_bwd(DiffArgs a, int n_lam, int n_k,
+                                                                                          int per_k, int n_q, int per_q) {
+    constexpr int W = kDiffRows / 32, BS = 64;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[DiffRing<D, W, BS, true>::LDS];
+    lds_u8* const lds = (lds_u8*)smem;
+    int g = blockIdx.x;
+    const int lam8 = (n_lam + 7) & ~7;  // (whole eights, so that a tile's XCD goes by its number)
+    if (g < lam8) {
+        if (g < n_lam) sum_lam(a, reinterpret_cast<double*>(smem), g);
+        return;
+    }
+    g -= lam8;
+    // dK and dV first, which have more to do
+    const bool kv = g < 8 * per_k;
+    if (!kv) g -= 8 * per_k;
+    const int split = kv ? a.split_k : a.split_q;
+    int item = (g & 7) * (kv ? per_k : per_q) + (g >> 3), part = 0;
+    if (item >= (kv ? n_k : n_q)) return;
+    if (SPLIT) {
+        part = item % split;
+        item /= split;
+    }
+    if (kv)
+        diff_walk<D, true, W, BS, SPLIT>(a, lds, item, part);
+    else
+        diff_walk<D, false, W, BS, SPLIT>(a, lds, item, part);
+}
+
+// Sums of a tile's parts: dK_1, dK_2, the halves of dV (blockIdx.y 0 .. 3; `tiles_k` of them in x), then dQ_1, dQ_2
+template <int D>
+__global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int tiles_k, int tiles_q) {
+    constexpr int TILE = kDiffRows * D;
+    const bool kv = blockIdx.y < 4;
+    if ((int)blockIdx.x >= (kv ? tiles_k : tiles_q)) return;
+    const int T = kv ? a.Tk : a.Tq, n_tile = (T + kDiffRows - 1) / kDiffRows, n = kv ? a.split_k : a.split_q;
+    const int bh = blockIdx.x / n_tile, row0 = (blockIdx.x - bh * n_tile) * kDiffRows;
+    const int width = kv && blockIdx.y >= 2 ? 2 * D : D, which = kv ? blockIdx.y : blockIdx.y - 4;
+    const size_t stride = (kv ? 4 : 2) * (size_t)TILE;
+    const float* part = (kv ? a.part_k : a.part_q) + (size_t)blockIdx.x * n * stride + (size_t)which * TILE;
+    uint16_t* out;
+    int skip = 0;  // elements of dV before this half
+    if (width == D) {
+        out = (kv ? a.dk : a.dq) + (size_t)(2 * bh + which) * T * D;
+    } else {
+        out = a.dv + (size_t)bh * T * (2 * D);
+        skip = (which - 2) * TILE;
+    }
+    const int j = blockIdx.z * 1024 + threadIdx.x * 4;
+    const int left = T - row0, size = (left < kDiffRows ? left : kDiffRows) * width;
+    if (j >= TILE || skip + j >= size) return;
+    f32x4 s = {};
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) s += *reinterpret_cast<const f32x4*>(part + p * stride + j);
+    uint32_t* to = reinterpret_cast<uint32_t*>(out + (size_t)row0 * width + skip + j);
+    to[0] = pack_bf16(s[0], s[1]);
+    to[1] = pack_bf16(s[2], s[3]);
+}
+
+template <int D>
+hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
+    const int64_t rows = (int64_t)a.n_bh * a.T64;
+    hipError_t e = hipSuccess;
+    if (rows > 0) {
+        hipLaunchKernelGGL((diff_rows<D>), dim3((uint32_t)((rows * 16 + 255) / 256)), dim3(256), 0, stream, a, rows);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const int tiles_k = a.n_bh * ((a.Tk + kDiffRows - 1) / kDiffRows), tiles_q = a.n_bh * ((a.Tq + kDiffRows - 1) / kDiffRows);
+    const bool split = a.split_k > 1 || a.split_q > 1;
+    const int n_k = tiles_k * a.split_k, n_q = tiles_q * a.split_q, per_k = (n_k + 7) / 8, per_q = (n_q + 7) / 8;
+    const int n_lam = a.lam_step ? a.H : 1;
+    const dim3 grid(((n_lam + 7) & ~7) + 8 * per_k + 8 * per_q);
+    if (!split) {
+        hipLaunchKernelGGL((diff_bwd<D, false>), grid, dim3(256), 0, stream, a, n_lam, n_k, per_k, n_q, per_q);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((diff_bwd<D, true>), grid, dim3(256), 0, stream, a, n_lam, n_k, per_k, n_q, per_q);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int most = tiles_k > tiles_q ? tiles_k : tiles_q;
+    hipLaunchKernelGGL((diff_sum<D>), dim3(most, 6, kDiffRows * D / 1024), dim3(256), 0, stream, a, tiles_k, tiles_q);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_diff(const DiffArgs& a, int D, hipStream_t stream) {
+    return D == 64 ? launch_fwd_d<64>(a, stream) : launch_fwd_d<72>(a, stream);
+}
+hipError_t launch_diff_backward(const DiffArgs& a, int D, hipStream_t stream) {
+    return D == 64 ? launch_bwd_d<64>(a, stream) : launch_bwd_d<72>(a, stream);
+}
+
+}  // namespace rt

@@ -34,7 +34,7 @@ def is_caching_step(t: int, full_steps: int, period: int) -> bool:
 
 
 def run(mask, qkv, n_steps, full_steps, period, lam, sigma, seed=0, diagnose=True, evolve=None, ratio=True,
-        qk_norm=None):
+        qk_norm=None, qk_rope=None):
     """Drives n_steps denoising steps of one attention layer.
 
     qkv: device bf16 (q, k, v) of step 0.  Each later step's inputs come from
@@ -43,12 +43,13 @@ def run(mask, qkv, n_steps, full_steps, period, lam, sigma, seed=0, diagnose=Tru
     ablation without the statistical reshape (cache O_full - O_sparse, later
     steps add it to the sparse output).  qk_norm: (weight, bias) pairs of the layer
     norms that each head's queries and keys pass through before attention, as
-    CogVideoX has them; what drifts are the rows before them.  Returns a list of per-step records (and
+    CogVideoX has them; what drifts are the rows before them.  qk_rope: (positions, RopePlan) of the
+    rotary positions that queries and keys then get.  Returns a list of per-step records (and
     the step outputs when ``diagnose`` is False, for callers that check them).
     """
     import torch
 
-    from . import StatCache, attn_cache, attn_sparse, layer_norm
+    from . import StatCache, attn_cache, attn_sparse, layer_norm, rope
 
     if evolve is None:
         def evolve(prev, t):
@@ -66,6 +67,8 @@ def run(mask, qkv, n_steps, full_steps, period, lam, sigma, seed=0, diagnose=Tru
         q, k, v = cur
         if qk_norm is not None:
             q, k = (layer_norm(x, *wb, eps=1e-6) for x, wb in zip((q, k), qk_norm))
+        if qk_rope is not None:
+            q, k = (rope(x, *qk_rope) for x in (q, k))
         caching = cache.is_caching_step(t) or cache.resid is None
         out = cache.attend(q, k, v, t)
         rec = {"t": t, "kind": ("full" if t < full_steps else "cache") if caching else "reshape"}
@@ -96,6 +99,26 @@ def run(mask, qkv, n_steps, full_steps, period, lam, sigma, seed=0, diagnose=Tru
     return records if diagnose else (records, outputs)
 
 
+def grid_rope(wl, device="cuda"):
+    """Positions and plan of rotary positions for a workload: frames, rows and columns of a video's tokens (text tokens
+    stay as they are), rows and columns of an image's, the token's number where there is no grid."""
+    import torch
+
+    from . import rope_plan, synth
+
+    t = torch.arange(wl.T - wl.n_text)
+    if wl.kind == synth.PAT_VIDEO3D:
+        hw = wl.grid_h * wl.grid_w
+        at = torch.stack([t // hw, t // wl.grid_w % wl.grid_h, t % wl.grid_w], -1)
+        widths = (wl.D // 8 * 2, (wl.D - wl.D // 8 * 2) // 4 * 2, (wl.D - wl.D // 8 * 2 + 2) // 4 * 2)
+    elif wl.kind == synth.PAT_LOCAL2D:
+        at, widths = torch.stack([t // wl.grid_w, t % wl.grid_w], -1), (wl.D // 4 * 2, (wl.D + 2) // 4 * 2)
+    else:
+        at, widths = t, None
+    at = torch.cat([torch.zeros((wl.n_text, *at.shape[1:]), dtype=at.dtype), at]).to(device)
+    return at, rope_plan(wl.D, widths=widths, device=device)
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     ap.add_argument("--workload", default="cogvideox_2b")
@@ -109,6 +132,8 @@ def main(argv=None):
                     help="the ablation without the statistical reshape (residual O_full - O_sparse)")
     ap.add_argument("--qk-norm", action="store_true",
                     help="queries and keys pass through a layer norm of each head's rows (weight 1, bias 0)")
+    ap.add_argument("--qk-rope", action="store_true",
+                    help="queries and keys get rotary positions by their place in the workload's grid")
     args = ap.parse_args(argv)
 
     import numpy as np
@@ -130,7 +155,7 @@ def main(argv=None):
         one, zero = torch.ones(wl.D, device="cuda"), torch.zeros(wl.D, device="cuda")
         norm = ((one, zero), (one, zero))
     recs = run(mask, qkv, args.steps, args.full_steps, args.period, args.lam, args.sigma, seed=args.seed,
-               ratio=not args.no_ratio, qk_norm=norm)
+               ratio=not args.no_ratio, qk_norm=norm, qk_rope=grid_rope(wl) if args.qk_rope else None)
     for r in recs:
         print(json.dumps(r), flush=True)
     rs = [r for r in recs if r["kind"] == "reshape"]
