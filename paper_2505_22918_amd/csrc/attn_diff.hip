@@ -41,6 +41,10 @@ __device__ __forceinline__ int wide_swz(int r) {
     return Geo<D>::SWZ ? ((r & 3) << 2) | ((r >> 2) & 3) : 0;
 }
 
+// hides a lane constant's value, so that what derives from it is formed anew (one v_xad_u32 a read) instead of held in
+// registers throughout a walk
+__device__ __forceinline__ void fresh(int& x) { asm volatile("" : "+v"(x)); }
+
 // A wave's reads of narrow rows (queries or keys, D wide) and of wide ones (values or output gradients, 2 D wide).
 // 72-wide heads: narrow rows' last 8 elements are half a k-step of the scores and a 16x16x32 product of the gradients,
 // of which they fill half; wide rows' last 16 fill both.
@@ -70,6 +74,27 @@ struct Reads {
         const int tr = 16 * (G4 & 1) + 4 * (G4 >> 1) + (L >> 2);
         n_t = tr * NB + (64 + 4 * (L & 1)) * 2;
         w_t = tr * WB + (128 + 4 * (L & 3)) * 2;
+    }
+    // offsets two to a register, from which unpack() forms them anew: a walk that is short of registers holds three
+    int pk[3];
+    __device__ __forceinline__ void pack() {
+        pk[0] = n_rd | n_tr << 16;
+        pk[1] = w_rd | w_tr << 16;
+        pk[2] = n_t | w_t << 16;
+    }
+    __device__ __forceinline__ void unpack() {
+        fresh(pk[0]);
+        fresh(pk[1]);
+        fresh(pk[2]);
+        n_rd = pk[0] & 0xffff;
+        n_tr = pk[0] >> 16;
+        w_rd = pk[1] & 0xffff;
+        w_tr = pk[1] >> 16;
+        n_t = pk[2] & 0xffff;
+        w_t = pk[2] >> 16;
+        fresh(lane);
+        l32 = lane & 31;
+        hi = lane >> 5;
     }
     __device__ __forceinline__ bf16x8 n_row(int base, int s) const {
         return *(const lds_bf16x8*)(lds + (SWZ ? (n_rd ^ (32 * s)) + base : n_rd + base + 32 * s));
@@ -135,11 +160,12 @@ struct DiffRing {
     static constexpr int NB = 2 * D, WB = 4 * D, NT = BS * NB, WT = BS * WB;
     static constexpr int WIDE = 2 * NT, VAL = WIDE + WT, STAGE = VAL + (VALS ? BS * 16 : 0);
     static constexpr int ZERO = 2 * STAGE, LDS = ZERO + 64;
+    static_assert(W == 1 || W == 4, "whole fours of kilobytes");
     static_assert(!VALS || BS * 16 % 512 == 0, "values in one load");
 
     uint32_t lds0;
     int lane, w;
-    int from_n[2], from_w, from_v;
+    int from_n[2], from_w, T64;
     i32x4 rs[3], vs;
 
     __device__ __forceinline__ void init(lds_u8* lds, const uint16_t* x1, const uint16_t* x2, const uint16_t* y, int rows) {
@@ -149,19 +175,25 @@ struct DiffRing {
         rs[0] = buffer_rsrc(x1, rows * NB);
         rs[1] = buffer_rsrc(x2, rows * NB);
         rs[2] = buffer_rsrc(y, rows * WB);
-        // a lane's source offset in a kilobyte (8 narrow rows, odd and even ones; 4 wide ones, see wide_of)
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-            from_n[p] = Geo<D>::SWZ ? (lane >> 3) * NB + (((lane & 7) ^ swz<D>((lane >> 3) | (p << 3))) * 16) : lane * 16;
-        from_w = Geo<D>::SWZ ? (lane >> 4) * WB + (((lane & 15) ^ wide_swz<D>(lane >> 4)) * 16) : lane * 16;
+        // (a wave of four fills kilobytes of one place in four: the same offsets every time)
+        from_n[0] = narrow_from(W == 4 ? w : 0);
+        from_n[1] = W == 4 ? from_n[0] : narrow_from(1);
+        from_w = wide_from(W == 4 ? w : 0);
         if (threadIdx.x < 4) *(lds_u32x4*)(lds + ZERO + 16 * threadIdx.x) = u32x4{};
     }
-    __device__ __forceinline__ void init_values(const float* vals, int T64) {
+    __device__ __forceinline__ void init_values(const float* vals, int T64_) {
+        T64 = T64_;
         vs = buffer_rsrc(vals, T64 * 16);
-        from_v = (lane / (BS / 4)) * T64 * 4 + (lane % (BS / 4)) * 16;
     }
-    __device__ __forceinline__ int narrow_of(int kb) const { return kb & 1 ? from_n[1] : from_n[0]; }
-    __device__ __forceinline__ int wide_of(int kb) const { return Geo<D>::SWZ ? from_w ^ ((kb & 3) * 16) : from_w; }
+    // a lane's source offset in kilobyte kb: 8 narrow rows, of odd and even ones, or 4 wide ones, of every fourth
+    __device__ __forceinline__ int narrow_from(int kb) const {
+        return Geo<D>::SWZ ? (lane >> 3) * NB + (((lane & 7) ^ swz<D>((lane >> 3) | ((kb & 1) << 3))) * 16) : lane * 16;
+    }
+    __device__ __forceinline__ int wide_from(int kb) const {
+        return Geo<D>::SWZ ? (lane >> 4) * WB + (((lane & 15) ^ wide_swz<D>((lane >> 4) | ((kb & 3) << 2))) * 16) : lane * 16;
+    }
+    __device__ __forceinline__ int narrow_of(int n) const { return W == 4 ? from_n[0] : from_n[n & 1]; }
+    __device__ __forceinline__ int wide_of(int n) const { return W == 4 || !Geo<D>::SWZ ? from_w : from_w ^ ((n & 3) * 16); }
     template <int SIZE, bool WD>
     __device__ __forceinline__ void fill(uint32_t dst, int at, const i32x4& r) const {
         constexpr int FULL = SIZE / (1024 * W), REST = (SIZE - FULL * 1024 * W) / (16 * W);
@@ -169,7 +201,7 @@ struct DiffRing {
 #pragma unroll
         for (int n = 0; n < FULL; ++n) {
             const int kb = n * W + w;
-            dma16(__builtin_amdgcn_readfirstlane(dst + kb * 1024), (WD ? wide_of(kb) : narrow_of(kb)) + at + kb * 1024, r);
+            dma16(__builtin_amdgcn_readfirstlane(dst + kb * 1024), (WD ? wide_of(n) : narrow_of(n)) + at + kb * 1024, r);
         }
         if (REST) {
             const int b = FULL * W * 1024 + w * REST * 16;
@@ -181,7 +213,17 @@ struct DiffRing {
         fill<NT, false>(dst, row0 * NB, rs[0]);
         fill<NT, false>(dst + NT, row0 * NB, rs[1]);
         fill<WT, true>(dst + WIDE, row0 * WB, rs[2]);
-        if (VALS && w == 0 && lane < BS) dma16(__builtin_amdgcn_readfirstlane(dst + VAL), from_v + row0 * 4, vs);
+        if (VALS && w == 0 && lane < BS) {
+            int l = lane;
+            fresh(l);
+            dma16(__builtin_amdgcn_readfirstlane(dst + VAL), (l / (BS / 4)) * T64 * 4 + (l % (BS / 4)) * 16 + row0 * 4, vs);
+        }
+    }
+    // 32 rows from row0 on of the wave's own wide ones
+    __device__ __forceinline__ void load_own(int to, int row0, const i32x4& r) const {
+#pragma unroll
+        for (int kb = 0; kb < 32 * WB / 1024; ++kb)
+            dma16(__builtin_amdgcn_readfirstlane(lds0 + to + kb * 1024), wide_from(kb) + row0 * WB + kb * 1024, r);
     }
     // the stage asked for has landed, and every wave is through the one before it
     __device__ __forceinline__ void turn() const {
@@ -570,10 +612,19 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     ring.load(0, s0 * BS);
     Rd rd;
     rd.init(lds);
-    bf16x8 n_op[2][4], n_tail[2], w_op[Rd::WS];
+    rd.pack();
+    bf16x8 n_op[2][4], n_tail[2], w_op[KV ? 1 : Rd::WS];
 #pragma unroll
     for (int i = 0; i < 2; ++i) rd.own_rows(own + (size_t)i * T * D, NB, row0, own_end, n_op[i], TAIL ? &n_tail[i] : nullptr);
-    rd.own_rows((KV ? a.v : a.d_o) + w_own, WB, row0, own_end, w_op, nullptr);
+    const int own_v = R::LDS + 32 * wave * WB, own_t = R::LDS + 32 * W * WB + wave * 1024;
+    if constexpr (KV) {
+        ring.load_own(own_v, row0, buffer_rsrc(a.v + w_own, own_end * WB));
+        if (TAIL && !rd.hi) {
+            *(lds_bf16x8*)(lds + own_t + rd.l32 * 16) = n_tail[0];
+            *(lds_bf16x8*)(lds + own_t + 512 + rd.l32 * 16) = n_tail[1];
+        }
+    } else
+        rd.own_rows(a.d_o + w_own, WB, row0, own_end, w_op, nullptr);
     float log[2] = {INFINITY, INFINITY}, minus = 0.f, more = 0.f;  // of the own query
     if (!KV && row0 + rd.l32 < T) {
         log[0] = vals[row0 + rd.l32];
@@ -601,6 +652,7 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
 #pragma unroll
             for (int h = 0; h < BS / 32; ++h) {
                 const int cw = st + R::WIDE + 32 * h * WB, first = s * BS + 32 * h;
+                if (KV) rd.unpack();
                 // four values of a chunk's rows 8 j + 4 hi ..
                 auto value = [&](int n, int j) {
                     return __builtin_bit_cast(f32x4, *(const lds_u32x4*)(lds + st + R::VAL + n * BS * 4 + (32 * h + 8 * j + 4 * rd.hi) * 4));
@@ -617,7 +669,7 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
                     dp = f32x16{} + minus;
                 }
 #pragma unroll
-                for (int k = 0; k < Rd::WS; ++k) dp = mma(rd.w_row(cw, k), w_op[k], dp);
+                for (int k = 0; k < Rd::WS; ++k) dp = mma(rd.w_row(cw, k), KV ? rd.w_row(own_v, k) : w_op[KV ? 0 : k], dp);
                 f32x16 p1;  // map 1's probabilities (KV)
                 uint32_t pk[8], ds[8];
 #pragma unroll
@@ -626,7 +678,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
                     f32x16 sc = {};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) sc = mma(rd.n_row(cx, k), n_op[i][k], sc);
-                    if (TAIL) sc = mma(rd.n_row_tail(cx, R::ZERO), n_tail[i], sc);
+                    if (TAIL)
+                        sc = mma(rd.n_row_tail(cx, R::ZERO), KV ? *(const lds_bf16x8*)(lds + (rd.hi ? R::ZERO : own_t + 512 * i + rd.l32 * 16)) : n_tail[i], sc);
                     if (!KV && first + 32 > keys) {
                         const int lim = keys - first - 4 * rd.hi;
 #pragma unroll
@@ -724,8 +777,9 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_bwd(DiffArgs a, int n_lam, int n_k,
                                                                                           int per_k, int n_q, int per_q) {
-    constexpr int W = kDiffRows / 32, BS = 64;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[DiffRing<D, W, BS, true>::LDS];
+    constexpr int W = kDiffRows / 32;
+    constexpr int LDS_K = DiffRing<D, W, 32, true>::LDS + kDiffRows * (4 * D + (D == 72 ? 32 : 0)), LDS_Q = DiffRing<D, W, 64, false>::LDS;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS_K > LDS_Q ? LDS_K : LDS_Q];
     lds_u8* const lds = (lds_u8*)smem;
     int g = blockIdx.x;
     const int lam8 = (n_lam + 7) & ~7;  // (whole eights, so that a tile's XCD goes by its number)
@@ -745,9 +799,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         item /= split;
     }
     if (kv)
-        diff_walk<D, true, W, BS, SPLIT>(a, lds, item, part);
+        diff_walk<D, true, W, 32, SPLIT>(a, lds, item, part);
     else
-        diff_walk<D, false, W, BS, SPLIT>(a, lds, item, part);
+        diff_walk<D, false, W, 64, SPLIT>(a, lds, item, part);
 }
 
 // Sums of a tile's parts: dK_1, dK_2, the halves of dV (blockIdx.y 0 .. 3; `tiles_k` of them in x), then dQ_1, dQ_2
