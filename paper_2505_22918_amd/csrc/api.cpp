@@ -1184,15 +1184,21 @@ DiffBytes diff_bytes(const rt_diff_dims& d, int32_t n_lam) {
             (int64_t)d.B * 4};
 }
 
-// Forward: waves of a workgroup, and workgroups that share a tile's keys where there are few tiles.
-int32_t diff_waves(const rt_diff_dims& d) { return d.Tq <= 32 ? 1 : 4; }
-int32_t diff_split(const rt_diff_dims& d) {
-    const int64_t w = diff_waves(d), n = (int64_t)d.B * d.H * ceil_div(d.Tq, 32 * w), stages = ceil_div(d.Tk, w == 1 ? 32 : 64);
-    const int64_t s = std::min((w == 1 ? 1024 : 512) / std::max<int64_t>(n, 1), stages / 4);
-    return s > 1 ? (int32_t)s : 1;
+// Forward: whether a workgroup's waves share the keys of 32 queries, and workgroups that share a tile's keys.
+struct DiffPlan {
+    int32_t by_keys, split;
+};
+DiffPlan diff_plan(const rt_diff_dims& d) {
+    const int64_t bh = (int64_t)d.B * d.H, n = bh * ceil_div(d.Tq, rt::kDiffRows), n32 = bh * ceil_div(d.Tq, 32);
+    if (n32 <= 512) {
+        const int64_t s = std::min(256 / std::max<int64_t>(n32, 1), ceil_div(d.Tk, 32) / 16);
+        return {1, s > 1 ? (int32_t)s : 1};
+    }
+    const int64_t s = std::min(512 / std::max<int64_t>(n, 1), ceil_div(d.Tk, 64) / 4);
+    return {0, s > 1 ? (int32_t)s : 1};
 }
 int64_t diff_workspace(const rt_diff_dims& d) {
-    const int64_t s = diff_split(d);
+    const int64_t s = diff_plan(d).split;
     return std::max<int64_t>(16, s > 1 ? (int64_t)d.B * d.H * s * 2 * d.Tq * (2 * d.D + 3) * 4 : 0);
 }
 
@@ -1272,7 +1278,8 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
         RT_TRY(check_stat(row_sum, "row_sum"));
     }
     const int64_t need = diff_workspace(dims);
-    a.split = diff_split(dims);
+    const DiffPlan plan = diff_plan(dims);
+    a.split = plan.split;
     const void* ws = a.split > 1 ? workspace : nullptr;
     if (a.split > 1) {
         RT_TRY(check_tensor(workspace, "workspace"));
@@ -1287,7 +1294,7 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
     a.o2 = static_cast<uint16_t*>(o2);
     a.row_max = row_max;
     a.row_sum = row_sum;
-    a.waves = diff_waves(dims);
+    a.by_keys = plan.by_keys;
     a.part = static_cast<float*>(workspace);
     return hip_status(rt::launch_diff(a, dims.D, static_cast<hipStream_t>(stream)), "differential attention launch");
 }

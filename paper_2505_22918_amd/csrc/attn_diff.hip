@@ -171,7 +171,7 @@ struct DiffRing {
     __device__ __forceinline__ void init(lds_u8* lds, const uint16_t* x1, const uint16_t* x2, const uint16_t* y, int rows) {
         lds0 = (uint32_t)(uintptr_t)lds;
         lane = threadIdx.x & 63;
-        w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        w = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         rs[0] = buffer_rsrc(x1, rows * NB);
         rs[1] = buffer_rsrc(x2, rows * NB);
         rs[2] = buffer_rsrc(y, rows * WB);
@@ -179,7 +179,7 @@ struct DiffRing {
         from_n[0] = narrow_from(W == 4 ? w : 0);
         from_n[1] = W == 4 ? from_n[0] : narrow_from(1);
         from_w = wide_from(W == 4 ? w : 0);
-        if (threadIdx.x < 4) *(lds_u32x4*)(lds + ZERO + 16 * threadIdx.x) = u32x4{};
+        if (w == 0 && lane < 4) *(lds_u32x4*)(lds + ZERO + 16 * lane) = u32x4{};
     }
     __device__ __forceinline__ void init_values(const float* vals, int T64_) {
         T64 = T64_;
@@ -234,6 +234,15 @@ struct DiffRing {
     }
 };
 
+typedef __attribute__((address_space(3))) float lds_f32;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+
+// The n-th head to be taken: heads of the samples in turn, so that samples of few and of many keys share the XCDs, each of
+// which takes heads that follow one another.
+__device__ __forceinline__ int head_of(const DiffArgs& a, int n) {
+    const int B = a.n_bh / a.H, h = n / B;
+    return (n - h * B) * a.H + h;
+}
 __device__ __forceinline__ int keys_of(const DiffArgs& a, int b) {
     if (!a.k_lens) return a.Tk;
     const int n = a.k_lens[b];
@@ -244,17 +253,21 @@ __device__ __forceinline__ int keys_of(const DiffArgs& a, int b) {
 
 constexpr float kMove = 24.0f;  // the running max moves when a probability against it passes 2^kMove
 
-// Workgroups of W waves, 32 queries each.  SPLIT: a part of the keys, whose sums against their own running max go to
-// a.part ([tile's head][part][map][query][2 D], then [..][3] of the max in score units, the sum and the true max).
-template <int D, int W, bool STATS, bool SPLIT>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W == 1 ? 1 : 2, W == 1 ? 1 : 2))) void
+// A workgroup of four waves takes 32 queries to a wave, which share a ring of keys and values; or (KEYS, where there are
+// few tiles) 32 queries in all, the waves every fourth 32 keys each from rings of their own, and joins their sums in LDS.
+// SPLIT: a part of the keys, whose sums against their own running max go to a.part ([tile's head][part][map][query][2 D],
+// then [..][3] of the max in score units, the sum and the true max).
+template <int D, bool KEYS, bool STATS, bool SPLIT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(KEYS ? 1 : 2, KEYS ? 1 : 2))) void
 diff_fwd(DiffArgs a, int n_items, int per_xcd) {
-    constexpr int BS = W == 1 ? 32 : 64;
-    using R = DiffRing<D, W, BS, false>;
+    constexpr int BS = KEYS ? 32 : 64, STEP = KEYS ? 4 : 1;  // keys of a stage; stages from one of a wave to its next
+    using R = DiffRing<D, KEYS ? 1 : 4, BS, false>;
     constexpr int NB = R::NB, WB = R::WB;
     constexpr bool TAIL = D == 72;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[R::LDS];
-    lds_u8* const lds = (lds_u8*)smem;
+    constexpr int STAT = 4 * R::LDS;  // KEYS: [wave][map][query] of the running max, the sum and the true max
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[KEYS ? STAT + 4 * 2 * 32 * 12 : R::LDS];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lds_u8* const lds = (lds_u8*)smem + (KEYS ? wave * R::LDS : 0);
 
     int item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), part = 0;
     if (item >= n_items) return;
@@ -262,16 +275,20 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
         part = item % a.split;
         item /= a.split;
     }
-    const int n_tile = (a.Tq + 32 * W - 1) / (32 * W), bh = item / n_tile, b = bh / a.H;
-    const int row0 = ((item - bh * n_tile) * W + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 32;
+    constexpr int ROWS = KEYS ? 32 : kDiffRows;
+    const int n_tile = (a.Tq + ROWS - 1) / ROWS, head = item / n_tile;
+    const int bh = head_of(a, head), b = bh / a.H;
+    const int row0 = (item - head * n_tile) * ROWS + (KEYS ? 0 : wave * 32);
     const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
-    const int s0 = SPLIT ? (int)((int64_t)n_st * part / a.split) : 0, s1 = SPLIT ? (int)((int64_t)n_st * (part + 1) / a.split) : n_st;
+    const int s0 = (SPLIT ? (int)((int64_t)n_st * part / a.split) : 0) + (KEYS ? wave : 0);
+    const int s1 = SPLIT ? (int)((int64_t)n_st * (part + 1) / a.split) : n_st;
 
     R ring;
     ring.init(lds, a.k + (size_t)(2 * bh) * a.Tk * D, a.k + (size_t)(2 * bh + 1) * a.Tk * D, a.v + (size_t)bh * a.Tk * (2 * D), keys);
     ring.load(0, s0 * BS);
     Reads<D> rd;
     rd.init(lds);
+    rd.pack();
     bf16x8 q[2][4], q_tail[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -295,13 +312,14 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     };
     const float c2 = a.scale_log2;
     int st = 0;
-    for (int s = s0; s < s1; ++s) {
+    for (int s = s0; s < s1; s += STEP) {
         ring.turn();
-        ring.load(R::STAGE - st, (s + 1) * BS);
+        ring.load(R::STAGE - st, (s + STEP) * BS);
         if (row0 < a.Tq) {
-#pragma unroll
+#pragma nounroll
             for (int h = 0; h < BS / 32; ++h) {
                 const int first = s * BS + 32 * h, cv = st + R::WIDE + 32 * h * WB;
+                if (!KEYS) rd.unpack();
                 uint32_t pk[2][8];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -374,6 +392,68 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
         l_run[i] = pair_sum(l_run[i]);
         if (STATS) m_top[i] = pair_max(m_top[i]);
     }
+    constexpr int TILES = KEYS ? 1 : 4;  // of 32 elements that a wave writes, from `col0` on
+    const int col0 = KEYS ? 32 * wave : 0;
+    const bool first = !KEYS || wave == 0;
+    if constexpr (KEYS) {
+        lds_u8* const all = (lds_u8*)smem;
+        auto stat = [&](int w, int i) { return (lds_f32*)(all + STAT) + ((w * 2 + i) * 32 + rd.l32) * 3; };
+        if (rd.hi == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                stat(wave, i)[0] = m_run[i];
+                stat(wave, i)[1] = l_run[i];
+                stat(wave, i)[2] = m_top[i];
+            }
+        }
+        __syncthreads();
+        // each wave's sums against the largest running max, in its own ring's place: [map][element tile][u][lane]
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float m = -INFINITY, l = 0.f, top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                m = fmaxf(m, stat(w, i)[0]);
+                top = fmaxf(top, stat(w, i)[2]);
+            }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) l = __builtin_fmaf(__builtin_amdgcn_exp2f((stat(w, i)[0] - m) * c2), stat(w, i)[1], l);
+            const float f = __builtin_amdgcn_exp2f((m_run[i] - m) * c2);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    *(lds_f32x4*)(lds + ((i * 4 + d) * 4 + u) * 1024 + rd.lane * 16) =
+                        f32x4{acc[i][d][4 * u] * f, acc[i][d][4 * u + 1] * f, acc[i][d][4 * u + 2] * f, acc[i][d][4 * u + 3] * f};
+            if (TAIL) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) *(lds_f32x4*)(lds + 32768 + (i * 2 + h) * 1024 + rd.lane * 16) = tacc[i][h] * tail_bcast(f, h);
+            }
+            m_run[i] = m;
+            l_run[i] = l;
+            m_top[i] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                f32x4 x = {};
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x += *(const lds_f32x4*)(all + w * R::LDS + ((i * 4 + wave) * 4 + u) * 1024 + rd.lane * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][0][4 * u + e] = x[e];
+            }
+            if (TAIL && wave == 0) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    tacc[i][h] = f32x4{};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) tacc[i][h] += *(const lds_f32x4*)(all + w * R::LDS + 32768 + (i * 2 + h) * 1024 + rd.lane * 16);
+                }
+            }
+        }
+    }
     if (SPLIT) {
         const size_t n_part = (size_t)a.n_bh * a.split, at = (size_t)bh * a.split + part;
 #pragma unroll
@@ -381,19 +461,19 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
             float* o = a.part + (at * 2 + i) * a.Tq * (2 * D);
             if (row < a.Tq) {
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
+                for (int d = 0; d < TILES; ++d)
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        *reinterpret_cast<f32x4*>(o + (size_t)row * (2 * D) + 32 * d + 16 * rd.hi + 4 * u) =
+                        *reinterpret_cast<f32x4*>(o + (size_t)row * (2 * D) + col0 + 32 * d + 16 * rd.hi + 4 * u) =
                             f32x4{acc[i][d][4 * u], acc[i][d][4 * u + 1], acc[i][d][4 * u + 2], acc[i][d][4 * u + 3]};
-                if (rd.hi == 0) {
+                if (first && rd.hi == 0) {
                     float* x = a.part + n_part * 2 * a.Tq * (2 * D) + ((at * 2 + i) * a.Tq + row) * 3;
                     x[0] = m_run[i];
                     x[1] = l_run[i];
                     x[2] = STATS ? m_top[i] : 0.f;
                 }
             }
-            if (TAIL) {
+            if (TAIL && first) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int r = row0 + 16 * h + (rd.lane & 15);
@@ -407,7 +487,7 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         inv[i] = l_run[i] == 0.f ? 0.f : 1.0f / l_run[i];  // no keys: 0
-        if (STATS && rd.hi == 0 && row < a.Tq) {
+        if (STATS && first && rd.hi == 0 && row < a.Tq) {
             const size_t at = (size_t)(2 * bh + i) * a.Tq + row;
             a.row_max[at] = m_top[i] * a.scale_nat;
             a.row_sum[at] = l_run[i] == 0.f ? 0.f : l_run[i] * __builtin_amdgcn_exp2f((m_run[i] - m_top[i]) * c2);
@@ -418,7 +498,7 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     uint16_t* const o2 = STATS ? a.o2 + (size_t)bh * a.Tq * (2 * D) : nullptr;
     if (row < a.Tq) {
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < TILES; ++d)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 uint32_t x[4], y[4];
@@ -429,12 +509,12 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
                     x[e] = pack_bf16(__builtin_fmaf(-lam, b0, acc[0][d][j] * inv[0]), __builtin_fmaf(-lam, b1, acc[0][d][j + 1] * inv[0]));
                     y[e] = pack_bf16(b0, b1);
                 }
-                const size_t at = (size_t)row * (2 * D) + 32 * d + 16 * rd.hi + 8 * u;
+                const size_t at = (size_t)row * (2 * D) + col0 + 32 * d + 16 * rd.hi + 8 * u;
                 *reinterpret_cast<u32x4*>(o + at) = u32x4{x[0], x[1], x[2], x[3]};
                 if (STATS) *reinterpret_cast<u32x4*>(o2 + at) = u32x4{y[0], y[1], y[2], y[3]};
             }
     }
-    if (TAIL) {
+    if (TAIL && first) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float i0 = tail_bcast(inv[0], h), i1 = tail_bcast(inv[1], h);
@@ -466,6 +546,7 @@ __global__ __launch_bounds__(256) void diff_join(DiffArgs a, int64_t rows) {
     for (int map = 0; map < 2; ++map) {
         auto at = [&](int p) { return ((bh * a.split + p) * 2 + map) * (size_t)a.Tq + row; };
         float m = -INFINITY, top = -INFINITY, l = 0.f;
+#pragma unroll 4
         for (int p = 0; p < a.split; ++p) {
             m = fmaxf(m, stats[at(p) * 3]);
             top = fmaxf(top, stats[at(p) * 3 + 2]);
@@ -494,10 +575,11 @@ __global__ __launch_bounds__(256) void diff_join(DiffArgs a, int64_t rows) {
     }
 }
 
-template <int D, int W, bool STATS, bool SPLIT>
+template <int D, bool KEYS, bool STATS, bool SPLIT>
 hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream) {
-    const int n = a.n_bh * ((a.Tq + 32 * W - 1) / (32 * W)) * (SPLIT ? a.split : 1), per = (n + 7) / 8;
-    hipLaunchKernelGGL((diff_fwd<D, W, STATS, SPLIT>), dim3(8 * per), dim3(64 * W), 0, stream, a, n, per);
+    constexpr int ROWS = KEYS ? 32 : kDiffRows;
+    const int n = a.n_bh * ((a.Tq + ROWS - 1) / ROWS) * (SPLIT ? a.split : 1), per = (n + 7) / 8;
+    hipLaunchKernelGGL((diff_fwd<D, KEYS, STATS, SPLIT>), dim3(8 * per), dim3(256), 0, stream, a, n, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !SPLIT) return e;
     constexpr int EACH = 256 / (D / 2);
@@ -505,14 +587,14 @@ hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((diff_join<D>), dim3((uint32_t)((rows + EACH - 1) / EACH)), dim3(256), 0, stream, a, rows);
     return hipGetLastError();
 }
-template <int D, int W>
-hipError_t launch_fwd_w(const DiffArgs& a, hipStream_t stream) {
-    if (a.split > 1) return a.o2 ? launch_fwd<D, W, true, true>(a, stream) : launch_fwd<D, W, false, true>(a, stream);
-    return a.o2 ? launch_fwd<D, W, true, false>(a, stream) : launch_fwd<D, W, false, false>(a, stream);
+template <int D, bool KEYS>
+hipError_t launch_fwd_k(const DiffArgs& a, hipStream_t stream) {
+    if (a.split > 1) return a.o2 ? launch_fwd<D, KEYS, true, true>(a, stream) : launch_fwd<D, KEYS, false, true>(a, stream);
+    return a.o2 ? launch_fwd<D, KEYS, true, false>(a, stream) : launch_fwd<D, KEYS, false, false>(a, stream);
 }
 template <int D>
 hipError_t launch_fwd_d(const DiffArgs& a, hipStream_t stream) {
-    return a.waves == 1 ? launch_fwd_w<D, 1>(a, stream) : launch_fwd_w<D, 4>(a, stream);
+    return a.by_keys ? launch_fwd_k<D, true>(a, stream) : launch_fwd_k<D, false>(a, stream);
 }
 
 // ---- backward ------------------------------------------------------------------------------
@@ -591,8 +673,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     constexpr int NB = R::NB, WB = R::WB, NW = KV ? 4 : 1;
     constexpr bool TAIL = D == 72;
     const int T = KV ? a.Tk : a.Tq, Tx = KV ? a.Tq : a.Tk;  // rows of the own side and of the other
-    const int n_tile = (T + 32 * W - 1) / (32 * W), bh = item / n_tile, b = bh / a.H;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = ((item - bh * n_tile) * W + wave) * 32;
+    const int n_tile = (T + 32 * W - 1) / (32 * W), head = item / n_tile, bh = head_of(a, head), b = bh / a.H;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = ((item - head * n_tile) * W + wave) * 32;
     const int keys = keys_of(a, b);
     const int own_end = KV ? keys : T, x_end = KV ? Tx : keys;
     const int tile0 = row0 - 32 * wave;
@@ -811,7 +893,7 @@ __global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int tiles_k, int til
     const bool kv = blockIdx.y < 4;
     if ((int)blockIdx.x >= (kv ? tiles_k : tiles_q)) return;
     const int T = kv ? a.Tk : a.Tq, n_tile = (T + kDiffRows - 1) / kDiffRows, n = kv ? a.split_k : a.split_q;
-    const int bh = blockIdx.x / n_tile, row0 = (blockIdx.x - bh * n_tile) * kDiffRows;
+    const int head = blockIdx.x / n_tile, bh = head_of(a, head), row0 = (blockIdx.x - head * n_tile) * kDiffRows;
     const int width = kv && blockIdx.y >= 2 ? 2 * D : D, which = kv ? blockIdx.y : blockIdx.y - 4;
     const size_t stride = (kv ? 4 : 2) * (size_t)TILE;
     const float* part = (kv ? a.part_k : a.part_q) + (size_t)blockIdx.x * n * stride + (size_t)which * TILE;

@@ -47,7 +47,7 @@ struct DiffArgs {
     uint16_t* o2;   // or null, with the statistics
     float* row_max;  // fp32 [B, 2 H, Tq]
     float* row_sum;
-    int32_t waves;  // of a workgroup: 1 or 4
+    int32_t by_keys;  // a workgroup's waves share the keys of 32 queries; else they take 32 queries each
     int32_t split;  // workgroups that share a tile's keys
     float* part;    // workspace of split walks
     // backward

@@ -149,7 +149,7 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t) {
 }
 hipError_t launch_diff(const DiffArgs& a, int D, hipStream_t) {
     EXPECT((D == 64 || D == 72) && a.q && a.lam && a.o && a.Tq > 0 && a.n_bh > 0 && a.n_bh % a.H == 0);
-    EXPECT(a.split >= 1 && (a.split == 1 || a.part) && (a.waves == 1 || a.waves == 4) && (a.waves == 4 || a.Tq <= 32));
+    EXPECT(a.split >= 1 && (a.split == 1 || a.part));
     EXPECT((a.o2 && a.row_max && a.row_sum) || (!a.o2 && !a.row_max && !a.row_sum));
     return hipSuccess;
 }
