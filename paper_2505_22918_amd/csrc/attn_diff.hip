@@ -258,7 +258,7 @@ constexpr float kMove = 24.0f;  // the running max moves when a probability agai
 // SPLIT: a part of the keys, whose sums against their own running max go to a.part ([tile's head][part][map][query][2 D],
 // then [..][3] of the max in score units, the sum and the true max).
 template <int D, bool KEYS, bool STATS, bool SPLIT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(KEYS ? 1 : 2, KEYS ? 1 : 2))) void
+__global__ __launch_bounds__(KEYS ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) void
 diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     constexpr int BS = KEYS ? 32 : 64, STEP = KEYS ? 4 : 1;  // keys of a stage; stages from one of a wave to its next
     using R = DiffRing<D, KEYS ? 1 : 4, BS, false>;
@@ -280,12 +280,12 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     const int bh = head_of(a, head), b = bh / a.H;
     const int row0 = (item - head * n_tile) * ROWS + (KEYS ? 0 : wave * 32);
     const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
-    const int s0 = (SPLIT ? (int)((int64_t)n_st * part / a.split) : 0) + (KEYS ? wave : 0);
-    const int s1 = SPLIT ? (int)((int64_t)n_st * (part + 1) / a.split) : n_st;
+    const int first_stage = (SPLIT ? (int)((int64_t)n_st * part / a.split) : 0) + (KEYS ? wave : 0);
+    const int end_stage = SPLIT ? (int)((int64_t)n_st * (part + 1) / a.split) : n_st;
 
     R ring;
     ring.init(lds, a.k + (size_t)(2 * bh) * a.Tk * D, a.k + (size_t)(2 * bh + 1) * a.Tk * D, a.v + (size_t)bh * a.Tk * (2 * D), keys);
-    ring.load(0, s0 * BS);
+    ring.load(0, first_stage * BS);
     Reads<D> rd;
     rd.init(lds);
     rd.pack();
@@ -312,32 +312,47 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     };
     const float c2 = a.scale_log2;
     int st = 0;
-    for (int s = s0; s < s1; s += STEP) {
+    for (int s = first_stage; s < end_stage; s += STEP) {
         ring.turn();
         ring.load(R::STAGE - st, (s + STEP) * BS);
         if (row0 < a.Tq) {
 #pragma nounroll
             for (int h = 0; h < BS / 32; ++h) {
                 const int first = s * BS + 32 * h, cv = st + R::WIDE + 32 * h * WB;
-                if (!KEYS) rd.unpack();
-                uint32_t pk[2][8];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int cx = st + i * R::NT + 32 * h * NB;
-                    f32x16 sc = {};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) sc = mma(rd.n_row(cx, k), q[i][k], sc);
-                    if (TAIL) sc = mma(rd.n_row_tail(cx, R::ZERO), q_tail[i], sc);
+                rd.unpack();
+                const int cx = st + 32 * h * NB;
+                auto mask = [&](f32x16& sc) {
                     if (first + 32 > keys) {
                         const int lim = keys - first - 4 * rd.hi;
 #pragma unroll
                         for (int x = 0; x < 16; ++x)
                             if (8 * (x >> 2) + (x & 3) >= lim) sc[x] = -INFINITY;
                     }
-                    float top = fmaxf(fmaxf(sc[0], sc[1]), sc[2]);
+                };
+                uint32_t pk[2][8];
+                // Probabilities of a map against its running max, a matrix product of the other's between two pairs of
+                // them; should one pass 2^kMove, the max moves and they are formed again.
+                auto soft = [&](int i, const f32x16& sc, auto&& product) {
+                    float top = -INFINITY;
+                    auto form = [&](auto&& between) {
+                        const float mc = m_run[i] * c2;
+                        float sum[2] = {0.f, 0.f};
 #pragma unroll
-                    for (int x = 3; x < 15; x += 2) top = fmaxf(fmaxf(top, sc[x]), sc[x + 1]);
-                    top = fmaxf(top, sc[15]);
+                        for (int x = 0; x < 16; x += 2) {
+                            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -mc));
+                            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -mc));
+                            sum[(x >> 1) & 1] += e0 + e1;
+                            pk[i][x / 2] = pack_bf16(e0, e1);
+                            between(x);
+                        }
+                        return sum[0] + sum[1];
+                    };
+                    float sum = form([&](int x) {
+                        top = fmaxf(fmaxf(top, sc[x]), sc[x + 1]);
+                        __builtin_amdgcn_sched_barrier(0);
+                        product(x / 2);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
                     if (STATS) m_top[i] = fmaxf(m_top[i], top);
                     if (__builtin_amdgcn_ballot_w64((top - m_run[i]) * c2 > kMove)) {
                         const float to = fmaxf(m_run[i], pair_max(top));
@@ -350,26 +365,33 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
                             tacc[i][0] *= tail_bcast(alpha, 0);
                             tacc[i][1] *= tail_bcast(alpha, 1);
                         }
+                        sum = form([](int) {});
                     }
-                    const float mc = m_run[i] * c2;
-                    float sum[2] = {0.f, 0.f};
+                    l_run[i] += sum;
+                };
+                f32x16 s0 = {}, s1 = {};
+                bf16x8 k1[4], v[8];
 #pragma unroll
-                    for (int x = 0; x < 16; x += 2) {
-                        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -mc));
-                        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -mc));
-                        sum[(x >> 1) & 1] += e0 + e1;
-                        pk[i][x / 2] = pack_bf16(e0, e1);
-                    }
-                    l_run[i] += sum[0] + sum[1];
-                }
+                for (int k = 0; k < 4; ++k) s0 = mma(rd.n_row(cx, k), q[0][k], s0);
 #pragma unroll
-                for (int ks = 0; ks < 2; ++ks)
+                for (int k = 0; k < 4; ++k) k1[k] = rd.n_row(cx + R::NT, k);
+                if (TAIL) s0 = mma(rd.n_row_tail(cx, R::ZERO), q_tail[0], s0);
+                mask(s0);
+                soft(0, s0, [&](int p) {
+                    if (p % 2 == 0) s1 = mma(k1[p / 2], q[1][p / 2], s1);
+                });
+                if (TAIL) s1 = mma(rd.n_row_tail(cx + R::NT, R::ZERO), q_tail[1], s1);
+                mask(s1);
+                auto v_at = [&](int p) { return rd.w_col(cv, p & 3, p >> 2); };
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        const bf16x8 v = rd.w_col(cv, d, ks);
-                        acc[0][d] = mma(v, op(pk[0], ks), acc[0][d]);
-                        acc[1][d] = mma(v, op(pk[1], ks), acc[1][d]);
-                    }
+                for (int p = 0; p < 8; ++p)
+                    if (!TAIL || p < 2) v[p] = v_at(p);
+                soft(1, s1, [&](int p) {
+                    acc[0][p & 3] = mma(TAIL ? v[p & 1] : v[p], op(pk[0], p >> 2), acc[0][p & 3]);
+                    if (TAIL && p < 6) v[p & 1] = v_at(p + 2);
+                });
+#pragma unroll
+                for (int p = 0; p < 8; ++p) acc[1][p & 3] = mma(TAIL ? v_at(p) : v[p], op(pk[1], p >> 2), acc[1][p & 3]);
                 if (TAIL) {
                     const bf16x8 v = rd.w_col_tail(cv);
 #pragma unroll
@@ -394,7 +416,7 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     }
     constexpr int TILES = KEYS ? 1 : 4;  // of 32 elements that a wave writes, from `col0` on
     const int col0 = KEYS ? 32 * wave : 0;
-    const bool first = !KEYS || wave == 0;
+    const bool lead = !KEYS || wave == 0;
     if constexpr (KEYS) {
         lds_u8* const all = (lds_u8*)smem;
         auto stat = [&](int w, int i) { return (lds_f32*)(all + STAT) + ((w * 2 + i) * 32 + rd.l32) * 3; };
@@ -466,14 +488,14 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
                     for (int u = 0; u < 4; ++u)
                         *reinterpret_cast<f32x4*>(o + (size_t)row * (2 * D) + col0 + 32 * d + 16 * rd.hi + 4 * u) =
                             f32x4{acc[i][d][4 * u], acc[i][d][4 * u + 1], acc[i][d][4 * u + 2], acc[i][d][4 * u + 3]};
-                if (first && rd.hi == 0) {
+                if (lead && rd.hi == 0) {
                     float* x = a.part + n_part * 2 * a.Tq * (2 * D) + ((at * 2 + i) * a.Tq + row) * 3;
                     x[0] = m_run[i];
                     x[1] = l_run[i];
                     x[2] = STATS ? m_top[i] : 0.f;
                 }
             }
-            if (TAIL && first) {
+            if (TAIL && lead) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int r = row0 + 16 * h + (rd.lane & 15);
@@ -487,7 +509,7 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         inv[i] = l_run[i] == 0.f ? 0.f : 1.0f / l_run[i];  // no keys: 0
-        if (STATS && first && rd.hi == 0 && row < a.Tq) {
+        if (STATS && lead && rd.hi == 0 && row < a.Tq) {
             const size_t at = (size_t)(2 * bh + i) * a.Tq + row;
             a.row_max[at] = m_top[i] * a.scale_nat;
             a.row_sum[at] = l_run[i] == 0.f ? 0.f : l_run[i] * __builtin_amdgcn_exp2f((m_run[i] - m_top[i]) * c2);
@@ -514,7 +536,7 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
                 if (STATS) *reinterpret_cast<u32x4*>(o2 + at) = u32x4{y[0], y[1], y[2], y[3]};
             }
     }
-    if (TAIL && first) {
+    if (TAIL && lead) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float i0 = tail_bcast(inv[0], h), i1 = tail_bcast(inv[1], h);
