@@ -1189,27 +1189,71 @@ struct DiffPlan {
     int32_t by_keys, split;
 };
 DiffPlan diff_plan(const rt_diff_dims& d) {
-    const int64_t bh = (int64_t)d.B * d.H, n = bh * ceil_div(d.Tq, rt::kDiffRows), n32 = bh * ceil_div(d.Tq, 32);
-    if (n32 <= 512) {
-        const int64_t s = std::min(256 / std::max<int64_t>(n32, 1), ceil_div(d.Tk, 32) / 16);
-        return {1, s > 1 ? (int32_t)s : 1};
+    const int64_t bh = (int64_t)d.B * d.H, chunks = ceil_div(d.Tk, 32);
+    DiffPlan p{0, 1};
+    int64_t best = INT64_MAX;
+    for (int by_keys = 0; by_keys < 2; ++by_keys) {
+        const int64_t n = bh * ceil_div(d.Tq, by_keys ? 32 : rt::kDiffRows), slots = by_keys ? 256 : 512;
+        for (int64_t s = 1; s <= 32; ++s) {
+            if (s > 1 && (n * s > 2 * slots || chunks < (by_keys ? 8 : 4) * s)) break;
+            // tenths of microseconds: of a chunk in a wave alone on its SIMD, or one of two; of a workgroup's start and end
+            const int64_t each = by_keys ? ceil_div(chunks, 4 * s) * 12 + 50 : ceil_div(chunks, s) * (n * s <= 256 ? 11 : 15) + 40;
+            int64_t t = ceil_div(n * s, slots) * each;
+            if (s > 1) t += 50 + bh * s * d.Tq * d.D * 32 / 400000;  // the parts, written and read
+            if (t < best) {
+                best = t;
+                p = DiffPlan{by_keys, (int32_t)s};
+            }
+        }
     }
-    const int64_t s = std::min(512 / std::max<int64_t>(n, 1), ceil_div(d.Tk, 64) / 4);
-    return {0, s > 1 ? (int32_t)s : 1};
+    return p;
 }
 int64_t diff_workspace(const rt_diff_dims& d) {
     const int64_t s = diff_plan(d).split;
     return std::max<int64_t>(16, s > 1 ? (int64_t)d.B * d.H * s * 2 * d.Tq * (2 * d.D + 3) * 4 : 0);
 }
 
-// Backward: the same for tiles of keys and of queries.
-void diff_back_split(const rt_diff_dims& d, int32_t* k, int32_t* q) {
-    const int64_t bh = (int64_t)d.B * d.H, sk = ceil_div(d.Tq, 64), sq = ceil_div(d.Tk, 64);  // stages of their walks
-    const int64_t n = bh * (ceil_div(d.Tk, rt::kDiffRows) + ceil_div(d.Tq, rt::kDiffRows));
-    const int64_t s = 512 / std::max<int64_t>(n, 1);
-    *k = (int32_t)std::max<int64_t>(1, std::min(s, sk / 4));
-    *q = (int32_t)std::max<int64_t>(1, std::min(s, sq / 4));
-    if (std::max(sk - ceil_div(sk, *k), sq - ceil_div(sq, *q)) < 8) *k = *q = 1;
+// When `slots` workgroups at once are through n1 of length l1 and then n2 of length l2.
+int64_t finish(int64_t n1, int64_t l1, int64_t n2, int64_t l2, int64_t slots) {
+    const int64_t rounds = n1 / slots, late = n1 % slots, early = slots - late;
+    int64_t t = rounds * l1;
+    if (late) {
+        const int64_t fit = ceil_div(l1, l2) * early;  // taken while the last of the first are under way
+        if (n2 <= fit) return std::max(t + l1, t + ceil_div(n2, early) * l2);
+        n2 -= fit;
+        t += l1;
+    }
+    return t + ceil_div(n2, slots) * l2;
+}
+
+// Backward: whether eight waves take a tile, and workgroups that share the walk of a tile of keys, of queries.
+struct DiffBackPlan {
+    int32_t two, split_k, split_q;
+};
+DiffBackPlan diff_back_plan(const rt_diff_dims& d) {
+    const int64_t bh = (int64_t)d.B * d.H, nk = bh * ceil_div(d.Tk, rt::kDiffRows), nq = bh * ceil_div(d.Tq, rt::kDiffRows);
+    DiffBackPlan p{0, 1, 1};
+    if (nk == 0 || nq == 0) return p;
+    // half microseconds: of a walk's chunks of 32 rows, two waves to a SIMD
+    const int64_t wk = 4 * ceil_div(d.Tq, 32), wq = 3 * ceil_div(d.Tk, 32);
+    int64_t best = INT64_MAX;
+    for (int two = 0; two < 2; ++two) {
+        for (int i = 1; i <= 16; ++i) {
+            const int64_t part = ceil_div(std::max(wk, wq), i);
+            const int64_t sk = std::max<int64_t>(1, ceil_div(wk, std::max<int64_t>(part, 1))), sq = std::max<int64_t>(1, ceil_div(wq, std::max<int64_t>(part, 1)));
+            if (i > 1 && part < 16) break;
+            const int64_t lk = ceil_div(wk, sk * (two + 1)) + 20 + 6 * two, lq = ceil_div(wq, sq * (two + 1)) + 20 + 6 * two;
+            int64_t t = finish(nk * sk, lk, nq * sq, lq, two ? 256 : 512);
+            if (sk > 1 || sq > 1)  // the parts, written and read
+                t += 10 + ((sk > 1 ? nk * sk * 4 : 0) + (sq > 1 ? nq * sq * 2 : 0)) * (rt::kDiffRows * 4 * 2) * d.D / 3000000;
+            if (t < best) {
+                best = t;
+                p = DiffBackPlan{two, (int32_t)sk, (int32_t)sq};
+            }
+            if (nk + nq > 4096) break;  // tiles enough
+        }
+    }
+    return p;
 }
 int64_t diff_vals(const rt_diff_dims& d) { return (int64_t)d.B * d.H * 4 * whole64(d.Tq); }
 int64_t diff_part_k(const rt_diff_dims& d, int64_t split) {
@@ -1219,9 +1263,8 @@ int64_t diff_part_q(const rt_diff_dims& d, int64_t split) {
     return (int64_t)d.B * d.H * ceil_div(d.Tq, rt::kDiffRows) * split * 2 * rt::kDiffRows * d.D;
 }
 int64_t diff_back_workspace(const rt_diff_dims& d) {
-    int32_t k = 1, q = 1;
-    diff_back_split(d, &k, &q);
-    const int64_t parts = k > 1 || q > 1 ? diff_part_k(d, k) + diff_part_q(d, q) : 0;
+    const DiffBackPlan p = diff_back_plan(d);
+    const int64_t parts = (p.split_k > 1 ? diff_part_k(d, p.split_k) : 0) + (p.split_q > 1 ? diff_part_q(d, p.split_q) : 0);
     return std::max<int64_t>(16, (diff_vals(d) + parts) * 4);
 }
 
@@ -1347,9 +1390,12 @@ rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, con
     a.d_lam = d_lam;
     a.T64 = whole64(dims.Tq);
     a.row_vals = static_cast<float*>(workspace);
-    diff_back_split(dims, &a.split_k, &a.split_q);
+    const DiffBackPlan plan = diff_back_plan(dims);
+    a.two = plan.two;
+    a.split_k = plan.split_k;
+    a.split_q = plan.split_q;
     a.part_k = a.row_vals + diff_vals(dims);
-    a.part_q = a.part_k + diff_part_k(dims, a.split_k);
+    a.part_q = a.part_k + (a.split_k > 1 ? diff_part_k(dims, a.split_k) : 0);
     if (n_lam == 0) return ok();  // no heads
     return hip_status(rt::launch_diff_backward(a, dims.D, static_cast<hipStream_t>(stream)),
                       "differential attention gradient launch");

@@ -160,7 +160,7 @@ struct DiffRing {
     static constexpr int NB = 2 * D, WB = 4 * D, NT = BS * NB, WT = BS * WB;
     static constexpr int WIDE = 2 * NT, VAL = WIDE + WT, STAGE = VAL + (VALS ? BS * 16 : 0);
     static constexpr int ZERO = 2 * STAGE, LDS = ZERO + 64;
-    static_assert(W == 1 || W == 4, "whole fours of kilobytes");
+    static_assert(W == 1 || W % 4 == 0, "whole fours of kilobytes");
     static_assert(!VALS || BS * 16 % 512 == 0, "values in one load");
 
     uint32_t lds0;
@@ -175,10 +175,10 @@ struct DiffRing {
         rs[0] = buffer_rsrc(x1, rows * NB);
         rs[1] = buffer_rsrc(x2, rows * NB);
         rs[2] = buffer_rsrc(y, rows * WB);
-        // (a wave of four fills kilobytes of one place in four: the same offsets every time)
-        from_n[0] = narrow_from(W == 4 ? w : 0);
-        from_n[1] = W == 4 ? from_n[0] : narrow_from(1);
-        from_w = wide_from(W == 4 ? w : 0);
+        // (a wave of four or eight fills kilobytes of one place in four: the same offsets every time)
+        from_n[0] = narrow_from(W > 1 ? w : 0);
+        from_n[1] = W > 1 ? from_n[0] : narrow_from(1);
+        from_w = wide_from(W > 1 ? w : 0);
         if (w == 0 && lane < 4) *(lds_u32x4*)(lds + ZERO + 16 * lane) = u32x4{};
     }
     __device__ __forceinline__ void init_values(const float* vals, int T64_) {
@@ -192,8 +192,8 @@ struct DiffRing {
     __device__ __forceinline__ int wide_from(int kb) const {
         return Geo<D>::SWZ ? (lane >> 4) * WB + (((lane & 15) ^ wide_swz<D>((lane >> 4) | ((kb & 3) << 2))) * 16) : lane * 16;
     }
-    __device__ __forceinline__ int narrow_of(int n) const { return W == 4 ? from_n[0] : from_n[n & 1]; }
-    __device__ __forceinline__ int wide_of(int n) const { return W == 4 || !Geo<D>::SWZ ? from_w : from_w ^ ((n & 3) * 16); }
+    __device__ __forceinline__ int narrow_of(int n) const { return W > 1 ? from_n[0] : from_n[n & 1]; }
+    __device__ __forceinline__ int wide_of(int n) const { return W > 1 || !Geo<D>::SWZ ? from_w : from_w ^ ((n & 3) * 16); }
     template <int SIZE, bool WD>
     __device__ __forceinline__ void fill(uint32_t dst, int at, const i32x4& r) const {
         constexpr int FULL = SIZE / (1024 * W), REST = (SIZE - FULL * 1024 * W) / (16 * W);
@@ -676,28 +676,36 @@ __device__ __forceinline__ void sum_lam(const DiffArgs& a, double* lds, int h) {
     for (int bh = h; bh < a.n_bh; bh += step) {
         const float* x = a.row_vals + ((size_t)bh * 4 + 2) * a.T64;
 #pragma unroll 4
-        for (int t = threadIdx.x; t < a.T64; t += 256) s += x[t];
+        for (int t = threadIdx.x; t < a.T64; t += blockDim.x) s += x[t];
     }
     lds[threadIdx.x] = s;
-    for (int n = 128; n; n /= 2) {
+    for (int n = blockDim.x / 2; n; n /= 2) {
         __syncthreads();
         if ((int)threadIdx.x < n) lds[threadIdx.x] += lds[threadIdx.x + n];
     }
     if (threadIdx.x == 0) a.d_lam[h] = (float)lds[0];
 }
 
+// 16-byte pieces of a lane's sums
+template <int D, bool KV>
+constexpr int SUMS = (KV ? 32 : 16) + (D == 72 ? (KV ? 6 : 4) : 0);
+
 // Own rows K_1, K_2, V (KV) against X = Q_1, Q_2 and Y = dO of the queries, or own Q_1, Q_2, dO against K_1, K_2, V:
-// 32 own rows to a wave, 32 W to a workgroup.  SPLIT: against a part of the other side.
-template <int D, bool KV, int W, int BS, bool SPLIT>
+// 32 own rows to a wave, kDiffRows to a workgroup of four waves, against stages of BS rows; or (TWO) to one of eight, of
+// which four take the first half of each stage and four the other, and join their sums in LDS.  SPLIT: against a part
+// of the other side.
+template <int D, bool KV, int BS, bool TWO, bool SPLIT>
 __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int item, int part) {
-    using R = DiffRing<D, W, BS, KV>;
+    constexpr int W = kDiffRows / 32;
+    static_assert(!TWO || BS == 64, "a half to each four waves");
+    using R = DiffRing<D, TWO ? 2 * W : W, BS, KV>;
     using Rd = Reads<D>;
     constexpr int NB = R::NB, WB = R::WB, NW = KV ? 4 : 1;
     constexpr bool TAIL = D == 72;
     const int T = KV ? a.Tk : a.Tq, Tx = KV ? a.Tq : a.Tk;  // rows of the own side and of the other
     const int n_tile = (T + 32 * W - 1) / (32 * W), head = item / n_tile, bh = head_of(a, head), b = bh / a.H;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = ((item - head * n_tile) * W + wave) * 32;
-    const int keys = keys_of(a, b);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = TWO ? w % W : w, half = TWO ? w / W : 0;
+    const int row0 = ((item - head * n_tile) * W + wave) * 32, keys = keys_of(a, b);
     const int own_end = KV ? keys : T, x_end = KV ? Tx : keys;
     const int tile0 = row0 - 32 * wave;
     int n_st = (x_end + BS - 1) / BS;
@@ -722,8 +730,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     for (int i = 0; i < 2; ++i) rd.own_rows(own + (size_t)i * T * D, NB, row0, own_end, n_op[i], TAIL ? &n_tail[i] : nullptr);
     const int own_v = R::LDS + 32 * wave * WB, own_t = R::LDS + 32 * W * WB + wave * 1024;
     if constexpr (KV) {
-        ring.load_own(own_v, row0, buffer_rsrc(a.v + w_own, own_end * WB));
-        if (TAIL && !rd.hi) {
+        if (half == 0) ring.load_own(own_v, row0, buffer_rsrc(a.v + w_own, own_end * WB));
+        if (TAIL && half == 0 && !rd.hi) {
             *(lds_bf16x8*)(lds + own_t + rd.l32 * 16) = n_tail[0];
             *(lds_bf16x8*)(lds + own_t + 512 + rd.l32 * 16) = n_tail[1];
         }
@@ -754,8 +762,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
         ring.load(R::STAGE - st, (s + 1) * BS);
         if (row0 < own_end) {
 #pragma unroll
-            for (int h = 0; h < BS / 32; ++h) {
-                const int cw = st + R::WIDE + 32 * h * WB, first = s * BS + 32 * h;
+            for (int i = 0; i < (TWO ? 1 : BS / 32); ++i) {
+                const int h = TWO ? half : i, cw = st + R::WIDE + 32 * h * WB, first = s * BS + 32 * h;
                 if (KV) rd.unpack();
                 // four values of a chunk's rows 8 j + 4 hi ..
                 auto value = [&](int n, int j) {
@@ -838,12 +846,44 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
         st = R::STAGE - st;
     }
     wait_vm<0>();  // nothing may land in LDS after the workgroup has ended
+    if constexpr (TWO) {
+        // the second four waves' sums, in pieces of 16 bytes a lane
+        lds_u8* const at = lds + wave * SUMS<D, KV> * 1024 + rd.lane * 16;
+        auto each = [&](auto&& fn) {
+            int n = 0;
+            auto tile = [&](f32x16& c) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u, ++n) {
+                    f32x4 x = {c[4 * u], c[4 * u + 1], c[4 * u + 2], c[4 * u + 3]};
+                    fn(x, (lds_f32x4*)(at + n * 1024));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) c[4 * u + e] = x[e];
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tile(acc[i / 2][i % 2]);
+#pragma unroll
+            for (int d = 0; d < (KV ? 4 : 0); ++d) tile(wacc[d]);
+            if (TAIL) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i, ++n) fn(tacc[i / 2][i % 2], (lds_f32x4*)(at + n * 1024));
+#pragma unroll
+                for (int i = 0; i < (KV ? 2 : 0); ++i, ++n) fn(wtacc[i], (lds_f32x4*)(at + n * 1024));
+            }
+        };
+        __syncthreads();
+        if (half) each([](f32x4& x, lds_f32x4* p) { *p = x; });
+        __syncthreads();
+        if (half) return;
+        each([](f32x4& x, lds_f32x4* p) { x += *p; });
+    }
 
     // rows of a tile as fp32 [32][width] of a part, or rounded into the output (rows past the keys as zeros)
+    const bool parts = SPLIT && split > 1;
     auto store = [&](const f32x16* c, int tiles, const f32x4* t, int t_n, int width, float f, float* to, uint16_t* out) {
         const int row = row0 + rd.l32;
         auto put = [&](int r, int col, float x0, float x1, float x2, float x3) {
-            if (SPLIT) {
+            if (parts) {
                 *reinterpret_cast<f32x4*>(to + (r - row0) * width + col) = f32x4{x0, x1, x2, x3};
             } else if (r < T) {
                 uint32_t* p = reinterpret_cast<uint32_t*>(out + (size_t)r * width + col);
@@ -871,19 +911,21 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     };
     const float f2 = -lam * a.scale_nat;
     constexpr int TILE = 32 * W * D;  // of one map
-    float* to = SPLIT ? (KV ? a.part_k : a.part_q) + ((size_t)item * split + part) * ((KV ? 4 : 2) * TILE) : nullptr;
+    float* to = parts ? (KV ? a.part_k : a.part_q) + ((size_t)item * split + part) * ((KV ? 4 : 2) * TILE) : nullptr;
     uint16_t* const out = (KV ? a.dk : a.dq) + n_own;
     store(acc[0], 2, tacc[0], 8, D, a.scale_nat, to + 32 * wave * D, out);
     store(acc[1], 2, tacc[1], 8, D, f2, to + TILE + 32 * wave * D, out + (size_t)T * D);
     if (KV) store(wacc, 4, wtacc, 16, 2 * D, 1.0f, to + 2 * TILE + 32 * wave * (2 * D), a.dv + w_own);
 }
 
-template <int D, bool SPLIT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_bwd(DiffArgs a, int n_lam, int n_k,
-                                                                                          int per_k, int n_q, int per_q) {
-    constexpr int W = kDiffRows / 32;
-    constexpr int LDS_K = DiffRing<D, W, 32, true>::LDS + kDiffRows * (4 * D + (D == 72 ? 32 : 0)), LDS_Q = DiffRing<D, W, 64, false>::LDS;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[LDS_K > LDS_Q ? LDS_K : LDS_Q];
+constexpr int most(int x, int y) { return x > y ? x : y; }
+
+template <int D, bool TWO, bool SPLIT>
+__global__ __launch_bounds__(TWO ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_bwd(DiffArgs a, int n_lam, int n_k,
+                                                                                                     int per_k, int n_q, int per_q) {
+    constexpr int W = TWO ? 8 : 4, BS_K = TWO ? 64 : 32;
+    constexpr int LDS_K = DiffRing<D, W, BS_K, true>::LDS + kDiffRows * (4 * D + (D == 72 ? 32 : 0)), LDS_Q = DiffRing<D, W, 64, false>::LDS;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[most(most(LDS_K, LDS_Q), TWO ? 4 * SUMS<D, true> * 1024 : 0)];
     lds_u8* const lds = (lds_u8*)smem;
     int g = blockIdx.x;
     const int lam8 = (n_lam + 7) & ~7;  // (whole eights, so that a tile's XCD goes by its number)
@@ -903,20 +945,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         item /= split;
     }
     if (kv)
-        diff_walk<D, true, W, 32, SPLIT>(a, lds, item, part);
+        diff_walk<D, true, BS_K, TWO, SPLIT>(a, lds, item, part);
     else
-        diff_walk<D, false, W, 64, SPLIT>(a, lds, item, part);
+        diff_walk<D, false, 64, TWO, SPLIT>(a, lds, item, part);
 }
 
-// Sums of a tile's parts: dK_1, dK_2, the halves of dV (blockIdx.y 0 .. 3; `tiles_k` of them in x), then dQ_1, dQ_2
+// Sums of a tile's parts: dK_1, dK_2, the halves of dV (kind 0 .. 3; `tiles_k` of them in x), then dQ_1, dQ_2 (4, 5);
+// blockIdx.y counts from `kind0`
 template <int D>
-__global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int tiles_k, int tiles_q) {
+__global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int kind0, int tiles_k, int tiles_q) {
     constexpr int TILE = kDiffRows * D;
-    const bool kv = blockIdx.y < 4;
+    const int kind = kind0 + blockIdx.y;
+    const bool kv = kind < 4;
     if ((int)blockIdx.x >= (kv ? tiles_k : tiles_q)) return;
     const int T = kv ? a.Tk : a.Tq, n_tile = (T + kDiffRows - 1) / kDiffRows, n = kv ? a.split_k : a.split_q;
     const int head = blockIdx.x / n_tile, bh = head_of(a, head), row0 = (blockIdx.x - head * n_tile) * kDiffRows;
-    const int width = kv && blockIdx.y >= 2 ? 2 * D : D, which = kv ? blockIdx.y : blockIdx.y - 4;
+    const int width = kv && kind >= 2 ? 2 * D : D, which = kv ? kind : kind - 4;
     const size_t stride = (kv ? 4 : 2) * (size_t)TILE;
     const float* part = (kv ? a.part_k : a.part_q) + (size_t)blockIdx.x * n * stride + (size_t)which * TILE;
     uint16_t* out;
@@ -952,15 +996,18 @@ hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
     const int n_k = tiles_k * a.split_k, n_q = tiles_q * a.split_q, per_k = (n_k + 7) / 8, per_q = (n_q + 7) / 8;
     const int n_lam = a.lam_step ? a.H : 1;
     const dim3 grid(((n_lam + 7) & ~7) + 8 * per_k + 8 * per_q);
-    if (!split) {
-        hipLaunchKernelGGL((diff_bwd<D, false>), grid, dim3(256), 0, stream, a, n_lam, n_k, per_k, n_q, per_q);
+    auto run = [&](auto kernel, int threads) {
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, a, n_lam, n_k, per_k, n_q, per_q);
         return hipGetLastError();
-    }
-    hipLaunchKernelGGL((diff_bwd<D, true>), grid, dim3(256), 0, stream, a, n_lam, n_k, per_k, n_q, per_q);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const int most = tiles_k > tiles_q ? tiles_k : tiles_q;
-    hipLaunchKernelGGL((diff_sum<D>), dim3(most, 6, kDiffRows * D / 1024), dim3(256), 0, stream, a, tiles_k, tiles_q);
+    };
+    if (a.two)
+        e = split ? run(diff_bwd<D, true, true>, 512) : run(diff_bwd<D, true, false>, 512);
+    else
+        e = split ? run(diff_bwd<D, false, true>, 256) : run(diff_bwd<D, false, false>, 256);
+    if (e != hipSuccess || !split) return e;
+    const int sums_k = a.split_k > 1 ? tiles_k : 0, sums_q = a.split_q > 1 ? tiles_q : 0, kind0 = sums_k ? 0 : 4;
+    hipLaunchKernelGGL((diff_sum<D>), dim3(most(sums_k, sums_q), (sums_q ? 6 : 4) - kind0, kDiffRows * D / 1024), dim3(256), 0, stream, a,
+                       kind0, sums_k, sums_q);
     return hipGetLastError();
 }
 
