@@ -858,31 +858,43 @@ def rope_plan(rotated, base=10000.0, widths=None, layout="interleaved", scaling=
 _ROPE_LAYOUTS = {"interleaved": _lib.RT_ROPE_INTERLEAVED, "half": _lib.RT_ROPE_HALF}
 
 
-def _rope_positions(positions, plan, x):
-    """Checks a plan and positions against x; the positions' C type and whether each sample has its own."""
+def _checked_plan(plan):
+    """The device index of a plan's arrays, checked once."""
     torch = _torch()
     if not isinstance(plan, RopePlan):
         raise ValueError("plan must be a RopePlan")
-    if plan.layout not in _ROPE_LAYOUTS:
-        raise ValueError(f"layout={plan.layout!r} (need one of {sorted(_ROPE_LAYOUTS)})")
-    _on_device(plan.freq, "plan.freq", x.device)
-    if plan.freq.dtype is not torch.float64 or plan.freq.dim() != 1 or not plan.freq.is_contiguous():
-        raise ValueError("plan.freq must be a contiguous fp64 vector")
-    if plan.axis is None:
-        if plan.axes != 1:
+    at = plan.__dict__.get("_at")
+    if at is None:
+        if plan.layout not in _ROPE_LAYOUTS:
+            raise ValueError(f"layout={plan.layout!r} (need one of {sorted(_ROPE_LAYOUTS)})")
+        _on_device(plan.freq, "plan.freq", None)
+        if plan.freq.dtype is not torch.float64 or plan.freq.dim() != 1 or not plan.freq.is_contiguous():
+            raise ValueError("plan.freq must be a contiguous fp64 vector")
+        if plan.axis is not None:
+            _on_device(plan.axis, "plan.axis", plan.freq.device)
+            if plan.axis.dtype is not torch.int32 or plan.axis.shape != plan.freq.shape or not plan.axis.is_contiguous():
+                raise ValueError("plan.axis must be a contiguous int32 vector of plan.freq's length")
+        elif plan.axes != 1:
             raise ValueError("plan.axis is needed where there are several axes")
-    else:
-        _on_device(plan.axis, "plan.axis", x.device)
-        if plan.axis.dtype is not torch.int32 or plan.axis.shape != plan.freq.shape or not plan.axis.is_contiguous():
-            raise ValueError("plan.axis must be a contiguous int32 vector of plan.freq's length")
-    _on_device(positions, "positions", x.device)
-    kind = {torch.int32: _lib.RT_POS_I32, torch.int64: _lib.RT_POS_I64, torch.float32: _lib.RT_POS_F32}.get(positions.dtype)
-    B, T = x.shape[0], x.shape[2]
-    last = () if plan.axes == 1 else (plan.axes,)
-    shape = tuple(positions.shape)
-    if kind is None or shape not in ((T,) + last, (B, T) + last) or not positions.is_contiguous():
+        at = plan.__dict__["_at"] = plan.freq.get_device()
+    return at
+
+
+@functools.lru_cache(maxsize=1024)
+def _rope_dims(shape, stride, dtype, out_stride, positions, kind, rotated, layout, axes, name):
+    """The rt_rope_dims of such a call and the strides of x and y (out_stride None: contiguous)."""
+    torch = _torch()
+    if len(shape) != 4:
+        raise ValueError(f"{name} must be a [B,H,T,D] tensor")
+    xs = _norm_strides(shape, stride, dtype, name)
+    B, H, T, D = shape
+    ys = _norm_strides(shape, (H * T * D, T * D, D, 1) if out_stride is None else out_stride, dtype, "out")
+    last = () if axes == 1 else (axes,)
+    kind = {torch.int32: _lib.RT_POS_I32, torch.int64: _lib.RT_POS_I64, torch.float32: _lib.RT_POS_F32}.get(kind)
+    if kind is None or positions not in ((T,) + last, (B, T) + last):
         raise ValueError(f"positions must be a contiguous int32, int64 or fp32 tensor of shape {(T,) + last} or {(B, T) + last}")
-    return kind, shape != (T,) + last
+    return _lib.RtRopeDims(*shape, _norm_types()[dtype], rotated, _ROPE_LAYOUTS[layout], axes, kind,
+                           positions != (T,) + last), xs, ys
 
 
 def _rope(fn, name, x, positions, plan, out):
@@ -890,24 +902,27 @@ def _rope(fn, name, x, positions, plan, out):
     lib = _lib.load()
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         _on_device(x, name, None)
-    shape = tuple(x.shape)
-    if len(shape) != 4:
-        raise ValueError(f"{name} must be a [B,H,T,D] tensor")
-    xs = _norm_strides(shape, x.stride(), x.dtype, name)
-    kind, per_sample = _rope_positions(positions, plan, x)
-    if out is None:
-        y = torch.empty(shape, dtype=x.dtype, device=x.device)
-        ys = _norm_strides(shape, y.stride(), x.dtype, "out")
-    else:
+    at, shape = x.get_device(), x.shape
+    if _checked_plan(plan) != at:
+        raise ValueError(f"plan is on device {plan.freq.device}, expected {x.device}")
+    if not isinstance(positions, torch.Tensor) or not positions.is_cuda or positions.get_device() != at:
+        _on_device(positions, "positions", x.device)
+    if not positions.is_contiguous():
+        raise ValueError("positions must be contiguous")
+    if out is not None:
         _on_device(out, "out", x.device)
-        if out.dtype is not x.dtype or out.shape != x.shape:
+        if out.dtype is not x.dtype or out.shape != shape:
             raise ValueError(f"out must have the type and shape of {name}")
-        y, ys = out, _norm_strides(shape, out.stride(), x.dtype, "out")
-    dims = _lib.RtRopeDims(*shape, _norm_types()[x.dtype], plan.rotated, _ROPE_LAYOUTS[plan.layout], plan.axes, kind,
-                           per_sample)
+    dims, xs, ys = _rope_dims(shape, x.stride(), x.dtype, None if out is None else out.stride(), positions.shape,
+                              positions.dtype, plan.rotated, plan.layout, plan.axes, name)
+    y = x.new_empty(shape) if out is None else out
+    axis = plan.axis
     with _on(x):
-        _lib.check(fn, getattr(lib, fn)(_ptr(x), xs, _ptr(positions), _ptr(plan.freq), _ptr(plan.axis),
-                                        float(plan.amplitude), dims, _ptr(y), ys, _stream(x)))
+        status = getattr(lib, fn)(x.data_ptr(), xs, positions.data_ptr(), plan.freq.data_ptr(),
+                                  None if axis is None else axis.data_ptr(), plan.amplitude, dims, y.data_ptr(), ys,
+                                  _stream(x))
+    if status:
+        _lib.check(fn, status)
     return y
 
 
@@ -930,34 +945,47 @@ def rope_backward(d_y, positions, plan: RopePlan, out=None):
 
 
 @functools.lru_cache(maxsize=1024)
-def _diff_bytes(fn, dims):
-    """Workspace of a differential attention call of these (B, H, Tq, Tk, D)."""
-    need = ctypes.c_int64(0)
-    _lib.check(fn, getattr(_lib.load(), fn)(_lib.RtDiffDims(*dims), ctypes.byref(need)))
-    return need.value
+def _diff_dims(q, k, v, lam, lens):
+    """Of a differential attention call of these shapes: the rt_diff_dims, o's and the statistics' shapes, the
+    workspaces of the forward and of the gradient call."""
+    if len(q) != 4 or len(k) != 4 or len(v) != 4:
+        raise ValueError("q, k and v must be tensors of 4 dimensions")
+    B, H2, Tq, D = q
+    H, Tk = H2 // 2, k[2]
+    if H2 % 2 or k != (B, H2, Tk, D) or v != (B, H, Tk, 2 * D):
+        raise ValueError("need q [B,2H,Tq,D], k [B,2H,Tk,D] and v [B,H,Tk,2D]")
+    if lam not in ((), (1,), (H,)):
+        raise ValueError(f"lam must be a contiguous fp32 tensor of shape (), (1,) or ({H},)")
+    if lens is not None and lens != (B,):
+        raise ValueError(f"k_lens must be a contiguous int32 tensor of shape ({B},)")
+    dims, lib, need = _lib.RtDiffDims(B, H, Tq, Tk, D), _lib.load(), []
+    for fn in ("rt_attn_diff_workspace", "rt_attn_diff_backward_workspace"):
+        n = ctypes.c_int64(0)
+        _lib.check(fn, getattr(lib, fn)(dims, ctypes.byref(n)))
+        need.append(n.value)
+    return dims, (B, H, Tq, 2 * D), (B, H2, Tq), need[0], need[1]
 
 
 def _diff_inputs(q, k, v, lam, k_lens):
-    """Checks the inputs of differential attention; (B, H, Tq, Tk, D)."""
+    """Checks the inputs of differential attention; _diff_dims of them."""
     torch = _torch()
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != q.get_device():
+    bf16 = torch.bfloat16
+    try:  # one expression for the usual case; anything else is named below
+        at = q.get_device()
+        fine = (at >= 0 and q.dtype is bf16 and k.dtype is bf16 and v.dtype is bf16 and lam.dtype is torch.float32
+                and k.get_device() == at and v.get_device() == at and lam.get_device() == at and q.is_contiguous()
+                and k.is_contiguous() and v.is_contiguous() and lam.is_contiguous()
+                and (k_lens is None or (k_lens.dtype is torch.int32 and k_lens.get_device() == at and k_lens.is_contiguous())))
+    except (AttributeError, TypeError):
+        fine = False
+    if not fine:
+        for name, t, dtype in (("q", q, bf16), ("k", k, bf16), ("v", v, bf16), ("lam", lam, torch.float32), ("k_lens", k_lens, torch.int32)):
+            if t is None and name == "k_lens":
+                continue
             _on_device(t, name, None if t is q else q.device)
-        if t.dtype is not torch.bfloat16 or t.dim() != 4 or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous bf16 tensor of 4 dimensions")
-    B, H2, Tq, D = q.shape
-    H, Tk = H2 // 2, k.shape[2]
-    if H2 % 2 or tuple(k.shape) != (B, H2, Tk, D) or tuple(v.shape) != (B, H, Tk, 2 * D):
-        raise ValueError("need q [B,2H,Tq,D], k [B,2H,Tk,D] and v [B,H,Tk,2D]")
-    if not (isinstance(lam, torch.Tensor) and lam.is_cuda and lam.get_device() == q.get_device()):
-        _on_device(lam, "lam", q.device)
-    if lam.dtype is not torch.float32 or tuple(lam.shape) not in ((), (1,), (H,)) or not lam.is_contiguous():
-        raise ValueError(f"lam must be a contiguous fp32 tensor of shape (), (1,) or ({H},)")
-    if k_lens is not None:
-        _on_device(k_lens, "k_lens", q.device)
-        if k_lens.dtype is not torch.int32 or tuple(k_lens.shape) != (B,) or not k_lens.is_contiguous():
-            raise ValueError(f"k_lens must be a contiguous int32 tensor of shape ({B},)")
-    return B, H, Tq, Tk, D
+            if t.dtype is not dtype or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {str(dtype)[6:]} tensor")
+    return _diff_dims(q.shape, k.shape, v.shape, lam.shape, None if k_lens is None else k_lens.shape)
 
 
 def attn_diff(q, k, v, lam, k_lens=None, stats=True, out=None):
@@ -968,22 +996,21 @@ def attn_diff(q, k, v, lam, k_lens=None, stats=True, out=None):
     with room for more); without keys the output is 0.  Returns o [B,H,Tq,2D], with stats (o, o2, row_max, row_sum) as
     attn_diff_backward takes them: the second map's output, and of both maps' rows the largest score and the sum of
     exponentials against it, fp32 [B,2H,Tq]."""
-    torch = _torch()
     lib = _lib.load()
-    B, H, Tq, Tk, D = dims = _diff_inputs(q, k, v, lam, k_lens)
-    shape = (B, H, Tq, 2 * D)
-    o = torch.empty(shape, dtype=q.dtype, device=q.device) if out is None else _bf16(out, shape, "out", q.device)
-    o2 = m = l = None
+    dims, shape, rows, need, _ = _diff_inputs(q, k, v, lam, k_lens)
+    o = q.new_empty(shape) if out is None else _bf16(out, shape, "out", q.device)
+    o2 = m = l = work = None
     if stats:
-        o2 = torch.empty_like(o)
-        m = torch.empty((B, 2 * H, Tq), dtype=torch.float32, device=q.device)
-        l = torch.empty_like(m)
-    need = _diff_bytes("rt_attn_diff_workspace", dims)
-    work = _workspace(need, q)
+        o2 = q.new_empty(shape)
+        m = lam.new_empty(rows)
+        l = lam.new_empty(rows)
+    if need > 16:  # keys in parts
+        work = _workspace(need, q)
     with _on(q):
-        _lib.check("rt_attn_diff",
-                   lib.rt_attn_diff(_ptr(q), _ptr(k), _ptr(v), _ptr(lam), lam.numel(), _ptr(k_lens), _lib.RtDiffDims(*dims),
-                                    _ptr(o), _ptr(o2), _ptr(m), _ptr(l), _ptr(work), need, _stream(q)))
+        status = lib.rt_attn_diff(q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), lam.numel(), _ptr(k_lens), dims,
+                                  o.data_ptr(), _ptr(o2), _ptr(m), _ptr(l), _ptr(work), need, _stream(q))
+    if status:
+        _lib.check("rt_attn_diff", status)
     return (o, o2, m, l) if stats else o
 
 
@@ -994,25 +1021,28 @@ def attn_diff_backward(q, k, v, o, o2, row_max, row_sum, d_o, lam, k_lens=None, 
     of new ones."""
     torch = _torch()
     lib = _lib.load()
-    B, H, Tq, Tk, D = dims = _diff_inputs(q, k, v, lam, k_lens)
+    dims, shape, rows, _, need = _diff_inputs(q, k, v, lam, k_lens)
     for name, t in (("o", o), ("o2", o2), ("d_o", d_o)):
-        _bf16(t, (B, H, Tq, 2 * D), name, q.device)
+        if not _same(t, torch.bfloat16, shape, q):
+            _bf16(t, shape, name, q.device)
     for name, t in (("row_max", row_max), ("row_sum", row_sum)):
-        _stat(t, (B, 2 * H, Tq), name, q.device)
+        if not _same(t, torch.float32, rows, q):
+            _stat(t, rows, name, q.device)
     if out is None:
-        dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
+        dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
     else:
         if len(out) != 3:
             raise ValueError("out must hold dq, dk and dv")
         dq, dk, dv = (_bf16(t, like.shape, name, q.device) for t, like, name in zip(out, (q, k, v), ("dq", "dk", "dv")))
-    d_lam = torch.empty_like(lam)
-    need = _diff_bytes("rt_attn_diff_backward_workspace", dims)
+    d_lam = lam.new_empty(lam.shape)
     work = _workspace(need, q)
     with _on(q):
-        _lib.check("rt_attn_diff_backward",
-                   lib.rt_attn_diff_backward(_ptr(q), _ptr(k), _ptr(v), _ptr(lam), lam.numel(), _ptr(k_lens), _ptr(o),
-                                             _ptr(o2), _ptr(row_max), _ptr(row_sum), _ptr(d_o), _lib.RtDiffDims(*dims),
-                                             _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_lam), _ptr(work), need, _stream(q)))
+        status = lib.rt_attn_diff_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), lam.numel(),
+                                           _ptr(k_lens), o.data_ptr(), o2.data_ptr(), row_max.data_ptr(),
+                                           row_sum.data_ptr(), d_o.data_ptr(), dims, dq.data_ptr(), dk.data_ptr(),
+                                           dv.data_ptr(), d_lam.data_ptr(), work.data_ptr(), need, _stream(q))
+    if status:
+        _lib.check("rt_attn_diff_backward", status)
     return dq, dk, dv, d_lam
 
 
