@@ -46,8 +46,8 @@ __device__ __forceinline__ int wide_swz(int r) {
 __device__ __forceinline__ void fresh(int& x) { asm volatile("" : "+v"(x)); }
 
 // A wave's reads of narrow rows (queries or keys, D wide) and of wide ones (values or output gradients, 2 D wide).
-// 72-wide heads: narrow rows' last 8 elements are half a k-step of the scores and a 16x16x32 product of the gradients,
-// of which they fill half; wide rows' last 16 fill both.
+// 72-wide heads: narrow rows' last 8 elements are half a k-step of the scores; in the gradients those of both maps share
+// the 16 rows of a 16x16x32 product, which wide rows' last 16 fill by themselves.
 template <int D>
 struct Reads {
     static constexpr int NB = 2 * D, WB = 4 * D;   // bytes of a row
@@ -120,7 +120,11 @@ struct Reads {
         return SWZ ? tr_read(p + (w_tr ^ (64 * dt)), p + 8 * WB + (w_tr ^ (64 * dt) ^ 32))
                    : tr_read(p + w_tr + 64 * dt, p + 8 * WB + w_tr + 64 * dt);
     }
-    __device__ __forceinline__ bf16x8 n_col_tail(int base) const { return tr_read(lds + base + n_t, lds + base + n_t + 8 * NB); }
+    // narrow rows' last 8 elements for map i: in rows 8 i .. + 7 of the product, zeros in the others
+    __device__ __forceinline__ bf16x8 n_col_tail(int base, int i, int zero) const {
+        const bool mine = ((lane >> 1) & 1) == i;
+        return tr_read(lds + (mine ? base + n_t : zero), lds + (mine ? base + n_t + 8 * NB : zero));
+    }
     __device__ __forceinline__ bf16x8 w_col_tail(int base) const { return tr_read(lds + base + w_t, lds + base + w_t + 8 * WB); }
 
     // rows row0 .. + 31 of x (zeros from row `end` on): lane holds row l32, elements 16 s + 8 hi ..
@@ -688,7 +692,7 @@ __device__ __forceinline__ void sum_lam(const DiffArgs& a, double* lds, int h) {
 
 // 16-byte pieces of a lane's sums
 template <int D, bool KV>
-constexpr int SUMS = (KV ? 32 : 16) + (D == 72 ? (KV ? 6 : 4) : 0);
+constexpr int SUMS = (KV ? 32 : 16) + (D == 72 ? (KV ? 4 : 2) : 0);
 
 // Own rows K_1, K_2, V (KV) against X = Q_1, Q_2 and Y = dO of the queries, or own Q_1, Q_2, dO against K_1, K_2, V:
 // 32 own rows to a wave, kDiffRows to a workgroup of four waves, against stages of BS rows; or (TWO) to one of eight, of
@@ -747,11 +751,11 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     const float c2 = a.scale_log2, lam = a.lam[(bh - b * a.H) * a.lam_step];
 
     f32x16 acc[2][2], wacc[NW];  // dK or dQ of each map; dV
-    f32x4 tacc[2][2], wtacc[2];
+    f32x4 tacc[2], wtacc[2];  // 72 wide: both maps' last 8 elements, dV's last 16, of 16 own rows each
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         acc[i][0] = acc[i][1] = f32x16{};
-        tacc[i][0] = tacc[i][1] = wtacc[i] = f32x4{};
+        tacc[i] = wtacc[i] = f32x4{};
     }
 #pragma unroll
     for (int d = 0; d < NW; ++d) wacc[d] = f32x16{};
@@ -821,12 +825,14 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
 #pragma unroll
                     for (int k = 0; k < 4; ++k) acc[i][k & 1] = mma(rd.n_col(cx, k & 1, k >> 1), op(ds, k >> 1), acc[i][k & 1]);
                     if (TAIL) {
-                        const bf16x8 c = rd.n_col_tail(cx);
+                        // (zeros meet the other map's NaN: a row that has one has it in both, through its delta)
+                        const bf16x8 c = rd.n_col_tail(cx, i, R::ZERO);
                         uint32_t y[8];
                         halves(ds, y);
-                        tacc[i][0] = mma16(c, op(y, 0), tacc[i][0]);
-                        tacc[i][1] = mma16(c, op(y, 1), tacc[i][1]);
+                        tacc[0] = mma16(c, op(y, 0), tacc[0]);
+                        tacc[1] = mma16(c, op(y, 1), tacc[1]);
                     }
+                    if (KV && TAIL) __builtin_amdgcn_sched_barrier(0);
                 }
                 if (KV) {
 #pragma unroll
@@ -866,7 +872,7 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
             for (int d = 0; d < (KV ? 4 : 0); ++d) tile(wacc[d]);
             if (TAIL) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i, ++n) fn(tacc[i / 2][i % 2], (lds_f32x4*)(at + n * 1024));
+                for (int i = 0; i < 2; ++i, ++n) fn(tacc[i], (lds_f32x4*)(at + n * 1024));
 #pragma unroll
                 for (int i = 0; i < (KV ? 2 : 0); ++i, ++n) fn(wtacc[i], (lds_f32x4*)(at + n * 1024));
             }
@@ -880,7 +886,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
 
     // rows of a tile as fp32 [32][width] of a part, or rounded into the output (rows past the keys as zeros)
     const bool parts = SPLIT && split > 1;
-    auto store = [&](const f32x16* c, int tiles, const f32x4* t, int t_n, int width, float f, float* to, uint16_t* out) {
+    // lanes from t0 on: the rows of t that hold the last elements
+    auto store = [&](const f32x16* c, int tiles, const f32x4* t, int t0, int t_n, int width, float f, float* to, uint16_t* out) {
         const int row = row0 + rd.l32;
         auto put = [&](int r, int col, float x0, float x1, float x2, float x3) {
             if (parts) {
@@ -900,12 +907,13 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
                 put(row, 32 * d + 16 * rd.hi + 4 * u, v(0), v(1), v(2), v(3));
             }
         }
-        if (TAIL && 4 * (rd.lane >> 4) < t_n) {
+        const int g = (rd.lane - t0) >> 4;  // group of four rows
+        if (TAIL && g >= 0 && 4 * g < t_n) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int r = row0 + 16 * h + (rd.lane & 15);
                 auto v = [&](int e) { return r >= own_end ? 0.f : t[h][e] * f; };
-                put(r, width - t_n + 4 * (rd.lane >> 4), v(0), v(1), v(2), v(3));
+                put(r, width - t_n + 4 * g, v(0), v(1), v(2), v(3));
             }
         }
     };
@@ -913,9 +921,9 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     constexpr int TILE = 32 * W * D;  // of one map
     float* to = parts ? (KV ? a.part_k : a.part_q) + ((size_t)item * split + part) * ((KV ? 4 : 2) * TILE) : nullptr;
     uint16_t* const out = (KV ? a.dk : a.dq) + n_own;
-    store(acc[0], 2, tacc[0], 8, D, a.scale_nat, to + 32 * wave * D, out);
-    store(acc[1], 2, tacc[1], 8, D, f2, to + TILE + 32 * wave * D, out + (size_t)T * D);
-    if (KV) store(wacc, 4, wtacc, 16, 2 * D, 1.0f, to + 2 * TILE + 32 * wave * (2 * D), a.dv + w_own);
+    store(acc[0], 2, tacc, 0, 8, D, a.scale_nat, to + 32 * wave * D, out);
+    store(acc[1], 2, tacc, 32, 8, D, f2, to + TILE + 32 * wave * D, out + (size_t)T * D);
+    if (KV) store(wacc, 4, wtacc, 0, 16, 2 * D, 1.0f, to + 2 * TILE + 32 * wave * (2 * D), a.dv + w_own);
 }
 
 constexpr int most(int x, int y) { return x > y ? x : y; }
