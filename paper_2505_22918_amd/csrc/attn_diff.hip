@@ -23,6 +23,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "attn_common.h"
 #include "attn_grad_tiles.h"
 #include "heads.h"
@@ -315,15 +317,15 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
         return __int_as_float(__builtin_amdgcn_ds_bpermute((16 * h + (rd.lane & 15)) << 2, __float_as_int(x)));
     };
     const float c2 = a.scale_log2;
-    int st = 0;
-    for (int s = first_stage; s < end_stage; s += STEP) {
+    auto stage = [&](auto odd, int s) {
+        constexpr int st = decltype(odd)::value ? R::STAGE : 0;
         ring.turn();
         ring.load(R::STAGE - st, (s + STEP) * BS);
         if (row0 < a.Tq) {
-#pragma nounroll
+#pragma unroll
             for (int h = 0; h < BS / 32; ++h) {
                 const int first = s * BS + 32 * h, cv = st + R::WIDE + 32 * h * WB;
-                rd.unpack();
+                if (D == 72) rd.unpack();
                 const int cx = st + 32 * h * NB;
                 auto mask = [&](f32x16& sc) {
                     if (first + 32 > keys) {
@@ -408,7 +410,10 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
                 }
             }
         }
-        st = R::STAGE - st;
+    };
+    for (int s = first_stage; s < end_stage; s += 2 * STEP) {
+        stage(std::integral_constant<bool, false>{}, s);
+        if (s + STEP < end_stage) stage(std::integral_constant<bool, true>{}, s + STEP);
     }
     wait_vm<0>();  // nothing may land in LDS after the workgroup has ended
     if (row0 >= a.Tq) return;
@@ -784,24 +789,19 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
                 } else {
                     dp = f32x16{} + minus;
                 }
-#pragma unroll
-                for (int k = 0; k < Rd::WS; ++k) dp = mma(rd.w_row(cw, k), KV ? rd.w_row(own_v, k) : w_op[KV ? 0 : k], dp);
-                f32x16 p1;  // map 1's probabilities (KV)
-                uint32_t pk[8], ds[8];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int cx = st + i * R::NT + 32 * h * NB;
-                    f32x16 sc = {};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) sc = mma(rd.n_row(cx, k), n_op[i][k], sc);
-                    if (TAIL)
-                        sc = mma(rd.n_row_tail(cx, R::ZERO), KV ? *(const lds_bf16x8*)(lds + (rd.hi ? R::ZERO : own_t + 512 * i + rd.l32 * 16)) : n_tail[i], sc);
+                const int cx = st + 32 * h * NB;
+                auto mask = [&](f32x16& sc) {
                     if (!KV && first + 32 > keys) {
                         const int lim = keys - first - 4 * rd.hi;
 #pragma unroll
                         for (int x = 0; x < 16; ++x)
                             if (8 * (x >> 2) + (x & 3) >= lim) sc[x] = -INFINITY;
                     }
+                };
+                f32x16 p1;  // map 1's probabilities (KV)
+                uint32_t pk[8], ds[2][8];
+                // P and dS of a map, a matrix product after every four of them
+                auto soft = [&](int i, const f32x16& sc, auto&& product) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         f32x4 lg = {log[i], log[i], log[i], log[i]}, mo = {more, more, more, more};
@@ -813,26 +813,57 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
                             const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -lg[e]));
                             const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -lg[e + 1]));
                             if (i == 0) {
-                                ds[x / 2] = pack_bf16(e0 * (dp[x] + mo[e]), e1 * (dp[x + 1] + mo[e + 1]));
+                                ds[0][x / 2] = pack_bf16(e0 * (dp[x] + mo[e]), e1 * (dp[x + 1] + mo[e + 1]));
                                 p1[x] = e0;
                                 p1[x + 1] = e1;
                             } else {
-                                ds[x / 2] = pack_bf16(e0 * dp[x], e1 * dp[x + 1]);
+                                ds[1][x / 2] = pack_bf16(e0 * dp[x], e1 * dp[x + 1]);
                                 if (KV) pk[x / 2] = pack_bf16(__builtin_fmaf(-lam, e0, p1[x]), __builtin_fmaf(-lam, e1, p1[x + 1]));
                             }
                         }
+                        product(j);
                     }
+                };
+                auto grad = [&](int i, int k) { acc[i][k & 1] = mma(rd.n_col(cx + i * R::NT, k & 1, k >> 1), op(ds[i], k >> 1), acc[i][k & 1]); };
+                f32x16 s0 = {}, s1 = {};
+                auto score = [&](int i, int k, f32x16& sc) { sc = mma(rd.n_row(cx + i * R::NT, k), n_op[i][k], sc); };
+                auto pull = [&](int k) { dp = mma(rd.w_row(cw, k), KV ? rd.w_row(own_v, k) : w_op[KV ? 0 : k], dp); };
+                if constexpr (!TAIL) {
+                    // what does not wait for what stands side by side: 16.2 to 15.9 ms at the CogVideoX shape
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[i][k & 1] = mma(rd.n_col(cx, k & 1, k >> 1), op(ds, k >> 1), acc[i][k & 1]);
-                    if (TAIL) {
-                        // (zeros meet the other map's NaN: a row that has one has it in both, through its delta)
-                        const bf16x8 c = rd.n_col_tail(cx, i, R::ZERO);
-                        uint32_t y[8];
-                        halves(ds, y);
-                        tacc[0] = mma16(c, op(y, 0), tacc[0]);
-                        tacc[1] = mma16(c, op(y, 1), tacc[1]);
+                    for (int k = 0; k < Rd::WS; ++k) {
+                        pull(k);
+                        if (k < 4) score(0, k, s0);
                     }
-                    if (KV && TAIL) __builtin_amdgcn_sched_barrier(0);
+                    mask(s0);
+                    soft(0, s0, [&](int k) { score(1, k, s1); });
+                    mask(s1);
+                    soft(1, s1, [&](int k) { grad(0, k); });
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) grad(1, k);
+                } else {
+                    // 72-wide heads have no registers for that (8.6 to 9.2 ms, 16 heads of 16384 tokens): a map at a time
+#pragma unroll
+                    for (int k = 0; k < Rd::WS; ++k) pull(k);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        f32x16& sc = i ? s1 : s0;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) score(i, k, sc);
+                        const bf16x8 y = KV ? *(const lds_bf16x8*)(lds + (rd.hi ? R::ZERO : own_t + 512 * i + rd.l32 * 16)) : n_tail[i];
+                        sc = mma(rd.n_row_tail(cx + i * R::NT, R::ZERO), y, sc);
+                        mask(sc);
+                        soft(i, sc, [](int) {});
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) grad(i, k);
+                        // (zeros meet the other map's NaN: a row that has one has it in both, through its delta)
+                        const bf16x8 c = rd.n_col_tail(cx + i * R::NT, i, R::ZERO);
+                        uint32_t z[8];
+                        halves(ds[i], z);
+                        tacc[0] = mma16(c, op(z, 0), tacc[0]);
+                        tacc[1] = mma16(c, op(z, 1), tacc[1]);
+                        if (KV) __builtin_amdgcn_sched_barrier(0);  // else registers spill
+                    }
                 }
                 if (KV) {
 #pragma unroll
