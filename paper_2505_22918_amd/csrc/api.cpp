@@ -1060,7 +1060,7 @@ rt_status rt_layer_norm_backward(const void* dy, const int64_t dy_stride[3], con
 namespace {
 
 // How a thread's pieces and heads are chosen: the widest piece that all rows start on and hold whole numbers of, and as
-// many heads as leave 16 waves to a CU (a token's angles are formed once for them all).
+// many heads as leave 32 waves to a CU (a token's angles are formed once for them all).
 void set_rope(rt::RopeArgs& a, std::initializer_list<std::pair<const void*, const int64_t*>> ts) {
     const int64_t size = type_bytes(a.type), n[3] = {a.B, a.H, a.T};
     a.vec = 1;
@@ -1076,7 +1076,7 @@ void set_rope(rt::RopeArgs& a, std::initializer_list<std::pair<const void*, cons
             break;
         }
     }
-    const int64_t one = std::max<int64_t>(1, (int64_t)a.B * a.T * rt::rope_places(a)), want = 256 * 16 * 64;
+    const int64_t one = std::max<int64_t>(1, (int64_t)a.B * a.T * rt::rope_places(a)), want = 256 * 32 * 64;
     const int64_t groups = std::min(ceil_div(want, one), ceil_div(a.H, rt::kRopeAhead));
     a.each = (int32_t)(ceil_div(ceil_div(a.H, groups), rt::kRopeAhead) * rt::kRopeAhead);
     a.groups = (int32_t)ceil_div(a.H, a.each);

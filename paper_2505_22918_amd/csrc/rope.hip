@@ -104,22 +104,25 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
         at0 = item * VEC;
         p0 = at0 / 2;
     }
+    const int h0 = g * a.each, h1 = h0 + a.each < a.H ? h0 + a.each : a.H;
+    const int64_t xat = b * a.xs[0] + t * a.xs[2], yat = b * a.ys[0] + t * a.ys[2];
+    Piece<TYPE, VEC> x[kRopeAhead], x2[kRopeAhead];
+    auto ask = [&](int h) {
+#pragma unroll
+        for (int u = 0; u < kRopeAhead; ++u) {
+            const int64_t from = xat + (h + u < h1 ? h + u : h1 - 1) * a.xs[1];
+            x[u].load(a.x, from + at0);
+            if (two) x2[u].load(a.x, from + at1);
+        }
+    };
+    ask(h0);
     float c[NP], s[NP];
     if (!TWO || two) {
 #pragma unroll
         for (int p = 0; p < NP; ++p)
             if (TWO || p0 + p < a.pairs) turn_of(a, row, p0 + p, c[p], s[p]);
     }
-    const int h0 = g * a.each, h1 = h0 + a.each < a.H ? h0 + a.each : a.H;
-    const int64_t xat = b * a.xs[0] + t * a.xs[2], yat = b * a.ys[0] + t * a.ys[2];
     for (int h = h0; h < h1; h += kRopeAhead) {
-        Piece<TYPE, VEC> x[kRopeAhead], x2[kRopeAhead];
-#pragma unroll
-        for (int u = 0; u < kRopeAhead; ++u) {
-            const int64_t from = xat + (h + u < h1 ? h + u : h) * a.xs[1];
-            x[u].load(a.x, from + at0);
-            if (two) x2[u].load(a.x, from + at1);
-        }
 #pragma unroll
         for (int u = 0; u < kRopeAhead; ++u) {
             if (h + u >= h1) break;
@@ -146,6 +149,7 @@ __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
             }
             x[u].store(a.y, to + at0);
         }
+        if (h + kRopeAhead < h1) ask(h + kRopeAhead);
     }
 }
 
