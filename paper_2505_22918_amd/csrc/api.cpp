@@ -1194,7 +1194,7 @@ DiffPlan diff_plan(const rt_diff_dims& d) {
     int64_t best = INT64_MAX;
     for (int by_keys = 0; by_keys < 2; ++by_keys) {
         const int64_t n = bh * ceil_div(d.Tq, by_keys ? 32 : rt::kDiffRows), slots = by_keys ? 256 : 512;
-        for (int64_t s = 1; s <= 32; ++s) {
+        for (int64_t s = 1; s <= rt::kDiffParts; ++s) {
             if (s > 1 && (n * s > 2 * slots || chunks < (by_keys ? 8 : 4) * s)) break;
             // tenths of microseconds: of a chunk in a wave alone on its SIMD, or one of two; of a workgroup's start and end
             const int64_t each = by_keys ? ceil_div(chunks, 4 * s) * 12 + 50 : ceil_div(chunks, s) * (n * s <= 256 ? 11 : 15) + 40;
@@ -1320,8 +1320,8 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
         RT_TRY(check_stat(row_max, "row_max"));
         RT_TRY(check_stat(row_sum, "row_sum"));
     }
-    const int64_t need = diff_workspace(dims);
     const DiffPlan plan = diff_plan(dims);
+    const int64_t need = diff_workspace(dims);
     a.split = plan.split;
     const void* ws = a.split > 1 ? workspace : nullptr;
     if (a.split > 1) {

@@ -286,8 +286,9 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     const int bh = head_of(a, head), b = bh / a.H;
     const int row0 = (item - head * n_tile) * ROWS + (KEYS ? 0 : wave * 32);
     const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
-    const int first_stage = (SPLIT ? (int)((int64_t)n_st * part / a.split) : 0) + (KEYS ? wave : 0);
-    const int end_stage = SPLIT ? (int)((int64_t)n_st * (part + 1) / a.split) : n_st;
+    // parts are as long for every sample, so that those of short ones cost little
+    const int per = SPLIT ? ((a.Tk + BS - 1) / BS + a.split - 1) / a.split : n_st;
+    const int first_stage = part * per + (KEYS ? wave : 0), end_stage = SPLIT && part * per + per < n_st ? part * per + per : n_st;
 
     R ring;
     ring.init(lds, a.k + (size_t)(2 * bh) * a.Tk * D, a.k + (size_t)(2 * bh + 1) * a.Tk * D, a.v + (size_t)bh * a.Tk * (2 * D), keys);
@@ -563,41 +564,57 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     }
 }
 
-// A query row of split walks: D / 2 threads, 4 elements of both maps each
+// A query row of split walks to a workgroup: D / 2 threads take 4 elements each of every EACH-th part
 template <int D>
-__global__ __launch_bounds__(256) void diff_join(DiffArgs a, int64_t rows) {
+__global__ __launch_bounds__(256) void diff_join(DiffArgs a) {
     constexpr int LANES = D / 2, EACH = 256 / LANES;
-    const int g = threadIdx.x / LANES, j = (threadIdx.x - g * LANES) * 4;
-    const int64_t i = (int64_t)blockIdx.x * EACH + g;
-    if (g >= EACH || i >= rows) return;
-    const int64_t bh = i / a.Tq, row = i - bh * a.Tq;
-    const float* stats = a.part + (size_t)a.n_bh * a.split * 2 * a.Tq * (2 * D);
+    __shared__ float stat[2][kDiffParts][3];
+    __shared__ f32x4 sums[2][EACH][LANES];
+    const int64_t bh = blockIdx.x / a.Tq, row = blockIdx.x - bh * a.Tq;
+    auto at = [&](int map, int p) { return ((bh * a.split + p) * 2 + map) * (size_t)a.Tq + row; };
+    if ((int)threadIdx.x < 2 * a.split) {
+        const int map = threadIdx.x & 1, p = threadIdx.x >> 1;
+        const float* x = a.part + (size_t)a.n_bh * a.split * 2 * a.Tq * (2 * D) + at(map, p) * 3;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) stat[map][p][i] = x[i];
+    }
+    __syncthreads();
+    const int g = threadIdx.x / LANES, j = threadIdx.x - g * LANES;
+    float m[2], top[2], l[2];
+#pragma unroll
+    for (int map = 0; map < 2; ++map) {
+        m[map] = top[map] = -INFINITY;
+        l[map] = 0.f;
+        for (int p = 0; p < a.split; ++p) {
+            m[map] = fmaxf(m[map], stat[map][p][0]);
+            top[map] = fmaxf(top[map], stat[map][p][2]);
+        }
+        auto factor = [&](int p) { return __builtin_amdgcn_exp2f((stat[map][p][0] - m[map]) * a.scale_log2); };
+        for (int p = 0; p < a.split; ++p) l[map] = __builtin_fmaf(factor(p), stat[map][p][1], l[map]);
+        if (g < EACH) {
+            f32x4 s = {};
+#pragma unroll 4
+            for (int p = g; p < a.split; p += EACH) s += *reinterpret_cast<const f32x4*>(a.part + at(map, p) * (2 * D) + 4 * j) * factor(p);
+            sums[map][g][j] = s;
+        }
+    }
+    __syncthreads();
+    if (g > 0) return;
     f32x4 o[2];
 #pragma unroll
     for (int map = 0; map < 2; ++map) {
-        auto at = [&](int p) { return ((bh * a.split + p) * 2 + map) * (size_t)a.Tq + row; };
-        float m = -INFINITY, top = -INFINITY, l = 0.f;
-#pragma unroll 4
-        for (int p = 0; p < a.split; ++p) {
-            m = fmaxf(m, stats[at(p) * 3]);
-            top = fmaxf(top, stats[at(p) * 3 + 2]);
-        }
-        f32x4 s = {};
-#pragma unroll 4
-        for (int p = 0; p < a.split; ++p) {
-            const float f = __builtin_amdgcn_exp2f((stats[at(p) * 3] - m) * a.scale_log2);
-            l = __builtin_fmaf(f, stats[at(p) * 3 + 1], l);
-            s += *reinterpret_cast<const f32x4*>(a.part + at(p) * (2 * D) + j) * f;
-        }
-        o[map] = s * (l == 0.f ? 0.f : 1.0f / l);
+        o[map] = f32x4{};
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) o[map] += sums[map][i][j];
+        o[map] *= l[map] == 0.f ? 0.f : 1.0f / l[map];
         if (a.row_max && j == 0) {
             const size_t to = (size_t)(2 * bh + map) * a.Tq + row;
-            a.row_max[to] = top * a.scale_nat;
-            a.row_sum[to] = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f((m - top) * a.scale_log2);
+            a.row_max[to] = top[map] * a.scale_nat;
+            a.row_sum[to] = l[map] == 0.f ? 0.f : l[map] * __builtin_amdgcn_exp2f((m[map] - top[map]) * a.scale_log2);
         }
     }
     const f32x4 d = o[0] - o[1] * a.lam[(bh % a.H) * a.lam_step];
-    const size_t to = (size_t)i * (2 * D) + j;
+    const size_t to = (size_t)blockIdx.x * (2 * D) + 4 * j;
     reinterpret_cast<uint32_t*>(a.o + to)[0] = pack_bf16(d[0], d[1]);
     reinterpret_cast<uint32_t*>(a.o + to)[1] = pack_bf16(d[2], d[3]);
     if (a.o2) {
@@ -613,9 +630,7 @@ hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((diff_fwd<D, KEYS, STATS, SPLIT>), dim3(8 * per), dim3(256), 0, stream, a, n, per);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !SPLIT) return e;
-    constexpr int EACH = 256 / (D / 2);
-    const int64_t rows = (int64_t)a.n_bh * a.Tq;
-    hipLaunchKernelGGL((diff_join<D>), dim3((uint32_t)((rows + EACH - 1) / EACH)), dim3(256), 0, stream, a, rows);
+    hipLaunchKernelGGL((diff_join<D>), dim3(a.n_bh * a.Tq), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 template <int D, bool KEYS>
@@ -720,7 +735,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     int n_st = (x_end + BS - 1) / BS;
     if (KV && tile0 >= keys) n_st = 0;  // keys that the sample does not have
     const int split = KV ? a.split_k : a.split_q;
-    const int s0 = SPLIT ? (int)((int64_t)n_st * part / split) : 0, s1 = SPLIT ? (int)((int64_t)n_st * (part + 1) / split) : n_st;
+    const int per = SPLIT ? ((Tx + BS - 1) / BS + split - 1) / split : n_st;
+    const int s0 = part * per, s1 = SPLIT && s0 + per < n_st ? s0 + per : n_st;
 
     const size_t n_x = (size_t)(2 * bh) * Tx * D, n_own = (size_t)(2 * bh) * T * D;
     const size_t w_x = (size_t)bh * Tx * (2 * D), w_own = (size_t)bh * T * (2 * D);

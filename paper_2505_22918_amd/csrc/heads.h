@@ -33,6 +33,7 @@ inline int64_t rope_blocks(const RopeArgs& a) { return (int64_t)a.B * a.groups *
 __attribute__((weak)) hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 
 constexpr int kDiffRows = 128;  // rows of a tile of four waves
+constexpr int kDiffParts = 32;  // parts of a tile's keys, at most
 struct DiffArgs {
     const uint16_t* q;  // bf16 [B, 2 H, Tq, D]
     const uint16_t* k;  // bf16 [B, 2 H, Tk, D]
