@@ -6,6 +6,7 @@
 //   dV = (P_1 - lam P_2)^T dO,  dQ_i = dS_i K_i / sqrt(D),  dK_i = dS_i^T Q_i / sqrt(D),  dlam = -sum of delta_2
 //
 //   diff_fwd    32 queries of both maps to a wave: one pass over the keys, V read once for both
+//   diff_few    the same for up to 16 queries, the maps side by side in a product's columns
 //   diff_join   the parts of split walks
 //   diff_rows   per query row: log2 of both denominators, -delta_2, delta_2 - delta_1
 //   diff_bwd    dK_1, dK_2 and dV of 128 keys, or dQ_1 and dQ_2 of 128 queries, to a workgroup of four waves; dlam
@@ -564,6 +565,223 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     }
 }
 
+// Up to 16 queries of a head, as diff_fwd's KEYS: map 1's in columns 0 .. 15 of the 32x32 products, map 2's in the others,
+// so that a chunk takes one softmax and V's products once (16 matrix products and 16 exponentials a lane instead of 24 and
+// 32).  Both maps' scores come out of one accumulator: the operand of a map's queries is zero in the other's columns, where
+// a key that is not finite in one map makes the other's statistics NaN (its output is NaN either way).
+template <int D, bool STATS, bool SPLIT>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_few(DiffArgs a, int n_items, int per_xcd) {
+    constexpr int BS = 32, STEP = 4;
+    using R = DiffRing<D, 1, BS, false>;
+    constexpr int NB = R::NB;
+    constexpr bool TAIL = D == 72;
+    constexpr int STAT = 4 * R::LDS;  // [wave][column] of the running max, the sum and the true max
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[STAT + 4 * 32 * 12];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lds_u8* const all = (lds_u8*)smem;
+    lds_u8* const lds = all + wave * R::LDS;
+
+    int item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), part = 0;
+    if (item >= n_items) return;
+    if (SPLIT) {
+        part = item % a.split;
+        item /= a.split;
+    }
+    const int bh = head_of(a, item), b = bh / a.H;
+    const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
+    const int per = SPLIT ? ((a.Tk + BS - 1) / BS + a.split - 1) / a.split : n_st;
+    const int first_stage = part * per + wave, end_stage = SPLIT && part * per + per < n_st ? part * per + per : n_st;
+
+    R ring;
+    ring.init(lds, a.k + (size_t)(2 * bh) * a.Tk * D, a.k + (size_t)(2 * bh + 1) * a.Tk * D, a.v + (size_t)bh * a.Tk * (2 * D), keys);
+    ring.load(0, first_stage * BS);
+    Reads<D> rd;
+    rd.init(lds);
+    const int map = rd.l32 >> 4, row = rd.l32 & 15;
+    bf16x8 q[2][4], q_tail[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)(a.q + (size_t)(2 * bh + i) * a.Tq * D), (short)0, a.Tq * NB, 0x00020000);
+        const int off = map == i ? row * NB : kOob;
+        auto load = [&](int o) { return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rs, o, 0, 0)); };
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[i][k] = load(off + 32 * k + 16 * rd.hi);
+        if (TAIL) q_tail[i] = load(rd.hi ? kOob : off + 128);
+    }
+    f32x16 acc[4];
+    f32x4 tacc[2];  // of map 1 and of map 2
+#pragma unroll
+    for (int d = 0; d < 4; ++d) acc[d] = f32x16{};
+    tacc[0] = tacc[1] = f32x4{};
+    float m_run = -1e30f, m_top = -INFINITY, l_run = 0.f;
+    // a value of each column as the tails' accumulators hold them: query lane % 16 of map i
+    auto tail_bcast = [&](float x, int i) { return __int_as_float(__builtin_amdgcn_ds_bpermute((16 * i + (rd.lane & 15)) << 2, __float_as_int(x))); };
+    const float c2 = a.scale_log2;
+    int st = 0;
+    for (int s = first_stage; s < end_stage; s += STEP) {
+        ring.turn();
+        ring.load(R::STAGE - st, (s + STEP) * BS);
+        const int cv = st + R::WIDE;
+        f32x16 sc = {};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sc = mma(rd.n_row(st + i * R::NT, k), q[i][k], sc);
+            if (TAIL) sc = mma(rd.n_row_tail(st + i * R::NT, R::ZERO), q_tail[i], sc);
+        }
+        if ((s + 1) * BS > keys) {
+            const int lim = keys - s * BS - 4 * rd.hi;
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+                if (8 * (x >> 2) + (x & 3) >= lim) sc[x] = -INFINITY;
+        }
+        float top = fmaxf(fmaxf(sc[0], sc[1]), sc[2]);
+#pragma unroll
+        for (int x = 3; x < 15; x += 2) top = fmaxf(fmaxf(top, sc[x]), sc[x + 1]);
+        top = fmaxf(top, sc[15]);
+        if (STATS) m_top = fmaxf(m_top, top);
+        if (__builtin_amdgcn_ballot_w64((top - m_run) * c2 > kMove)) {
+            const float to = fmaxf(m_run, pair_max(top));
+            const float alpha = __builtin_amdgcn_exp2f((m_run - to) * c2);
+            m_run = to;
+            l_run *= alpha;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) acc[d] *= alpha;
+            if (TAIL) {
+                tacc[0] *= tail_bcast(alpha, 0);
+                tacc[1] *= tail_bcast(alpha, 1);
+            }
+        }
+        const float mc = m_run * c2;
+        float sum[2] = {0.f, 0.f};
+        uint32_t pk[8];
+#pragma unroll
+        for (int x = 0; x < 16; x += 2) {
+            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -mc));
+            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -mc));
+            sum[(x >> 1) & 1] += e0 + e1;
+            pk[x / 2] = pack_bf16(e0, e1);
+        }
+        l_run += sum[0] + sum[1];
+#pragma unroll
+        for (int p = 0; p < 8; ++p) acc[p & 3] = mma(rd.w_col(cv, p & 3, p >> 2), op(pk, p >> 2), acc[p & 3]);
+        if (TAIL) {
+            const bf16x8 v = rd.w_col_tail(cv);
+            uint32_t y[8];
+            halves(pk, y);
+            tacc[0] = mma16(v, op(y, 0), tacc[0]);
+            tacc[1] = mma16(v, op(y, 1), tacc[1]);
+        }
+        st = R::STAGE - st;
+    }
+    wait_vm<0>();  // nothing may land in LDS after the workgroup has ended
+
+    // the waves' sums against the largest running max, each in its own ring's place, then a tile of 32 elements to a wave
+    l_run = pair_sum(l_run);
+    if (STATS) m_top = pair_max(m_top);
+    auto stat = [&](int w) { return (lds_f32*)(all + STAT) + (w * 32 + rd.l32) * 3; };
+    if (rd.hi == 0) {
+        stat(wave)[0] = m_run;
+        stat(wave)[1] = l_run;
+        stat(wave)[2] = m_top;
+    }
+    __syncthreads();
+    float m = -INFINITY, l = 0.f;
+    m_top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        m = fmaxf(m, stat(w)[0]);
+        m_top = fmaxf(m_top, stat(w)[2]);
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w) l = __builtin_fmaf(__builtin_amdgcn_exp2f((stat(w)[0] - m) * c2), stat(w)[1], l);
+    const float f = __builtin_amdgcn_exp2f((m_run - m) * c2);
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            *(lds_f32x4*)(lds + (d * 4 + u) * 1024 + rd.lane * 16) =
+                f32x4{acc[d][4 * u] * f, acc[d][4 * u + 1] * f, acc[d][4 * u + 2] * f, acc[d][4 * u + 3] * f};
+    if (TAIL) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *(lds_f32x4*)(lds + 16384 + i * 1024 + rd.lane * 16) = tacc[i] * tail_bcast(f, i);
+    }
+    __syncthreads();
+    float inv = l == 0.f ? 0.f : 1.0f / l;  // no keys: 0
+    f32x4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        x[u] = f32x4{};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) x[u] += *(const lds_f32x4*)(all + w * R::LDS + (wave * 4 + u) * 1024 + rd.lane * 16);
+    }
+    if (TAIL && wave == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            tacc[i] = f32x4{};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) tacc[i] += *(const lds_f32x4*)(all + w * R::LDS + 16384 + i * 1024 + rd.lane * 16);
+        }
+    }
+    const int col = 32 * wave + 16 * rd.hi;
+    if (SPLIT) {
+        if (row < a.Tq) {
+            const size_t at = ((size_t)bh * a.split + part) * 2 + map;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) *reinterpret_cast<f32x4*>(a.part + (at * a.Tq + row) * (2 * D) + col + 4 * u) = x[u];
+            if (wave == 0 && rd.hi == 0) {
+                float* y = a.part + (size_t)a.n_bh * a.split * 2 * a.Tq * (2 * D) + (at * a.Tq + row) * 3;
+                y[0] = m;
+                y[1] = l;
+                y[2] = STATS ? m_top : 0.f;
+            }
+        }
+        if (TAIL && wave == 0 && (rd.lane & 15) < a.Tq) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *reinterpret_cast<f32x4*>(a.part + ((((size_t)bh * a.split + part) * 2 + i) * a.Tq + (rd.lane & 15)) * (2 * D) + 128 + 4 * (rd.lane >> 4)) = tacc[i];
+        }
+        return;
+    }
+    if (STATS && wave == 0 && rd.hi == 0 && row < a.Tq) {
+        const size_t at = (size_t)(2 * bh + map) * a.Tq + row;
+        a.row_max[at] = m_top * a.scale_nat;
+        a.row_sum[at] = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f((m - m_top) * c2);
+    }
+    const float lam = a.lam[(bh - b * a.H) * a.lam_step];
+    // the maps' values of a query from the lanes of both: map 1's lanes write o, map 2's o2
+    uint32_t out[8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t v = __float_as_uint(x[u][e] * inv);
+            auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+            y[e] = map ? __uint_as_float(r[1]) : __builtin_fmaf(-lam, __uint_as_float(r[1]), __uint_as_float(r[0]));
+        }
+        out[2 * u] = pack_bf16(y[0], y[1]);
+        out[2 * u + 1] = pack_bf16(y[2], y[3]);
+    }
+    if (row < a.Tq && (STATS || map == 0)) {
+        uint16_t* const to = (map ? a.o2 : a.o) + ((size_t)bh * a.Tq + row) * (2 * D) + col;
+        *reinterpret_cast<u32x4*>(to) = u32x4{out[0], out[1], out[2], out[3]};
+        *reinterpret_cast<u32x4*>(to + 8) = u32x4{out[4], out[5], out[6], out[7]};
+    }
+    if (TAIL && wave == 0) {
+        const float i0 = tail_bcast(inv, 0), i1 = tail_bcast(inv, 1);
+        if ((rd.lane & 15) < a.Tq) {
+            const size_t at = ((size_t)bh * a.Tq + (rd.lane & 15)) * (2 * D) + 128 + 4 * (rd.lane >> 4);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float b0 = tacc[1][2 * e] * i1, b1 = tacc[1][2 * e + 1] * i1;
+                reinterpret_cast<uint32_t*>(a.o + at)[e] = pack_bf16(__builtin_fmaf(-lam, b0, tacc[0][2 * e] * i0), __builtin_fmaf(-lam, b1, tacc[0][2 * e + 1] * i0));
+                if (STATS) reinterpret_cast<uint32_t*>(a.o2 + at)[e] = pack_bf16(b0, b1);
+            }
+        }
+    }
+}
+
 // A query row of split walks to a workgroup: D / 2 threads take 4 elements each of every EACH-th part
 template <int D>
 __global__ __launch_bounds__(256) void diff_join(DiffArgs a) {
@@ -623,24 +841,23 @@ __global__ __launch_bounds__(256) void diff_join(DiffArgs a) {
     }
 }
 
-template <int D, bool KEYS, bool STATS, bool SPLIT>
+template <int D, bool STATS, bool SPLIT>
 hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream) {
-    constexpr int ROWS = KEYS ? 32 : kDiffRows;
-    const int n = a.n_bh * ((a.Tq + ROWS - 1) / ROWS) * (SPLIT ? a.split : 1), per = (n + 7) / 8;
-    hipLaunchKernelGGL((diff_fwd<D, KEYS, STATS, SPLIT>), dim3(8 * per), dim3(256), 0, stream, a, n, per);
-    const hipError_t e = hipGetLastError();
+    auto run = [&](auto kernel, int rows) {
+        const int n = a.n_bh * ((a.Tq + rows - 1) / rows) * (SPLIT ? a.split : 1), per = (n + 7) / 8;
+        hipLaunchKernelGGL(kernel, dim3(8 * per), dim3(256), 0, stream, a, n, per);
+        return hipGetLastError();
+    };
+    const hipError_t e = !a.by_keys ? run(diff_fwd<D, false, STATS, SPLIT>, kDiffRows)
+                                    : (a.Tq <= 16 ? run(diff_few<D, STATS, SPLIT>, 16) : run(diff_fwd<D, true, STATS, SPLIT>, 32));
     if (e != hipSuccess || !SPLIT) return e;
     hipLaunchKernelGGL((diff_join<D>), dim3(a.n_bh * a.Tq), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
-template <int D, bool KEYS>
-hipError_t launch_fwd_k(const DiffArgs& a, hipStream_t stream) {
-    if (a.split > 1) return a.o2 ? launch_fwd<D, KEYS, true, true>(a, stream) : launch_fwd<D, KEYS, false, true>(a, stream);
-    return a.o2 ? launch_fwd<D, KEYS, true, false>(a, stream) : launch_fwd<D, KEYS, false, false>(a, stream);
-}
 template <int D>
 hipError_t launch_fwd_d(const DiffArgs& a, hipStream_t stream) {
-    return a.by_keys ? launch_fwd_k<D, true>(a, stream) : launch_fwd_k<D, false>(a, stream);
+    if (a.split > 1) return a.o2 ? launch_fwd<D, true, true>(a, stream) : launch_fwd<D, false, true>(a, stream);
+    return a.o2 ? launch_fwd<D, true, false>(a, stream) : launch_fwd<D, false, false>(a, stream);
 }
 
 // ---- backward ------------------------------------------------------------------------------

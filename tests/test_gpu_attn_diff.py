@@ -70,7 +70,7 @@ def _lens(lens):
     return None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
 
 
-SIZES = [(1, 1, 1, 1), (1, 1, 1, 2), (2, 1, 32, 32), (1, 2, 33, 31), (1, 1, 64, 65), (2, 2, 127, 63), (1, 1, 128, 200), (1, 3, 129, 129),
+SIZES = [(1, 1, 1, 1), (1, 1, 1, 2), (2, 3, 1, 300), (1, 2, 15, 2000), (1, 1, 16, 33), (2, 1, 17, 700), (2, 1, 32, 32), (1, 2, 33, 31), (1, 1, 64, 65), (2, 2, 127, 63), (1, 1, 128, 200), (1, 3, 129, 129),
          (1, 1, 300, 1), (1, 1, 5, 700), (1, 2, 700, 5), (1, 1, 257, 1100)]
 
 
@@ -89,7 +89,7 @@ def test_sizes(gpu, B, H, Tq, Tk, D):
 
 
 @pytest.mark.parametrize("D", [64, 72])
-@pytest.mark.parametrize("Tq,Tk,lens", [(40, 100, [100, 37, 0, 1]), (1, 500, [500, 33, 0, 256]), (200, 130, [64, 128, 129, 0]),
+@pytest.mark.parametrize("Tq,Tk,lens", [(40, 100, [100, 37, 0, 1]), (1, 500, [500, 33, 0, 256]), (16, 3000, [3000, 1, 0, 1700]), (9, 130, [130, 97, 0, 64]), (200, 130, [64, 128, 129, 0]),
                                         (300, 700, [700, 5, 0, 333]), (7, 65, [-3, 99, 64, 65])])
 def test_padded_keys(gpu, Tq, Tk, lens, D):
     import torch
@@ -115,9 +115,10 @@ def test_padded_keys(gpu, Tq, Tk, lens, D):
 
 
 @pytest.mark.parametrize("D", [64, 72])
-def test_running_max_moves(gpu, D):
+@pytest.mark.parametrize("Tq", [5, 70, 300])
+def test_running_max_moves(gpu, Tq, D):
     # scores that rise by hundreds from tile to tile, fall again, and lie far below zero
-    q, k, v, do, lam = _inputs(1, 1, 70, 400, D, 9)
+    q, k, v, do, lam = _inputs(1, 1, Tq, 400, D, 9)
     import torch
 
     ramp = torch.linspace(-40, 60, 400, device="cuda")
@@ -234,15 +235,15 @@ def test_given_outputs_and_their_neighbours(gpu):
 def test_non_finite_rows_stay_in_their_row(gpu):
     import torch
 
-    for D in (64, 72):
-        q, k, v, _, lam = _inputs(1, 1, 70, 90, D, 16)
+    for D, Tq, bad in ((64, 70, (5, 40)), (72, 70, (5, 40)), (64, 11, (3, 9)), (72, 11, (3, 9)), (72, 900, (300, 301))):
+        q, k, v, _, lam = _inputs(1, 1, Tq, 90, D, 16)
         want = rt.attn_diff(q, k, v, lam)
-        q[0, 0, 5, 3], q[0, 1, 40, 60] = float("nan"), float("inf")
+        q[0, 0, bad[0], 3], q[0, 1, bad[1], 60] = float("nan"), float("inf")
         got = rt.attn_diff(q, k, v, lam)
-        rows = [r for r in range(70) if r not in (5, 40)]
+        rows = [r for r in range(Tq) if r not in bad]
         for x, y in zip(got, want):
             assert torch.equal(x[:, :, rows], y[:, :, rows])
-        assert bool(torch.isnan(got[0][0, 0, [5, 40]]).all())
+        assert bool(torch.isnan(got[0][0, 0, list(bad)]).all())
 
 
 def test_graphs_share_inputs_not_workspaces(gpu):
