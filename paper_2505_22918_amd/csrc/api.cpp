@@ -1192,7 +1192,8 @@ DiffPlan diff_plan(const rt_diff_dims& d) {
     const int64_t bh = (int64_t)d.B * d.H, chunks = ceil_div(d.Tk, 32);
     DiffPlan p{0, 1};
     int64_t best = INT64_MAX;
-    for (int by_keys = 0; by_keys < 2; ++by_keys) {
+    // (of 32 queries, a tile of four waves would keep one busy)
+    for (int by_keys = d.Tq <= 32 && chunks > 4; by_keys < 2; ++by_keys) {
         const int64_t n = bh * ceil_div(d.Tq, by_keys ? 32 : rt::kDiffRows), slots = by_keys ? 256 : 512;
         for (int64_t s = 1; s <= rt::kDiffParts; ++s) {
             if (s > 1 && (n * s > 2 * slots || chunks < (by_keys ? 8 : 4) * s)) break;
@@ -1237,8 +1238,9 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d) {
     // half microseconds: of a walk's chunks of 32 rows, two waves to a SIMD
     const int64_t wk = 4 * ceil_div(d.Tq, 32), wq = 3 * ceil_div(d.Tk, 32);
     int64_t best = INT64_MAX;
-    for (int two = 0; two < 2; ++two) {
-        for (int i = 1; i <= 16; ++i) {
+    const bool many = nk + nq > 4096;  // tiles enough: a walk each, four waves
+    for (int two = 0; two < (many ? 1 : 2); ++two) {
+        for (int i = 1; i <= (many ? 1 : 16); ++i) {
             const int64_t part = ceil_div(std::max(wk, wq), i);
             const int64_t sk = std::max<int64_t>(1, ceil_div(wk, std::max<int64_t>(part, 1))), sq = std::max<int64_t>(1, ceil_div(wq, std::max<int64_t>(part, 1)));
             if (i > 1 && part < 16) break;
@@ -1250,7 +1252,6 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d) {
                 best = t;
                 p = DiffBackPlan{two, (int32_t)sk, (int32_t)sq};
             }
-            if (nk + nq > 4096) break;  // tiles enough
         }
     }
     return p;
