@@ -1184,7 +1184,11 @@ DiffBytes diff_bytes(const rt_diff_dims& d, int32_t n_lam) {
             (int64_t)d.B * 4};
 }
 
-// Forward: whether a workgroup's waves share the keys of 32 queries, and workgroups that share a tile's keys.
+// Forward: whether a workgroup's waves share the keys of 32 queries, and workgroups that share a tile's keys, by an
+// estimate of the times.  Sharing keys starts four times as many workgroups, one to a CU, and reads the keys four times
+// as often: 30 heads of 512 tokens 22 us against 36 of tiles of 128 in parts, 15 heads of 1500 tokens 51 against 65; but
+// 16 heads of 1024 queries over 226 keys 20 against 17.5, 4 heads of 3000 tokens 81 against 67.  Parts cost their sums'
+// way through memory: one head of 4096 tokens 32 us in two parts, 58 in eight.
 struct DiffPlan {
     int32_t by_keys, split;
 };
@@ -1227,7 +1231,12 @@ int64_t finish(int64_t n1, int64_t l1, int64_t n2, int64_t l2, int64_t slots) {
     return t + ceil_div(n2, slots) * l2;
 }
 
-// Backward: whether eight waves take a tile, and workgroups that share the walk of a tile of keys, of queries.
+// Backward: whether eight waves take a tile, and workgroups that share the walk of a tile of keys, of queries, by an
+// estimate of when the last workgroup ends.  Eight waves to a tile, two to a SIMD where there is a tile to a CU: 16 heads
+// of 1024 tokens, 72 wide, 60 us against 73, one head of 4096 56 against 62; but 15 heads of 1500 tokens 100 against 84.
+// Parts, of either side's walks: 15 heads of 2734 queries over 1175 keys and fewer 137 -> 97 us, 32 heads of 4096 queries
+// over 226 keys and fewer 283 -> 103 (their dK and dV are 64 tiles of 128 chunks each), the other way round (200 queries
+// over 6000 keys) 104 -> 34.
 struct DiffBackPlan {
     int32_t two, split_k, split_q;
 };
