@@ -265,6 +265,17 @@ __device__ __forceinline__ int keys_of(const DiffArgs& a, int b) {
 
 // ---- forward -------------------------------------------------------------------------------
 
+// the part of a tile's rows for which a sample has no keys: its statistics alone, by which diff_join leaves the sums out
+template <int D>
+__device__ __forceinline__ void empty_part(const DiffArgs& a, int bh, int part, int row0, int rows) {
+    const int map = threadIdx.x & 1, row = row0 + (threadIdx.x >> 1);
+    if ((int)threadIdx.x >= 2 * rows || row >= a.Tq) return;
+    float* x = a.part + (size_t)a.n_bh * a.split * 2 * a.Tq * (2 * D) + ((((size_t)bh * a.split + part) * 2 + map) * a.Tq + row) * 3;
+    x[0] = -1e30f;
+    x[1] = 0.f;
+    x[2] = -INFINITY;
+}
+
 constexpr float kMove = 24.0f;  // the running max moves when a probability against it passes 2^kMove
 
 // A workgroup of four waves takes 32 queries to a wave, which share a ring of keys and values; or (KEYS, where there are
@@ -297,6 +308,10 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     // parts are as long for every sample, so that those of short ones cost little
     const int per = SPLIT ? ((a.Tk + BS - 1) / BS + a.split - 1) / a.split : n_st;
     const int first_stage = part * per + (KEYS ? wave : 0), end_stage = SPLIT && part * per + per < n_st ? part * per + per : n_st;
+    if (SPLIT && part * per >= n_st) {
+        empty_part<D>(a, bh, part, (item - head * n_tile) * ROWS, ROWS);
+        return;
+    }
 
     R ring;
     ring.init(lds, a.k + (size_t)(2 * bh) * a.Tk * D, a.k + (size_t)(2 * bh + 1) * a.Tk * D, a.v + (size_t)bh * a.Tk * (2 * D), keys);
@@ -598,6 +613,10 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
     const int per = SPLIT ? ((a.Tk + BS - 1) / BS + a.split - 1) / a.split : n_st;
     const int first_stage = part * per + wave, end_stage = SPLIT && part * per + per < n_st ? part * per + per : n_st;
+    if (SPLIT && part * per >= n_st) {
+        empty_part<D>(a, bh, part, 0, 16);
+        return;
+    }
 
     R ring;
     ring.init(lds, a.k + (size_t)(2 * bh) * a.Tk * D, a.k + (size_t)(2 * bh + 1) * a.Tk * D, a.v + (size_t)bh * a.Tk * (2 * D), keys);
@@ -819,7 +838,8 @@ __global__ __launch_bounds__(256) void diff_join(DiffArgs a) {
         if (g < EACH) {
             f32x4 s = {};
 #pragma unroll 4
-            for (int p = g; p < a.split; p += EACH) s += *reinterpret_cast<const f32x4*>(a.part + at(map, p) * (2 * D) + 4 * j) * factor(p);
+            for (int p = g; p < a.split; p += EACH)
+                if (stat[map][p][1] != 0.f) s += *reinterpret_cast<const f32x4*>(a.part + at(map, p) * (2 * D) + 4 * j) * factor(p);
             sums[map][g][j] = s;
         }
     }
@@ -961,6 +981,7 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     const int split = KV ? a.split_k : a.split_q;
     const int per = SPLIT ? ((Tx + BS - 1) / BS + split - 1) / split : n_st;
     const int s0 = part * per, s1 = SPLIT && s0 + per < n_st ? s0 + per : n_st;
+    if (SPLIT && split > 1 && s0 >= n_st) return;  // diff_sum leaves it out
 
     const size_t n_x = (size_t)(2 * bh) * Tx * D, n_own = (size_t)(2 * bh) * T * D;
     const size_t w_x = (size_t)bh * Tx * (2 * D), w_own = (size_t)bh * T * (2 * D);
@@ -1230,9 +1251,9 @@ __global__ __launch_bounds__(TWO ? 512 : 256) __attribute__((amdgpu_waves_per_eu
 }
 
 // Sums of a tile's parts: dK_1, dK_2, the halves of dV (kind 0 .. 3; `tiles_k` of them in x), then dQ_1, dQ_2 (4, 5);
-// blockIdx.y counts from `kind0`
+// blockIdx.y counts from `kind0`; bs_k: rows of a stage of dK and dV's walks
 template <int D>
-__global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int kind0, int tiles_k, int tiles_q) {
+__global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int bs_k, int kind0, int tiles_k, int tiles_q) {
     constexpr int TILE = kDiffRows * D;
     const int kind = kind0 + blockIdx.y;
     const bool kv = kind < 4;
@@ -1253,9 +1274,12 @@ __global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int kind0, int tiles
     const int j = blockIdx.z * 1024 + threadIdx.x * 4;
     const int left = T - row0, size = (left < kDiffRows ? left : kDiffRows) * width;
     if (j >= TILE || skip + j >= size) return;
+    // parts that hold rows of the other side, as diff_walk has them; none for keys that the sample does not have
+    const int keys = keys_of(a, bh / a.H), Tx = kv ? a.Tq : a.Tk, bs = kv ? bs_k : 64, per = ((Tx + bs - 1) / bs + n - 1) / n;
+    const int stages = kv ? (row0 < keys ? (Tx + bs - 1) / bs : 0) : (keys + bs - 1) / bs, full = (stages + per - 1) / per;
     f32x4 s = {};
 #pragma unroll 4
-    for (int p = 0; p < n; ++p) s += *reinterpret_cast<const f32x4*>(part + p * stride + j);
+    for (int p = 0; p < full; ++p) s += *reinterpret_cast<const f32x4*>(part + p * stride + j);
     uint32_t* to = reinterpret_cast<uint32_t*>(out + (size_t)row0 * width + skip + j);
     to[0] = pack_bf16(s[0], s[1]);
     to[1] = pack_bf16(s[2], s[3]);
@@ -1286,7 +1310,7 @@ hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
     if (e != hipSuccess || !split) return e;
     const int sums_k = a.split_k > 1 ? tiles_k : 0, sums_q = a.split_q > 1 ? tiles_q : 0, kind0 = sums_k ? 0 : 4;
     hipLaunchKernelGGL((diff_sum<D>), dim3(most(sums_k, sums_q), (sums_q ? 6 : 4) - kind0, kDiffRows * D / 1024), dim3(256), 0, stream, a,
-                       kind0, sums_k, sums_q);
+                       a.two ? 64 : 32, kind0, sums_k, sums_q);
     return hipGetLastError();
 }
 
