@@ -1238,28 +1238,31 @@ int64_t finish(int64_t n1, int64_t l1, int64_t n2, int64_t l2, int64_t slots) {
 // over 226 keys and fewer 283 -> 103 (their dK and dV are 64 tiles of 128 chunks each), the other way round (200 queries
 // over 6000 keys) 104 -> 34.
 struct DiffBackPlan {
-    int32_t two, split_k, split_q;
+    int32_t two, q_first, split_k, split_q;
 };
 DiffBackPlan diff_back_plan(const rt_diff_dims& d) {
     const int64_t bh = (int64_t)d.B * d.H, nk = bh * ceil_div(d.Tk, rt::kDiffRows), nq = bh * ceil_div(d.Tq, rt::kDiffRows);
-    DiffBackPlan p{0, 1, 1};
+    DiffBackPlan p{0, 0, 1, 1};
     if (nk == 0 || nq == 0) return p;
     // half microseconds: of a walk's chunks of 32 rows, two waves to a SIMD
     const int64_t wk = 4 * ceil_div(d.Tq, 32), wq = 3 * ceil_div(d.Tk, 32);
+    const int64_t longest = std::max(wk, wq);
     int64_t best = INT64_MAX;
-    const bool many = nk + nq > 4096;  // tiles enough: a walk each, four waves
-    for (int two = 0; two < (many ? 1 : 2); ++two) {
-        for (int i = 1; i <= (many ? 1 : 16); ++i) {
-            const int64_t part = ceil_div(std::max(wk, wq), i);
-            const int64_t sk = std::max<int64_t>(1, ceil_div(wk, std::max<int64_t>(part, 1))), sq = std::max<int64_t>(1, ceil_div(wq, std::max<int64_t>(part, 1)));
-            if (i > 1 && part < 16) break;
+    for (int two = 0; two < (nk + nq > 4096 ? 1 : 2); ++two) {
+        for (int i = 1; i <= 16; ++i) {
+            const int64_t part = std::max<int64_t>(1, ceil_div(longest, i));
+            const int64_t sk = std::max<int64_t>(1, ceil_div(wk, part)), sq = std::max<int64_t>(1, ceil_div(wq, part));
+            // the parts in whole tiles of 128 x D; a gigabyte and a half of them at most
+            const int64_t parts = (sk > 1 ? nk * sk * 4 : 0) + (sq > 1 ? nq * sq * 2 : 0);
+            if (i > 1 && (part < 16 || parts > 40000)) break;
             const int64_t lk = ceil_div(wk, sk * (two + 1)) + 20 + 6 * two, lq = ceil_div(wq, sq * (two + 1)) + 20 + 6 * two;
-            int64_t t = finish(nk * sk, lk, nq * sq, lq, two ? 256 : 512);
-            if (sk > 1 || sq > 1)  // the parts, written and read
-                t += 10 + ((sk > 1 ? nk * sk * 4 : 0) + (sq > 1 ? nq * sq * 2 : 0)) * (rt::kDiffRows * 4 * 2) * d.D / 3000000;
+            const int64_t slots = two ? 256 : 512;
+            const bool q_first = lq > lk;  // what takes longer begins first
+            int64_t t = q_first ? finish(nq * sq, lq, nk * sk, lk, slots) : finish(nk * sk, lk, nq * sq, lq, slots);
+            if (parts) t += 10 + parts * (rt::kDiffRows * 4 * 2) * d.D / 3000000;  // written and read
             if (t < best) {
                 best = t;
-                p = DiffBackPlan{two, (int32_t)sk, (int32_t)sq};
+                p = DiffBackPlan{two, q_first, (int32_t)sk, (int32_t)sq};
             }
         }
     }
@@ -1402,6 +1405,7 @@ rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, con
     a.row_vals = static_cast<float*>(workspace);
     const DiffBackPlan plan = diff_back_plan(dims);
     a.two = plan.two;
+    a.q_first = plan.q_first;
     a.split_k = plan.split_k;
     a.split_q = plan.split_q;
     a.part_k = a.row_vals + diff_vals(dims);

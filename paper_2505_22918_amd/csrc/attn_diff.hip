@@ -1234,9 +1234,10 @@ __global__ __launch_bounds__(TWO ? 512 : 256) __attribute__((amdgpu_waves_per_eu
         return;
     }
     g -= lam8;
-    // dK and dV first, which have more to do
-    const bool kv = g < 8 * per_k;
-    if (!kv) g -= 8 * per_k;
+    // what takes longer first
+    const int ahead = 8 * (a.q_first ? per_q : per_k);
+    const bool kv = (g < ahead) != (a.q_first != 0);
+    if (g >= ahead) g -= ahead;
     const int split = kv ? a.split_k : a.split_q;
     int item = (g & 7) * (kv ? per_k : per_q) + (g >> 3), part = 0;
     if (item >= (kv ? n_k : n_q)) return;

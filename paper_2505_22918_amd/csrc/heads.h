@@ -59,6 +59,7 @@ struct DiffArgs {
     float* d_lam;
     float* row_vals;  // workspace [B, H][4][T64]
     int32_t T64;      // Tq in whole 64
+    int32_t q_first;  // tiles of queries before those of keys
     int32_t two;      // eight waves to a tile, four of them for each half of a stage
     int32_t split_k, split_q;  // workgroups that share the walk of a tile of keys, of queries
     float* part_k;    // workspace of split walks
