@@ -1004,8 +1004,8 @@ def attn_diff(q, k, v, lam, k_lens=None, stats=True, out=None):
         o2 = q.new_empty(shape)
         m = lam.new_empty(rows)
         l = lam.new_empty(rows)
-    if need > 16:  # keys in parts
-        work = _workspace(need, q)
+    if need > 16:  # keys in parts; it returns to torch's stream-ordered cache after the call
+        work = lam.new_empty(need >> 2)
     with _on(q):
         status = lib.rt_attn_diff(q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), lam.numel(), _ptr(k_lens), dims,
                                   o.data_ptr(), _ptr(o2), _ptr(m), _ptr(l), _ptr(work), need, _stream(q))
@@ -1022,11 +1022,19 @@ def attn_diff_backward(q, k, v, o, o2, row_max, row_sum, d_o, lam, k_lens=None, 
     torch = _torch()
     lib = _lib.load()
     dims, shape, rows, _, need = _diff_inputs(q, k, v, lam, k_lens)
-    for name, t in (("o", o), ("o2", o2), ("d_o", d_o)):
-        if not _same(t, torch.bfloat16, shape, q):
+    bf16, fp32, at = torch.bfloat16, torch.float32, q.get_device()
+    try:  # one expression for the usual case; anything else is named below
+        fine = (o.dtype is bf16 and o2.dtype is bf16 and d_o.dtype is bf16 and row_max.dtype is fp32 and row_sum.dtype is fp32
+                and o.shape == shape and o2.shape == shape and d_o.shape == shape and row_max.shape == rows
+                and row_sum.shape == rows and o.is_contiguous() and o2.is_contiguous() and d_o.is_contiguous()
+                and row_max.is_contiguous() and row_sum.is_contiguous() and o.get_device() == at and o2.get_device() == at
+                and d_o.get_device() == at and row_max.get_device() == at and row_sum.get_device() == at)
+    except (AttributeError, TypeError):
+        fine = False
+    if not fine:
+        for name, t in (("o", o), ("o2", o2), ("d_o", d_o)):
             _bf16(t, shape, name, q.device)
-    for name, t in (("row_max", row_max), ("row_sum", row_sum)):
-        if not _same(t, torch.float32, rows, q):
+        for name, t in (("row_max", row_max), ("row_sum", row_sum)):
             _stat(t, rows, name, q.device)
     if out is None:
         dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
@@ -1035,7 +1043,7 @@ def attn_diff_backward(q, k, v, o, o2, row_max, row_sum, d_o, lam, k_lens=None, 
             raise ValueError("out must hold dq, dk and dv")
         dq, dk, dv = (_bf16(t, like.shape, name, q.device) for t, like, name in zip(out, (q, k, v), ("dq", "dk", "dv")))
     d_lam = lam.new_empty(lam.shape)
-    work = _workspace(need, q)
+    work = lam.new_empty(need >> 2)
     with _on(q):
         status = lib.rt_attn_diff_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), lam.data_ptr(), lam.numel(),
                                            _ptr(k_lens), o.data_ptr(), o2.data_ptr(), row_max.data_ptr(),
