@@ -1252,7 +1252,7 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d, bool lens) {
     const int64_t share = lens ? 6 : 8, rk = ceil_div(nk * share, 8), rq = ceil_div(nq * share, 8);
     int64_t best = INT64_MAX;
     for (int two = 0; two < (nk + nq > 4096 ? 1 : 2); ++two) {
-        for (int i = 1; i <= 16; ++i) {
+        for (int i = 1; i <= 32; ++i) {
             const int64_t part = std::max<int64_t>(1, ceil_div(longest, i));
             const int64_t sk = std::max<int64_t>(1, ceil_div(wk, part)), sq = std::max<int64_t>(1, ceil_div(wq, part));
             // the parts in whole tiles of 128 x D; a gigabyte and a half of them at most
@@ -1271,7 +1271,9 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d, bool lens) {
     }
     return p;
 }
+// Floats of the row values, and of the sums of 16 rows for dlam, in 64 bits
 int64_t diff_vals(const rt_diff_dims& d) { return (int64_t)d.B * d.H * 4 * whole64(d.Tq); }
+int64_t diff_lam_part(const rt_diff_dims& d) { return (int64_t)d.B * d.H * (whole64(d.Tq) / 16) * 2; }
 int64_t diff_part_k(const rt_diff_dims& d, int64_t split) {
     return (int64_t)d.B * d.H * ceil_div(d.Tk, rt::kDiffRows) * split * 4 * rt::kDiffRows * d.D;
 }
@@ -1280,7 +1282,7 @@ int64_t diff_part_q(const rt_diff_dims& d, int64_t split) {
 }
 int64_t diff_back_workspace(const rt_diff_dims& d, const DiffBackPlan& p) {
     const int64_t parts = (p.split_k > 1 ? diff_part_k(d, p.split_k) : 0) + (p.split_q > 1 ? diff_part_q(d, p.split_q) : 0);
-    return std::max<int64_t>(16, (diff_vals(d) + parts) * 4);
+    return std::max<int64_t>(16, (diff_vals(d) + diff_lam_part(d) + parts) * 4);
 }
 
 // What both calls check and set alike.
@@ -1410,7 +1412,8 @@ rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, con
     a.q_first = plan.q_first;
     a.split_k = plan.split_k;
     a.split_q = plan.split_q;
-    a.part_k = a.row_vals + diff_vals(dims);
+    a.lam_part = reinterpret_cast<double*>(a.row_vals + diff_vals(dims));
+    a.part_k = a.row_vals + diff_vals(dims) + diff_lam_part(dims);
     a.part_q = a.part_k + (a.split_k > 1 ? diff_part_k(dims, a.split_k) : 0);
     if (n_lam == 0) return ok();  // no heads
     return hip_status(rt::launch_diff_backward(a, dims.D, static_cast<hipStream_t>(stream)),

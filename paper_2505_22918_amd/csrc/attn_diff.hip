@@ -890,20 +890,17 @@ hipError_t launch_fwd_d(const DiffArgs& a, hipStream_t stream) {
 // ---- backward ------------------------------------------------------------------------------
 
 // 16 lanes a row (the first two of them take a 72-wide head's last chunks too); rows are counted with each head's padded
-// to whole 64, whose values are zeros
+// to whole 64, whose values are zeros.  A workgroup's 16 rows, of one head, leave their sum of -delta_2 for dlam.
 template <int D>
-__global__ __launch_bounds__(256) void diff_rows(DiffArgs a, int64_t rows) {
+__global__ __launch_bounds__(256) void diff_rows(DiffArgs a) {
+    __shared__ float lam_row[16];
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
     const int c = threadIdx.x & 15;
-    if (i >= rows) return;
     const int64_t bh = i / a.T64;
     const int t = (int)(i - bh * a.T64);
     float* vals = a.row_vals + bh * 4 * a.T64 + t;
-    if (t >= a.Tq) {
-        if (c < 4) vals[(size_t)c * a.T64] = 0.f;
-        return;
-    }
-    const int64_t row = bh * a.Tq + t;
+    const bool there = t < a.Tq;
+    const int64_t row = bh * a.Tq + (there ? t : 0);
     float s = 0.f, s2 = 0.f;
     auto add = [&](int ch) {
         const size_t at = row * (2 * D) + 8 * ch;
@@ -917,8 +914,10 @@ __global__ __launch_bounds__(256) void diff_rows(DiffArgs a, int64_t rows) {
             s2 = __builtin_fmaf(hi_f(x2[w]), hi_f(y[w]), s2);
         }
     };
-    add(c);
-    if (D == 72 && c < 2) add(16 + c);
+    if (there) {
+        add(c);
+        if (D == 72 && c < 2) add(16 + c);
+    }
     s += dpp<0xB1>(s);
     s2 += dpp<0xB1>(s2);
     s += dpp<0x4E>(s);
@@ -927,6 +926,18 @@ __global__ __launch_bounds__(256) void diff_rows(DiffArgs a, int64_t rows) {
     s2 += dpp<0x141>(s2);
     s += dpp<0x140>(s);
     s2 += dpp<0x140>(s2);
+    if (c == 0) lam_row[threadIdx.x >> 4] = -s2;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double sum = 0.0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += lam_row[r];
+        a.lam_part[blockIdx.x] = sum;
+    }
+    if (!there) {
+        if (c < 4) vals[(size_t)c * a.T64] = 0.f;
+        return;
+    }
     if (c < 2) {
         const size_t at = (size_t)(2 * bh + c) * a.Tq + t;
         const float l = a.row_sum[at];
@@ -937,19 +948,20 @@ __global__ __launch_bounds__(256) void diff_rows(DiffArgs a, int64_t rows) {
     if (c == 3) vals[(size_t)3 * a.T64] = s2 - __builtin_fmaf(a.lam[(bh % a.H) * a.lam_step], s2, s);
 }
 
-// dlam of head h (all heads where they share it): the sum of -delta_2, in 64 bits
+// dlam of head h (all heads where they share it), in 64 bits
 __device__ __forceinline__ void sum_lam(const DiffArgs& a, double* lds, int h) {
     double s = 0.0;
-    const int step = a.lam_step ? a.H : 1;
+    const int each = a.T64 / 16;  // sums of a head
+    const int n = a.lam_step ? each : a.n_bh * each, step = a.lam_step ? a.H : a.n_bh;
     for (int bh = h; bh < a.n_bh; bh += step) {
-        const float* x = a.row_vals + ((size_t)bh * 4 + 2) * a.T64;
+        const double* x = a.lam_part + (size_t)bh * each;
 #pragma unroll 4
-        for (int t = threadIdx.x; t < a.T64; t += blockDim.x) s += x[t];
+        for (int t = threadIdx.x; t < n; t += blockDim.x) s += x[t];
     }
     lds[threadIdx.x] = s;
-    for (int n = blockDim.x / 2; n; n /= 2) {
+    for (int m = blockDim.x / 2; m; m /= 2) {
         __syncthreads();
-        if ((int)threadIdx.x < n) lds[threadIdx.x] += lds[threadIdx.x + n];
+        if ((int)threadIdx.x < m) lds[threadIdx.x] += lds[threadIdx.x + m];
     }
     if (threadIdx.x == 0) a.d_lam[h] = (float)lds[0];
 }
@@ -1291,7 +1303,7 @@ hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
     const int64_t rows = (int64_t)a.n_bh * a.T64;
     hipError_t e = hipSuccess;
     if (rows > 0) {
-        hipLaunchKernelGGL((diff_rows<D>), dim3((uint32_t)((rows * 16 + 255) / 256)), dim3(256), 0, stream, a, rows);
+        hipLaunchKernelGGL((diff_rows<D>), dim3((uint32_t)(rows / 16)), dim3(256), 0, stream, a);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

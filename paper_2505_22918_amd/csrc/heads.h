@@ -58,6 +58,7 @@ struct DiffArgs {
     uint16_t* dv;
     float* d_lam;
     float* row_vals;  // workspace [B, H][4][T64]
+    double* lam_part;  // workspace [B, H][T64 / 16]: sums of -delta_2
     int32_t T64;      // Tq in whole 64
     int32_t q_first;  // tiles of queries before those of keys
     int32_t two;      // eight waves to a tile, four of them for each half of a stage
