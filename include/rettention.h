@@ -400,7 +400,8 @@ rt_status rt_rope_backward(const void* dy, const int64_t dy_stride[3], const voi
  * and its sum of exp(score - m); without keys -inf and 0.  P is rounded to bf16 for the matrix
  * products, whose sums are fp32.  Equal calls give equal bits.  workspace: device, 16-byte
  * aligned, of the bytes that rt_attn_diff_workspace reports, overwritten (parts of the keys where
- * there are few rows).  Outputs and workspace must not overlap each other or an input.
+ * there are few rows; it may be NULL where 16 are reported).  Outputs and workspace must not
+ * overlap each other or an input.
  * D is 64 or 72; B H < 2^23, 4 T D <= 2^30 and B H T (in whole 64) < 2^28 for T = Tq and Tk. */
 typedef struct {
     int32_t B, H, Tq, Tk, D;

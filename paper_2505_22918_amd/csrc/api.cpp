@@ -1410,6 +1410,10 @@ rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, con
     a.row_vals = static_cast<float*>(workspace);
     a.two = plan.two;
     a.q_first = plan.q_first;
+    // one launch where all run at once on the chip, and the workgroup that sums a weight's gradient has few rows (16 heads of 60 that share one: 16.9 against 24 us)
+    const int64_t tiles = (int64_t)a.n_bh * (ceil_div(dims.Tk, rt::kDiffRows) + ceil_div(dims.Tq, rt::kDiffRows));
+    a.short_rows = dims.Tq <= rt::kDiffShort && tiles <= 256 && plan.split_k == 1 && plan.split_q == 1 &&
+                   (int64_t)(a.lam_step ? dims.B : a.n_bh) * dims.Tq <= 256;
     a.split_k = plan.split_k;
     a.split_q = plan.split_q;
     a.lam_part = reinterpret_cast<double*>(a.row_vals + diff_vals(dims));

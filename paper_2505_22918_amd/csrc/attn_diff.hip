@@ -889,19 +889,11 @@ hipError_t launch_fwd_d(const DiffArgs& a, hipStream_t stream) {
 
 // ---- backward ------------------------------------------------------------------------------
 
-// 16 lanes a row (the first two of them take a 72-wide head's last chunks too); rows are counted with each head's padded
-// to whole 64, whose values are zeros.  A workgroup's 16 rows, of one head, leave their sum of -delta_2 for dlam.
+// By 16 lanes a row (lane c of them; the first two take a 72-wide head's last chunks too): dO . O and dO . O_2 of row `row`
+// (counted over the heads), in all of them
 template <int D>
-__global__ __launch_bounds__(256) void diff_rows(DiffArgs a) {
-    __shared__ float lam_row[16];
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int c = threadIdx.x & 15;
-    const int64_t bh = i / a.T64;
-    const int t = (int)(i - bh * a.T64);
-    float* vals = a.row_vals + bh * 4 * a.T64 + t;
-    const bool there = t < a.Tq;
-    const int64_t row = bh * a.Tq + (there ? t : 0);
-    float s = 0.f, s2 = 0.f;
+__device__ __forceinline__ void row_products(const DiffArgs& a, int64_t row, int c, float& s, float& s2) {
+    s = s2 = 0.f;
     auto add = [&](int ch) {
         const size_t at = row * (2 * D) + 8 * ch;
         const u32x4 x = *reinterpret_cast<const u32x4*>(a.o + at), x2 = *reinterpret_cast<const u32x4*>(a.o2 + at),
@@ -914,10 +906,8 @@ __global__ __launch_bounds__(256) void diff_rows(DiffArgs a) {
             s2 = __builtin_fmaf(hi_f(x2[w]), hi_f(y[w]), s2);
         }
     };
-    if (there) {
-        add(c);
-        if (D == 72 && c < 2) add(16 + c);
-    }
+    add(c);
+    if (D == 72 && c < 2) add(16 + c);
     s += dpp<0xB1>(s);
     s2 += dpp<0xB1>(s2);
     s += dpp<0x4E>(s);
@@ -926,6 +916,29 @@ __global__ __launch_bounds__(256) void diff_rows(DiffArgs a) {
     s2 += dpp<0x141>(s2);
     s += dpp<0x140>(s);
     s2 += dpp<0x140>(s2);
+}
+// value c (0 .. 3) of row t of head bh from these products: log2 of a map's denominator, -delta_2, delta_2 - delta_1
+__device__ __forceinline__ float row_value(const DiffArgs& a, int64_t bh, int t, int c, float s, float s2) {
+    if (c < 2) {
+        const size_t at = (size_t)(2 * bh + c) * a.Tq + t;
+        const float l = a.row_sum[at];
+        return l == 0.f ? INFINITY : __builtin_fmaf(a.row_max[at], kLog2e, log2f(l));
+    }
+    // delta_1 = dO . O + lam delta_2
+    return c == 2 ? -s2 : s2 - __builtin_fmaf(a.lam[(bh % a.H) * a.lam_step], s2, s);
+}
+
+// Rows are counted with each head's padded to whole 64, whose values are zeros.  A workgroup's 16 rows, of one head, leave
+// their sum of -delta_2 for dlam.
+template <int D>
+__global__ __launch_bounds__(256) void diff_rows(DiffArgs a) {
+    __shared__ float lam_row[16];
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const int c = threadIdx.x & 15;
+    const int64_t bh = i / a.T64;
+    const int t = (int)(i - bh * a.T64);
+    float s = 0.f, s2 = 0.f;
+    if (t < a.Tq) row_products<D>(a, bh * a.Tq + t, c, s, s2);
     if (c == 0) lam_row[threadIdx.x >> 4] = -s2;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -934,29 +947,41 @@ __global__ __launch_bounds__(256) void diff_rows(DiffArgs a) {
         for (int r = 0; r < 16; ++r) sum += lam_row[r];
         a.lam_part[blockIdx.x] = sum;
     }
-    if (!there) {
-        if (c < 4) vals[(size_t)c * a.T64] = 0.f;
-        return;
+    if (c < 4) a.row_vals[bh * 4 * a.T64 + (size_t)c * a.T64 + t] = t < a.Tq ? row_value(a, bh, t, c, s, s2) : 0.f;
+}
+
+// SHORT: the values of rows t0 .. t0 + n - 1 of a head into LDS, [4][pitch]
+template <int D>
+__device__ __forceinline__ void rows_to_lds(const DiffArgs& a, lds_u8* to, int pitch, int bh, int t0, int n) {
+    const int c = threadIdx.x & 15;
+    for (int i = threadIdx.x >> 4; i < n; i += blockDim.x >> 4) {
+        float s = 0.f, s2 = 0.f;
+        const int t = t0 + i;
+        if (t < a.Tq) row_products<D>(a, (int64_t)bh * a.Tq + t, c, s, s2);
+        if (c < 4) *(lds_f32*)(to + (c * pitch + i) * 4) = t < a.Tq ? row_value(a, bh, t, c, s, s2) : 0.f;
     }
-    if (c < 2) {
-        const size_t at = (size_t)(2 * bh + c) * a.Tq + t;
-        const float l = a.row_sum[at];
-        vals[(size_t)c * a.T64] = l == 0.f ? INFINITY : __builtin_fmaf(a.row_max[at], kLog2e, log2f(l));
-    }
-    // delta_1 = dO . O + lam delta_2
-    if (c == 2) vals[(size_t)2 * a.T64] = -s2;
-    if (c == 3) vals[(size_t)3 * a.T64] = s2 - __builtin_fmaf(a.lam[(bh % a.H) * a.lam_step], s2, s);
 }
 
 // dlam of head h (all heads where they share it), in 64 bits
+template <int D, bool SHORT>
 __device__ __forceinline__ void sum_lam(const DiffArgs& a, double* lds, int h) {
     double s = 0.0;
-    const int each = a.T64 / 16;  // sums of a head
-    const int n = a.lam_step ? each : a.n_bh * each, step = a.lam_step ? a.H : a.n_bh;
-    for (int bh = h; bh < a.n_bh; bh += step) {
-        const double* x = a.lam_part + (size_t)bh * each;
+    const int step = a.lam_step ? a.H : 1;
+    if (SHORT) {
+        for (int bh = h; bh < a.n_bh; bh += step)
+            for (int t = threadIdx.x >> 4; t < a.Tq; t += blockDim.x >> 4) {
+                float x, x2;
+                row_products<D>(a, (int64_t)bh * a.Tq + t, threadIdx.x & 15, x, x2);
+                if ((threadIdx.x & 15) == 0) s -= x2;
+            }
+    } else {
+        const int each = a.T64 / 16;  // sums of a head
+        const int n = a.lam_step ? each : a.n_bh * each;
+        for (int bh = h; bh < a.n_bh; bh += a.lam_step ? a.H : a.n_bh) {
+            const double* x = a.lam_part + (size_t)bh * each;
 #pragma unroll 4
-        for (int t = threadIdx.x; t < n; t += blockDim.x) s += x[t];
+            for (int t = threadIdx.x; t < n; t += blockDim.x) s += x[t];
+        }
     }
     lds[threadIdx.x] = s;
     for (int m = blockDim.x / 2; m; m /= 2) {
@@ -966,6 +991,11 @@ __device__ __forceinline__ void sum_lam(const DiffArgs& a, double* lds, int h) {
     if (threadIdx.x == 0) a.d_lam[h] = (float)lds[0];
 }
 
+// Heads of up to kShortRows queries in few tiles: the workgroups form the row values themselves (those of dK and dV all of
+// a head's, in LDS), which saves the launch of diff_rows: one head of 100 tokens 16.7 -> 13.9 us; of 256, in turns of 16
+// rows, 17.6 -> 20.
+constexpr int kShortRows = kDiffShort;
+
 // 16-byte pieces of a lane's sums
 template <int D, bool KV>
 constexpr int SUMS = (KV ? 32 : 16) + (D == 72 ? (KV ? 4 : 2) : 0);
@@ -974,11 +1004,12 @@ constexpr int SUMS = (KV ? 32 : 16) + (D == 72 ? (KV ? 4 : 2) : 0);
 // 32 own rows to a wave, kDiffRows to a workgroup of four waves, against stages of BS rows; or (TWO) to one of eight, of
 // which four take the first half of each stage and four the other, and join their sums in LDS.  SPLIT: against a part
 // of the other side.
-template <int D, bool KV, int BS, bool TWO, bool SPLIT>
+template <int D, bool KV, int BS, bool TWO, bool SPLIT, bool SHORT>
 __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int item, int part) {
     constexpr int W = kDiffRows / 32;
     static_assert(!TWO || BS == 64, "a half to each four waves");
-    using R = DiffRing<D, TWO ? 2 * W : W, BS, KV>;
+    using R = DiffRing<D, TWO ? 2 * W : W, BS, KV && !SHORT>;
+    constexpr int OWN = R::LDS + (SHORT ? kShortRows * 16 : 0);  // LDS offset of what the walk keeps of its own
     using Rd = Reads<D>;
     constexpr int NB = R::NB, WB = R::WB, NW = KV ? 4 : 1;
     constexpr bool TAIL = D == 72;
@@ -1002,7 +1033,7 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     R ring;
     ring.init(lds, x, x + (size_t)Tx * D, (KV ? a.d_o : a.v) + w_x, x_end);
     const float* vals = a.row_vals + (size_t)bh * 4 * a.T64;
-    if (KV) ring.init_values(vals, a.T64);
+    if (KV && !SHORT) ring.init_values(vals, a.T64);
     ring.load(0, s0 * BS);
     Rd rd;
     rd.init(lds);
@@ -1010,7 +1041,7 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     bf16x8 n_op[2][4], n_tail[2], w_op[KV ? 1 : Rd::WS];
 #pragma unroll
     for (int i = 0; i < 2; ++i) rd.own_rows(own + (size_t)i * T * D, NB, row0, own_end, n_op[i], TAIL ? &n_tail[i] : nullptr);
-    const int own_v = R::LDS + 32 * wave * WB, own_t = R::LDS + 32 * W * WB + wave * 1024;
+    const int own_v = OWN + 32 * wave * WB, own_t = OWN + 32 * W * WB + wave * 1024;
     if constexpr (KV) {
         if (half == 0) ring.load_own(own_v, row0, buffer_rsrc(a.v + w_own, own_end * WB));
         if (TAIL && half == 0 && !rd.hi) {
@@ -1020,11 +1051,16 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     } else
         rd.own_rows(a.d_o + w_own, WB, row0, own_end, w_op, nullptr);
     float log[2] = {INFINITY, INFINITY}, minus = 0.f, more = 0.f;  // of the own query
+    if (SHORT) {
+        rows_to_lds<D>(a, lds + R::LDS, kShortRows, bh, KV ? 0 : tile0, KV ? a.T64 : 32 * W);
+        __syncthreads();
+    }
     if (!KV && row0 + rd.l32 < T) {
-        log[0] = vals[row0 + rd.l32];
-        log[1] = vals[a.T64 + row0 + rd.l32];
-        minus = vals[2 * a.T64 + row0 + rd.l32];
-        more = vals[3 * a.T64 + row0 + rd.l32];
+        auto value = [&](int n) { return SHORT ? *(lds_f32*)(lds + R::LDS + (n * kShortRows + 32 * wave + rd.l32) * 4) : vals[n * a.T64 + row0 + rd.l32]; };
+        log[0] = value(0);
+        log[1] = value(1);
+        minus = value(2);
+        more = value(3);
     }
     const float c2 = a.scale_log2, lam = a.lam[(bh - b * a.H) * a.lam_step];
 
@@ -1049,7 +1085,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
                 if (KV) rd.unpack();
                 // four values of a chunk's rows 8 j + 4 hi ..
                 auto value = [&](int n, int j) {
-                    return __builtin_bit_cast(f32x4, *(const lds_u32x4*)(lds + st + R::VAL + n * BS * 4 + (32 * h + 8 * j + 4 * rd.hi) * 4));
+                    const int at = SHORT ? R::LDS + (n * kShortRows + s * BS) * 4 : st + R::VAL + n * BS * 4;
+                    return __builtin_bit_cast(f32x4, *(const lds_u32x4*)(lds + at + (32 * h + 8 * j + 4 * rd.hi) * 4));
                 };
                 f32x16 dp;  // dA - delta_2
                 if (KV) {
@@ -1232,17 +1269,18 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
 
 constexpr int most(int x, int y) { return x > y ? x : y; }
 
-template <int D, bool TWO, bool SPLIT>
+template <int D, bool TWO, bool SPLIT, bool SHORT>
 __global__ __launch_bounds__(TWO ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_bwd(DiffArgs a, int n_lam, int n_k,
                                                                                                      int per_k, int n_q, int per_q) {
     constexpr int W = TWO ? 8 : 4, BS_K = TWO ? 64 : 32;
-    constexpr int LDS_K = DiffRing<D, W, BS_K, true>::LDS + kDiffRows * (4 * D + (D == 72 ? 32 : 0)), LDS_Q = DiffRing<D, W, 64, false>::LDS;
-    __shared__ __attribute__((aligned(1024))) unsigned char smem[most(most(LDS_K, LDS_Q), TWO ? 4 * SUMS<D, true> * 1024 : 0)];
+    constexpr int LDS_K = DiffRing<D, W, BS_K, !SHORT>::LDS + kDiffRows * (4 * D + (D == 72 ? 32 : 0)), LDS_Q = DiffRing<D, W, 64, false>::LDS;
+    constexpr int VALS = SHORT ? kShortRows * 16 : 0;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[most(most(LDS_K, LDS_Q) + VALS, TWO ? 4 * SUMS<D, true> * 1024 : 0)];
     lds_u8* const lds = (lds_u8*)smem;
     int g = blockIdx.x;
     const int lam8 = (n_lam + 7) & ~7;  // (whole eights, so that a tile's XCD goes by its number)
     if (g < lam8) {
-        if (g < n_lam) sum_lam(a, reinterpret_cast<double*>(smem), g);
+        if (g < n_lam) sum_lam<D, SHORT>(a, reinterpret_cast<double*>(smem), g);
         return;
     }
     g -= lam8;
@@ -1258,9 +1296,9 @@ __global__ __launch_bounds__(TWO ? 512 : 256) __attribute__((amdgpu_waves_per_eu
         item /= split;
     }
     if (kv)
-        diff_walk<D, true, BS_K, TWO, SPLIT>(a, lds, item, part);
+        diff_walk<D, true, BS_K, TWO, SPLIT, SHORT>(a, lds, item, part);
     else
-        diff_walk<D, false, 64, TWO, SPLIT>(a, lds, item, part);
+        diff_walk<D, false, 64, TWO, SPLIT, SHORT>(a, lds, item, part);
 }
 
 // Sums of a tile's parts: dK_1, dK_2, the halves of dV (kind 0 .. 3; `tiles_k` of them in x), then dQ_1, dQ_2 (4, 5);
@@ -1302,7 +1340,7 @@ template <int D>
 hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
     const int64_t rows = (int64_t)a.n_bh * a.T64;
     hipError_t e = hipSuccess;
-    if (rows > 0) {
+    if (rows > 0 && !a.short_rows) {
         hipLaunchKernelGGL((diff_rows<D>), dim3((uint32_t)(rows / 16)), dim3(256), 0, stream, a);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -1316,10 +1354,12 @@ hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
         hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, stream, a, n_lam, n_k, per_k, n_q, per_q);
         return hipGetLastError();
     };
-    if (a.two)
-        e = split ? run(diff_bwd<D, true, true>, 512) : run(diff_bwd<D, true, false>, 512);
+    if (a.short_rows)
+        e = a.two ? run(diff_bwd<D, true, false, true>, 512) : run(diff_bwd<D, false, false, true>, 256);
+    else if (a.two)
+        e = split ? run(diff_bwd<D, true, true, false>, 512) : run(diff_bwd<D, true, false, false>, 512);
     else
-        e = split ? run(diff_bwd<D, false, true>, 256) : run(diff_bwd<D, false, false>, 256);
+        e = split ? run(diff_bwd<D, false, true, false>, 256) : run(diff_bwd<D, false, false, false>, 256);
     if (e != hipSuccess || !split) return e;
     const int sums_k = a.split_k > 1 ? tiles_k : 0, sums_q = a.split_q > 1 ? tiles_q : 0, kind0 = sums_k ? 0 : 4;
     hipLaunchKernelGGL((diff_sum<D>), dim3(most(sums_k, sums_q), (sums_q ? 6 : 4) - kind0, kDiffRows * D / 1024), dim3(256), 0, stream, a,

@@ -33,6 +33,7 @@ inline int64_t rope_blocks(const RopeArgs& a) { return (int64_t)a.B * a.groups *
 __attribute__((weak)) hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
 
 constexpr int kDiffRows = 128;  // rows of a tile of four waves
+constexpr int kDiffShort = 128;  // most rows of queries whose values a workgroup forms
 constexpr int kDiffParts = 32;  // parts of a tile's keys, at most
 struct DiffArgs {
     const uint16_t* q;  // bf16 [B, 2 H, Tq, D]
@@ -60,6 +61,7 @@ struct DiffArgs {
     float* row_vals;  // workspace [B, H][4][T64]
     double* lam_part;  // workspace [B, H][T64 / 16]: sums of -delta_2
     int32_t T64;      // Tq in whole 64
+    int32_t short_rows;  // the workgroups form the row values
     int32_t q_first;  // tiles of queries before those of keys
     int32_t two;      // eight waves to a tile, four of them for each half of a stage
     int32_t split_k, split_q;  // workgroups that share the walk of a tile of keys, of queries

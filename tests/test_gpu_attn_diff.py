@@ -72,7 +72,7 @@ def _lens(lens):
 
 
 SIZES = [(1, 1, 1, 1), (1, 1, 1, 2), (2, 3, 1, 300), (1, 2, 15, 2000), (1, 1, 16, 33), (2, 1, 17, 700), (2, 1, 32, 32), (1, 2, 33, 31), (1, 1, 64, 65), (2, 2, 127, 63), (1, 1, 128, 200), (1, 3, 129, 129),
-         (1, 1, 300, 1), (1, 1, 5, 700), (1, 2, 700, 5), (1, 1, 257, 1100),
+         (1, 1, 300, 1), (1, 1, 5, 700), (2, 3, 100, 70), (1, 1, 128, 128), (1, 2, 90, 500), (1, 2, 700, 5), (1, 1, 257, 1100),
          # waves of four on 128 rows, whole and in parts; gradients in parts of either side's walk, and of both
          (1, 40, 300, 130), (1, 40, 200, 1500), (1, 1, 33, 1000), (1, 1, 33, 700), (1, 1, 129, 700), (1, 1, 513, 64), (1, 20, 33, 1000),
          (3, 12, 513, 64), (1, 8, 1100, 1000)]
