@@ -1193,9 +1193,9 @@ struct DiffPlan {
     int32_t by_keys, split;
 };
 DiffPlan diff_plan(const rt_diff_dims& d, bool lens) {
-    // where samples have numbers of keys of their own, as if three quarters of the heads had work (9 heads of 7238 tokens and
-    // fewer keys 525 -> 394 us, 60 heads of 177 queries over 6590 keys and fewer 98 -> 88; of one token 15.4 against 16.0)
-    const int64_t bh = ceil_div((int64_t)d.B * d.H * (lens && d.Tq > 32 ? 6 : 8), 8), chunks = ceil_div(d.Tk, 32);
+    // where samples have numbers of keys of their own, as if five eighths of the heads had work (60 heads of 177 queries over
+    // 6590 keys and fewer 98 us as if all had, 88 six eighths, 55 five; 9 heads of 7238 tokens and fewer keys 322, 263, 263)
+    const int64_t bh = ceil_div((int64_t)d.B * d.H * (lens && d.Tq > 32 ? 5 : 8), 8), chunks = ceil_div(d.Tk, 32);
     DiffPlan p{0, 1};
     int64_t best = INT64_MAX;
     // (of 32 queries, a tile of four waves would keep one busy)
@@ -1249,9 +1249,9 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d, bool lens) {
     // half microseconds: of a walk's chunks of 32 rows, two waves to a SIMD
     const int64_t wk = 4 * ceil_div(d.Tq, 32), wq = 3 * ceil_div(d.Tk, 32);
     const int64_t longest = std::max(wk, wq);
-    // where samples have numbers of keys of their own, tiles and parts are counted as if three quarters had work (12 heads of
-    // 3000 tokens, of a sample with all keys and one with few, 169 us against 230, a sample's 4000 tokens 129 against 110)
-    const int64_t share = lens ? 6 : 8, rk = ceil_div(nk * share, 8), rq = ceil_div(nq * share, 8);
+    // where samples have numbers of keys of their own, tiles and parts are counted as if seven eighths had work (12 heads of
+    // 3000 tokens and fewer keys 195 us as if all had, 167 seven eighths or six; 24 heads of 1542 119 as if all, 119, 126)
+    const int64_t share = lens ? 7 : 8, rk = ceil_div(nk * share, 8), rq = ceil_div(nq * share, 8);
     int64_t best = INT64_MAX;
     for (int two = 0; two < (nk + nq > 4096 ? 1 : 2); ++two) {
         for (int i = 1; i <= 32; ++i) {
@@ -1305,6 +1305,8 @@ rt_status diff_args(const void* q, const void* k, const void* v, const float* la
     a.lam = lam;
     a.lam_step = n_lam == d.H && d.H > 1 ? 1 : 0;
     a.k_lens = k_lens;
+    a.by_len = k_lens && d.Tq > 32 && d.B > 1 && d.B <= 64;
+    a.B = d.B;
     a.H = d.H;
     a.Tq = d.Tq;
     a.Tk = d.Tk;

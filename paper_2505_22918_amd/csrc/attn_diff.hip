@@ -251,16 +251,44 @@ struct DiffRing {
 typedef __attribute__((address_space(3))) float lds_f32;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
-// The n-th head to be taken: heads of the samples in turn, so that samples of few and of many keys share the XCDs, each of
-// which takes heads that follow one another.
-__device__ __forceinline__ int head_of(const DiffArgs& a, int n) {
-    const int B = a.n_bh / a.H, h = n / B;
-    return (n - h * B) * a.H + h;
+// Heads are taken in the order of head_of().  Where samples have numbers of keys of their own (a.by_len, for up to 64
+// samples): those of the samples with most keys first, so that the longest walks begin first, and each XCD takes an eighth
+// of every sample's tiles, in tiles that follow one another (9 heads of 7238 tokens and fewer keys 391 -> 264 us, gradients
+// of 25 heads of 4789 760 -> 572).  Else heads of the samples in turn, an eighth of all tiles to an XCD.
+
+// Workgroups of an XCD for n items, and the item of workgroup g, or -1: an XCD has every eighth workgroup.
+__host__ __device__ inline int per_xcd(const DiffArgs& a, int n) {
+    return a.by_len ? a.B * ((n / a.B + 7) / 8) : (n + 7) / 8;
 }
-__device__ __forceinline__ int keys_of(const DiffArgs& a, int b) {
-    if (!a.k_lens) return a.Tk;
-    const int n = a.k_lens[b];
-    return n < 0 ? 0 : (n > a.Tk ? a.Tk : n);
+__device__ __forceinline__ int item_of(const DiffArgs& a, int g, int n) {
+    int x = g & 7, j = g >> 3, m = n, before = 0;
+    if (a.by_len) {
+        m = n / a.B;
+        const int per = (m + 7) / 8, r = j / per;
+        x = (x + r) & 7;  // what a sample's tiles leave of eight is another XCD's each time
+        j -= r * per;
+        before = r * m;
+    }
+    j += (int)((int64_t)x * m / 8);
+    return j < (int)((int64_t)(x + 1) * m / 8) ? before + j : -1;
+}
+__device__ __forceinline__ int keys_in(const DiffArgs& a, int n) { return n < 0 ? 0 : (n > a.Tk ? a.Tk : n); }
+// The n-th head to be taken, b H + h, and its keys.
+__device__ __forceinline__ int head_of(const DiffArgs& a, int n, int& keys) {
+    if (a.by_len) {
+        const int lane = threadIdx.x & 63, r = n / a.H, mine = lane < a.B ? keys_in(a, a.k_lens[lane]) : 0;
+        int rank = lane < a.B ? 0 : 64;
+        for (int b = 0; b < a.B; ++b) {
+            const int other = __builtin_amdgcn_readlane(mine, b);
+            rank += other > mine || (other == mine && b < lane);
+        }
+        const int b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == r));
+        keys = __builtin_amdgcn_readlane(mine, b);
+        return b * a.H + n - r * a.H;
+    }
+    const int h = n / a.B, b = n - h * a.B;
+    keys = a.k_lens ? keys_in(a, a.k_lens[b]) : a.Tk;
+    return b * a.H + h;
 }
 
 // ---- forward -------------------------------------------------------------------------------
@@ -284,7 +312,7 @@ constexpr float kMove = 24.0f;  // the running max moves when a probability agai
 // then [..][3] of the max in score units, the sum and the true max).
 template <int D, bool KEYS, bool STATS, bool SPLIT>
 __global__ __launch_bounds__(KEYS ? 512 : 256) __attribute__((amdgpu_waves_per_eu(2, 2))) void
-diff_fwd(DiffArgs a, int n_items, int per_xcd) {
+diff_fwd(DiffArgs a, int n_items) {
     constexpr int BS = KEYS ? 32 : 64, STEP = KEYS ? 4 : 1;  // keys of a stage; stages from one of a wave to its next
     using R = DiffRing<D, KEYS ? 1 : 4, BS, false>;
     constexpr int NB = R::NB, WB = R::WB;
@@ -294,17 +322,18 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     lds_u8* const lds = (lds_u8*)smem + (KEYS ? wave * R::LDS : 0);
 
-    int item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), part = 0;
-    if (item >= n_items) return;
+    int item = item_of(a, blockIdx.x, n_items), part = 0;
+    if (item < 0) return;
     if (SPLIT) {
         part = item % a.split;
         item /= a.split;
     }
     constexpr int ROWS = KEYS ? 32 : kDiffRows;
     const int n_tile = (a.Tq + ROWS - 1) / ROWS, head = item / n_tile;
-    const int bh = head_of(a, head), b = bh / a.H;
+    int keys;
+    const int bh = head_of(a, head, keys);
     const int row0 = (item - head * n_tile) * ROWS + (KEYS ? 0 : wave * 32);
-    const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
+    const int n_st = (keys + BS - 1) / BS;
     // parts are as long for every sample, so that those of short ones cost little
     const int per = SPLIT ? ((a.Tk + BS - 1) / BS + a.split - 1) / a.split : n_st;
     const int first_stage = part * per + (KEYS ? wave : 0), end_stage = SPLIT && part * per + per < n_st ? part * per + per : n_st;
@@ -548,7 +577,7 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
             a.row_sum[at] = l_run[i] == 0.f ? 0.f : l_run[i] * __builtin_amdgcn_exp2f((m_run[i] - m_top[i]) * c2);
         }
     }
-    const float lam = a.lam[(bh - b * a.H) * a.lam_step];
+    const float lam = a.lam[(bh % a.H) * a.lam_step];
     uint16_t* const o = a.o + (size_t)bh * a.Tq * (2 * D);
     uint16_t* const o2 = STATS ? a.o2 + (size_t)bh * a.Tq * (2 * D) : nullptr;
     if (row < a.Tq) {
@@ -592,7 +621,7 @@ diff_fwd(DiffArgs a, int n_items, int per_xcd) {
 // 32).  Both maps' scores come out of one accumulator: the operand of a map's queries is zero in the other's columns, where
 // a key that is not finite in one map makes the other's statistics NaN (its output is NaN either way).
 template <int D, bool STATS, bool SPLIT>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_few(DiffArgs a, int n_items, int per_xcd) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_few(DiffArgs a, int n_items) {
     constexpr int BS = 32, STEP = 4;
     using R = DiffRing<D, 1, BS, false>;
     constexpr int NB = R::NB;
@@ -603,14 +632,15 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     lds_u8* const all = (lds_u8*)smem;
     lds_u8* const lds = all + wave * R::LDS;
 
-    int item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3), part = 0;
-    if (item >= n_items) return;
+    int item = item_of(a, blockIdx.x, n_items), part = 0;
+    if (item < 0) return;
     if (SPLIT) {
         part = item % a.split;
         item /= a.split;
     }
-    const int bh = head_of(a, item), b = bh / a.H;
-    const int keys = keys_of(a, b), n_st = (keys + BS - 1) / BS;
+    int keys;
+    const int bh = head_of(a, item, keys);
+    const int n_st = (keys + BS - 1) / BS;
     const int per = SPLIT ? ((a.Tk + BS - 1) / BS + a.split - 1) / a.split : n_st;
     const int first_stage = part * per + wave, end_stage = SPLIT && part * per + per < n_st ? part * per + per : n_st;
     if (SPLIT && part * per >= n_st) {
@@ -774,7 +804,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         a.row_max[at] = m_top * a.scale_nat;
         a.row_sum[at] = l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f((m - m_top) * c2);
     }
-    const float lam = a.lam[(bh - b * a.H) * a.lam_step];
+    const float lam = a.lam[(bh % a.H) * a.lam_step];
     // the maps' values of a query from the lanes of both: map 1's lanes write o, map 2's o2
     uint32_t out[8];
 #pragma unroll
@@ -871,8 +901,8 @@ __global__ __launch_bounds__(256) void diff_join(DiffArgs a) {
 template <int D, bool STATS, bool SPLIT>
 hipError_t launch_fwd(const DiffArgs& a, hipStream_t stream) {
     auto run = [&](auto kernel, int rows) {
-        const int n = a.n_bh * ((a.Tq + rows - 1) / rows) * (SPLIT ? a.split : 1), per = (n + 7) / 8;
-        hipLaunchKernelGGL(kernel, dim3(8 * per), dim3(256), 0, stream, a, n, per);
+        const int n = a.n_bh * ((a.Tq + rows - 1) / rows) * (SPLIT ? a.split : 1), per = per_xcd(a, n);
+        hipLaunchKernelGGL(kernel, dim3(8 * per), dim3(256), 0, stream, a, n);
         return hipGetLastError();
     };
     const hipError_t e = !a.by_keys ? run(diff_fwd<D, false, STATS, SPLIT>, kDiffRows)
@@ -1014,9 +1044,11 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     constexpr int NB = R::NB, WB = R::WB, NW = KV ? 4 : 1;
     constexpr bool TAIL = D == 72;
     const int T = KV ? a.Tk : a.Tq, Tx = KV ? a.Tq : a.Tk;  // rows of the own side and of the other
-    const int n_tile = (T + 32 * W - 1) / (32 * W), head = item / n_tile, bh = head_of(a, head), b = bh / a.H;
+    const int n_tile = (T + 32 * W - 1) / (32 * W), head = item / n_tile;
+    int keys;
+    const int bh = head_of(a, head, keys);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = TWO ? w % W : w, half = TWO ? w / W : 0;
-    const int row0 = ((item - head * n_tile) * W + wave) * 32, keys = keys_of(a, b);
+    const int row0 = ((item - head * n_tile) * W + wave) * 32;
     const int own_end = KV ? keys : T, x_end = KV ? Tx : keys;
     const int tile0 = row0 - 32 * wave;
     int n_st = (x_end + BS - 1) / BS;
@@ -1062,7 +1094,7 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
         minus = value(2);
         more = value(3);
     }
-    const float c2 = a.scale_log2, lam = a.lam[(bh - b * a.H) * a.lam_step];
+    const float c2 = a.scale_log2, lam = a.lam[(bh % a.H) * a.lam_step];
 
     f32x16 acc[2][2], wacc[NW];  // dK or dQ of each map; dV
     f32x4 tacc[2], wtacc[2];  // 72 wide: both maps' last 8 elements, dV's last 16, of 16 own rows each
@@ -1289,8 +1321,8 @@ __global__ __launch_bounds__(TWO ? 512 : 256) __attribute__((amdgpu_waves_per_eu
     const bool kv = (g < ahead) != (a.q_first != 0);
     if (g >= ahead) g -= ahead;
     const int split = kv ? a.split_k : a.split_q;
-    int item = (g & 7) * (kv ? per_k : per_q) + (g >> 3), part = 0;
-    if (item >= (kv ? n_k : n_q)) return;
+    int item = item_of(a, g, kv ? n_k : n_q), part = 0;
+    if (item < 0) return;
     if (SPLIT) {
         part = item % split;
         item /= split;
@@ -1310,7 +1342,8 @@ __global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int bs_k, int kind0,
     const bool kv = kind < 4;
     if ((int)blockIdx.x >= (kv ? tiles_k : tiles_q)) return;
     const int T = kv ? a.Tk : a.Tq, n_tile = (T + kDiffRows - 1) / kDiffRows, n = kv ? a.split_k : a.split_q;
-    const int head = blockIdx.x / n_tile, bh = head_of(a, head), row0 = (blockIdx.x - head * n_tile) * kDiffRows;
+    int keys;
+    const int head = blockIdx.x / n_tile, bh = head_of(a, head, keys), row0 = (blockIdx.x - head * n_tile) * kDiffRows;
     const int width = kv && kind >= 2 ? 2 * D : D, which = kv ? kind : kind - 4;
     const size_t stride = (kv ? 4 : 2) * (size_t)TILE;
     const float* part = (kv ? a.part_k : a.part_q) + (size_t)blockIdx.x * n * stride + (size_t)which * TILE;
@@ -1326,7 +1359,7 @@ __global__ __launch_bounds__(256) void diff_sum(DiffArgs a, int bs_k, int kind0,
     const int left = T - row0, size = (left < kDiffRows ? left : kDiffRows) * width;
     if (j >= TILE || skip + j >= size) return;
     // parts that hold rows of the other side, as diff_walk has them; none for keys that the sample does not have
-    const int keys = keys_of(a, bh / a.H), Tx = kv ? a.Tq : a.Tk, bs = kv ? bs_k : 64, per = ((Tx + bs - 1) / bs + n - 1) / n;
+    const int Tx = kv ? a.Tq : a.Tk, bs = kv ? bs_k : 64, per = ((Tx + bs - 1) / bs + n - 1) / n;
     const int stages = kv ? (row0 < keys ? (Tx + bs - 1) / bs : 0) : (keys + bs - 1) / bs, full = (stages + per - 1) / per;
     f32x4 s = {};
 #pragma unroll 4
@@ -1347,7 +1380,7 @@ hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
     }
     const int tiles_k = a.n_bh * ((a.Tk + kDiffRows - 1) / kDiffRows), tiles_q = a.n_bh * ((a.Tq + kDiffRows - 1) / kDiffRows);
     const bool split = a.split_k > 1 || a.split_q > 1;
-    const int n_k = tiles_k * a.split_k, n_q = tiles_q * a.split_q, per_k = (n_k + 7) / 8, per_q = (n_q + 7) / 8;
+    const int n_k = tiles_k * a.split_k, n_q = tiles_q * a.split_q, per_k = per_xcd(a, n_k), per_q = per_xcd(a, n_q);
     const int n_lam = a.lam_step ? a.H : 1;
     const dim3 grid(((n_lam + 7) & ~7) + 8 * per_k + 8 * per_q);
     auto run = [&](auto kernel, int threads) {

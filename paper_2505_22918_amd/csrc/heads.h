@@ -42,7 +42,8 @@ struct DiffArgs {
     const float* lam;   // [H], or one value (lam_step 0)
     int32_t lam_step;
     const int32_t* k_lens;  // [B], or null
-    int32_t H, Tq, Tk, n_bh;
+    int32_t by_len;  // the samples with most keys first (B up to 64)
+    int32_t B, H, Tq, Tk, n_bh;
     float scale_nat, scale_log2;
     // forward
     uint16_t* o;    // bf16 [B, H, Tq, 2 D]

@@ -118,6 +118,29 @@ def test_padded_keys(gpu, Tq, Tk, lens, D):
         assert not got[1][b, :, n:].any() and not got[2][b, :, n:].any()
 
 
+# samples are taken by their numbers of keys up to 64 of them, in whatever order they lie
+@pytest.mark.parametrize("B,H,Tq,Tk,D", [(64, 1, 40, 70, 64), (65, 1, 40, 70, 72), (3, 5, 260, 300, 72), (2, 3, 700, 50, 64), (5, 1, 33, 1500, 64), (9, 2, 129, 257, 72)])
+def test_padded_order(gpu, B, H, Tq, Tk, D):
+    import torch
+
+    print(f"[diff] order of samples B={B} H={H} Tq={Tq} Tk={Tk} D={D}", flush=True)
+    q, k, v, do, lam = _inputs(B, H, Tq, Tk, D, 13)
+    g = torch.Generator().manual_seed(13)
+    used = [int(x) for x in torch.randint(-3, Tk + 4, (B,), generator=g)]
+    used[-1], used[0] = Tk, used[B // 2]  # the longest last, two alike
+    lens, clamped = _lens(used), [min(max(n, 0), Tk) for n in used]
+    out = rt.attn_diff(q, k, v, lam, k_lens=lens)
+    _check_forward(out, q, k, v, lam, clamped)
+    got = rt.attn_diff_backward(q, k, v, *out, do, lam, k_lens=lens)
+    _check_backward(got, q, k, v, out, do, lam, clamped)
+    to = torch.randperm(B, generator=g).cuda()
+    moved = rt.attn_diff(q[to], k[to], v[to], lam, k_lens=lens[to])
+    for x, y in zip(moved, out):
+        assert torch.equal(x, y[to])
+    for x, y in zip(rt.attn_diff_backward(q[to], k[to], v[to], *moved, do[to], lam, k_lens=lens[to])[:3], got):
+        assert torch.equal(x, y[to])
+
+
 @pytest.mark.parametrize("D", [64, 72])
 @pytest.mark.parametrize("Tq", [5, 70, 300])
 def test_running_max_moves(gpu, Tq, D):
