@@ -20,6 +20,9 @@
 // The products are transposed as in attn_grad_tiles.h: a 32x32x16 accumulator hands each lane 16 rows of the side
 // read from LDS for one own row, which is what the B operand of the next product takes, so that P and dS never leave
 // registers; they are rounded to bf16 there, as the matrix products take them.  Scores, statistics and sums are fp32.
+// That rounding puts 0.0020 of O's norm beside the 0.0017 of O's own (the maps' errors add up where what their outputs have
+// in common cancels); a second product with what the rounding left would take a third to a half longer (2 samples of 15 heads
+// 17776 tokens 6.56 -> 10.0 ms, one head of 4096 35 -> 49 us).  diff_few, which waits for memory, makes it.
 //
 // Bound by the matrix cores and vector issue under the power limit, as plain attention is: 2 samples of 15 heads, 17776
 // tokens, D = 64 take 6.7 to 7.1 ms (1.03 to 1.09 PFLOP/s of 12 D; matrix cores busy 55 % at 1.7 GHz, 176 vector
@@ -617,8 +620,9 @@ diff_fwd(DiffArgs a, int n_items) {
 }
 
 // Up to 16 queries of a head, as diff_fwd's KEYS: map 1's in columns 0 .. 15 of the 32x32 products, map 2's in the others,
-// so that a chunk takes one softmax and V's products once (16 matrix products and 16 exponentials a lane instead of 24 and
-// 32).  Both maps' scores come out of one accumulator: the operand of a map's queries is zero in the other's columns, where
+// so that a chunk takes one softmax and V's products once (24 matrix products and 16 exponentials a lane, where two maps
+// apart would make 40 and 32).  Probabilities go into the products in two bf16 pieces, which leaves the error to O's own
+// rounding (8 x 15 tokens over up to 8192 keys 35.0 -> 36.2 us, 53.6 either way with keys and values cold).  Both maps' scores come out of one accumulator: the operand of a map's queries is zero in the other's columns, where
 // a key that is not finite in one map makes the other's statistics NaN (its output is NaN either way).
 template <int D, bool STATS, bool SPLIT>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_few(DiffArgs a, int n_items) {
@@ -710,21 +714,29 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         const float mc = m_run * c2;
         float sum[2] = {0.f, 0.f};
-        uint32_t pk[8];
+        uint32_t pk[8], rest[8];
 #pragma unroll
         for (int x = 0; x < 16; x += 2) {
             const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -mc));
             const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -mc));
             sum[(x >> 1) & 1] += e0 + e1;
             pk[x / 2] = pack_bf16(e0, e1);
+            rest[x / 2] = pack_bf16(e0 - lo_f(pk[x / 2]), e1 - hi_f(pk[x / 2]));
         }
         l_run += sum[0] + sum[1];
 #pragma unroll
-        for (int p = 0; p < 8; ++p) acc[p & 3] = mma(rd.w_col(cv, p & 3, p >> 2), op(pk, p >> 2), acc[p & 3]);
+        for (int p = 0; p < 8; ++p) {
+            const bf16x8 v = rd.w_col(cv, p & 3, p >> 2);
+            acc[p & 3] = mma(v, op(pk, p >> 2), acc[p & 3]);
+            acc[p & 3] = mma(v, op(rest, p >> 2), acc[p & 3]);
+        }
         if (TAIL) {
             const bf16x8 v = rd.w_col_tail(cv);
             uint32_t y[8];
             halves(pk, y);
+            tacc[0] = mma16(v, op(y, 0), tacc[0]);
+            tacc[1] = mma16(v, op(y, 1), tacc[1]);
+            halves(rest, y);
             tacc[0] = mma16(v, op(y, 0), tacc[0]);
             tacc[1] = mma16(v, op(y, 1), tacc[1]);
         }
