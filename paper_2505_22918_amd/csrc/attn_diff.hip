@@ -258,11 +258,34 @@ typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 // samples): those of the samples with most keys first, so that the longest walks begin first, and each XCD takes an eighth
 // of every sample's tiles, in tiles that follow one another (9 heads of 7238 tokens and fewer keys 391 -> 264 us, gradients
 // of 25 heads of 4789 760 -> 572).  Else heads of the samples in turn, an eighth of all tiles to an XCD.
-
+__device__ __forceinline__ int keys_in(const DiffArgs& a, int n) { return n < 0 ? 0 : (n > a.Tk ? a.Tk : n); }
+// by_len: the sample with the r-th most keys, and their number
+__device__ __forceinline__ int sample_of(const DiffArgs& a, int r, int& keys) {
+    const int lane = threadIdx.x & 63, mine = lane < a.B ? keys_in(a, a.k_lens[lane]) : 0;
+    int rank = lane < a.B ? 0 : 64;
+    for (int b = 0; b < a.B; ++b) {
+        const int other = __builtin_amdgcn_readlane(mine, b);
+        rank += other > mine || (other == mine && b < lane);
+    }
+    const int b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == r));
+    keys = __builtin_amdgcn_readlane(mine, b);
+    return b;
+}
+// The n-th head to be taken, b H + h, and its keys.
+__device__ __forceinline__ int head_of(const DiffArgs& a, int n, int& keys) {
+    if (a.by_len) {
+        const int r = n / a.H;
+        return sample_of(a, r, keys) * a.H + n - r * a.H;
+    }
+    const int h = n / a.B, b = n - h * a.B;
+    keys = a.k_lens ? keys_in(a, a.k_lens[b]) : a.Tk;
+    return b * a.H + h;
+}
 // Workgroups of an XCD for n items, and the item of workgroup g, or -1: an XCD has every eighth workgroup.
 __host__ __device__ inline int per_xcd(const DiffArgs& a, int n) {
     return a.by_len ? a.B * ((n / a.B + 7) / 8) : (n + 7) / 8;
 }
+__device__ __forceinline__ int eighth(int x, int n) { return (int)((int64_t)x * n / 8); }
 __device__ __forceinline__ int item_of(const DiffArgs& a, int g, int n) {
     int x = g & 7, j = g >> 3, m = n, before = 0;
     if (a.by_len) {
@@ -272,26 +295,30 @@ __device__ __forceinline__ int item_of(const DiffArgs& a, int g, int n) {
         j -= r * per;
         before = r * m;
     }
-    j += (int)((int64_t)x * m / 8);
-    return j < (int)((int64_t)(x + 1) * m / 8) ? before + j : -1;
+    j += eighth(x, m);
+    return j < eighth(x + 1, m) ? before + j : -1;
 }
-__device__ __forceinline__ int keys_in(const DiffArgs& a, int n) { return n < 0 ? 0 : (n > a.Tk ? a.Tk : n); }
-// The n-th head to be taken, b H + h, and its keys.
-__device__ __forceinline__ int head_of(const DiffArgs& a, int n, int& keys) {
-    if (a.by_len) {
-        const int lane = threadIdx.x & 63, r = n / a.H, mine = lane < a.B ? keys_in(a, a.k_lens[lane]) : 0;
-        int rank = lane < a.B ? 0 : 64;
-        for (int b = 0; b < a.B; ++b) {
-            const int other = __builtin_amdgcn_readlane(mine, b);
-            rank += other > mine || (other == mine && b < lane);
-        }
-        const int b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(rank == r));
-        keys = __builtin_amdgcn_readlane(mine, b);
-        return b * a.H + n - r * a.H;
+// The same for items of which only those of a head's tiles below `full` have work, of n_tile in parts of `split`: an XCD
+// takes an eighth of these and then one of the others, so that a head over many XCDs leaves none without work
+// (gradients of a head of 4000 tokens and one of 1550 keys 126 -> 84 us, of 45 heads of 700 52 -> 46).
+__host__ __device__ inline int per_xcd_k(const DiffArgs& a, int n) { return per_xcd(a, n) + (a.by_len ? a.B : 0); }
+// by_len; also the item's head and keys
+__device__ __forceinline__ int item_of_k(const DiffArgs& a, int g, int n, int n_tile, int split, int& bh, int& keys) {
+    const int m = n / a.B, per = (m + 7) / 8 + 1, r = (g >> 3) / per, x = (g + r) & 7;
+    int j = (g >> 3) - r * per;
+    const int b = sample_of(a, r, keys);
+    int first = 0, tiles = (keys + kDiffRows - 1) / kDiffRows, of = a.H * tiles * split;
+    if (const int here = eighth(x + 1, of) - eighth(x, of); j >= here) {
+        j -= here;
+        first = tiles;
+        tiles = n_tile - tiles;
+        of = a.H * tiles * split;
     }
-    const int h = n / a.B, b = n - h * a.B;
-    keys = a.k_lens ? keys_in(a, a.k_lens[b]) : a.Tk;
-    return b * a.H + h;
+    j += eighth(x, of);
+    if (j >= eighth(x + 1, of)) return -1;
+    const int h = j / (tiles * split);
+    bh = b * a.H + h;
+    return r * m + (h * n_tile + first) * split + j - h * tiles * split;
 }
 
 // ---- forward -------------------------------------------------------------------------------
@@ -1047,7 +1074,7 @@ constexpr int SUMS = (KV ? 32 : 16) + (D == 72 ? (KV ? 4 : 2) : 0);
 // which four take the first half of each stage and four the other, and join their sums in LDS.  SPLIT: against a part
 // of the other side.
 template <int D, bool KV, int BS, bool TWO, bool SPLIT, bool SHORT>
-__device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int item, int part) {
+__device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int item, int part, int tile, int bh, int keys) {
     constexpr int W = kDiffRows / 32;
     static_assert(!TWO || BS == 64, "a half to each four waves");
     using R = DiffRing<D, TWO ? 2 * W : W, BS, KV && !SHORT>;
@@ -1056,11 +1083,8 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
     constexpr int NB = R::NB, WB = R::WB, NW = KV ? 4 : 1;
     constexpr bool TAIL = D == 72;
     const int T = KV ? a.Tk : a.Tq, Tx = KV ? a.Tq : a.Tk;  // rows of the own side and of the other
-    const int n_tile = (T + 32 * W - 1) / (32 * W), head = item / n_tile;
-    int keys;
-    const int bh = head_of(a, head, keys);
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wave = TWO ? w % W : w, half = TWO ? w / W : 0;
-    const int row0 = ((item - head * n_tile) * W + wave) * 32;
+    const int row0 = (tile * W + wave) * 32;
     const int own_end = KV ? keys : T, x_end = KV ? Tx : keys;
     const int tile0 = row0 - 32 * wave;
     int n_st = (x_end + BS - 1) / BS;
@@ -1332,17 +1356,25 @@ __global__ __launch_bounds__(TWO ? 512 : 256) __attribute__((amdgpu_waves_per_eu
     const int ahead = 8 * (a.q_first ? per_q : per_k);
     const bool kv = (g < ahead) != (a.q_first != 0);
     if (g >= ahead) g -= ahead;
-    const int split = kv ? a.split_k : a.split_q;
-    int item = item_of(a, g, kv ? n_k : n_q), part = 0;
-    if (item < 0) return;
-    if (SPLIT) {
-        part = item % split;
-        item /= split;
-    }
+    auto walk = [&](auto side) {
+        constexpr bool KV = decltype(side)::value;
+        const int split = KV ? a.split_k : a.split_q, n_tile = ((KV ? a.Tk : a.Tq) + kDiffRows - 1) / kDiffRows;
+        int bh = 0, keys = 0, part = 0;
+        const bool some = KV && a.by_len;  // of a head's tiles have work
+        int item = some ? item_of_k(a, g, n_k, n_tile, split, bh, keys) : item_of(a, g, KV ? n_k : n_q);
+        if (item < 0) return;
+        if (SPLIT) {
+            part = item % split;
+            item /= split;
+        }
+        const int head = item / n_tile, tile = item - head * n_tile;
+        if (!some) bh = head_of(a, head, keys);
+        diff_walk<D, KV, KV ? BS_K : 64, TWO, SPLIT, SHORT>(a, lds, item, part, tile, bh, keys);
+    };
     if (kv)
-        diff_walk<D, true, BS_K, TWO, SPLIT, SHORT>(a, lds, item, part);
+        walk(std::integral_constant<bool, true>{});
     else
-        diff_walk<D, false, 64, TWO, SPLIT, SHORT>(a, lds, item, part);
+        walk(std::integral_constant<bool, false>{});
 }
 
 // Sums of a tile's parts: dK_1, dK_2, the halves of dV (kind 0 .. 3; `tiles_k` of them in x), then dQ_1, dQ_2 (4, 5);
@@ -1392,7 +1424,7 @@ hipError_t launch_bwd_d(const DiffArgs& a, hipStream_t stream) {
     }
     const int tiles_k = a.n_bh * ((a.Tk + kDiffRows - 1) / kDiffRows), tiles_q = a.n_bh * ((a.Tq + kDiffRows - 1) / kDiffRows);
     const bool split = a.split_k > 1 || a.split_q > 1;
-    const int n_k = tiles_k * a.split_k, n_q = tiles_q * a.split_q, per_k = per_xcd(a, n_k), per_q = per_xcd(a, n_q);
+    const int n_k = tiles_k * a.split_k, n_q = tiles_q * a.split_q, per_k = per_xcd_k(a, n_k), per_q = per_xcd(a, n_q);
     const int n_lam = a.lam_step ? a.H : 1;
     const dim3 grid(((n_lam + 7) & ~7) + 8 * per_k + 8 * per_q);
     auto run = [&](auto kernel, int threads) {
