@@ -8,7 +8,7 @@
 //   diff_fwd    32 queries of both maps to a wave: one pass over the keys, V read once for both
 //   diff_few    the same for up to 16 queries, the maps side by side in a product's columns
 //   diff_join   the parts of split walks
-//   diff_rows   per query row: log2 of both denominators, -delta_2, delta_2 - delta_1
+//   diff_rows   per query row: log2 of both denominators, -delta_2, delta_2 - delta_1; per 16 rows the sum of -delta_2
 //   diff_bwd    dK_1, dK_2 and dV of 128 keys, or dQ_1 and dQ_2 of 128 queries, to a workgroup of four waves; dlam
 //   diff_sum    the parts of split walks
 //
@@ -298,11 +298,11 @@ __device__ __forceinline__ int item_of(const DiffArgs& a, int g, int n) {
     j += eighth(x, m);
     return j < eighth(x + 1, m) ? before + j : -1;
 }
-// The same for items of which only those of a head's tiles below `full` have work, of n_tile in parts of `split`: an XCD
-// takes an eighth of these and then one of the others, so that a head over many XCDs leaves none without work
-// (gradients of a head of 4000 tokens and one of 1550 keys 126 -> 84 us, of 45 heads of 700 52 -> 46).
+// The same (by_len) for tiles of keys, n_tile a head in parts of `split`; also the item's head and keys.  Those past a
+// sample's keys have no work: an XCD takes an eighth of the others and then an eighth of these, so that a head over many
+// XCDs leaves none of them idle (gradients of a head of 4000 tokens and one of 1550 keys 126 -> 84 us, of 45 heads of 700
+// 52 -> 46).
 __host__ __device__ inline int per_xcd_k(const DiffArgs& a, int n) { return per_xcd(a, n) + (a.by_len ? a.B : 0); }
-// by_len; also the item's head and keys
 __device__ __forceinline__ int item_of_k(const DiffArgs& a, int g, int n, int n_tile, int split, int& bh, int& keys) {
     const int m = n / a.B, per = (m + 7) / 8 + 1, r = (g >> 3) / per, x = (g + r) & 7;
     int j = (g >> 3) - r * per;
