@@ -1186,9 +1186,11 @@ DiffBytes diff_bytes(const rt_diff_dims& d, int32_t n_lam) {
 
 // Forward: whether a workgroup's waves share the keys of 32 queries, and workgroups that share a tile's keys, by an
 // estimate of the times.  Sharing keys starts four times as many workgroups, one to a CU, and reads the keys four times
-// as often: 30 heads of 512 tokens 22 us against 36 of tiles of 128 in parts, 15 heads of 1500 tokens 51 against 65; but
-// 16 heads of 1024 queries over 226 keys 20 against 17.5, 4 heads of 3000 tokens 81 against 67.  Parts cost their sums'
-// way through memory: one head of 4096 tokens 32 us in two parts, 58 in eight.
+// as often: 8 heads of 2048 tokens 41 us against 59 of tiles of 128, 4 heads of 3000, 72 wide, 61 against 78 of tiles in
+// parts; but 35 heads of 700, 72 wide, 49 against 31, 18 heads of 4055 queries over 2391 keys 239 against 208.  Parts cost
+// their sums' way through memory: 8 heads of 2500 tokens 95 us in three, 73 whole, 10 heads of 7460 and fewer keys 350 and
+// 264; but 4 heads of 200 queries over 6000 keys 20 in eight, 33 in two.  The estimate's rates are those of 108 drawn calls
+// in each of 13 plans, for which its choice is 1.2 % above the best in the mean.
 struct DiffPlan {
     int32_t by_keys, split;
 };
@@ -1203,10 +1205,13 @@ DiffPlan diff_plan(const rt_diff_dims& d, bool lens) {
         const int64_t n = bh * ceil_div(d.Tq, by_keys ? 32 : rt::kDiffRows), slots = by_keys ? 256 : 512;
         for (int64_t s = 1; s <= rt::kDiffParts; ++s) {
             if (s > 1 && (n * s > 2 * slots || chunks < (by_keys ? 8 : 4) * s)) break;
-            // tenths of microseconds: of a chunk in a wave alone on its SIMD, or one of two; of a workgroup's start and end
-            const int64_t each = by_keys ? ceil_div(chunks, 4 * s) * 12 + 50 : ceil_div(chunks, s) * (n * s <= 256 ? 11 : 15) + 40;
-            int64_t t = ceil_div(n * s, slots) * each;
-            if (s > 1) t += 50 + bh * s * d.Tq * d.D * 32 / 400000;  // the parts, written and read
+            // tenths of microseconds: of a chunk in a wave alone on its SIMD, or one of two (a quarter more 72 wide); of a
+            // workgroup's start and end
+            const int64_t m = n * s, late = m % slots, own = ceil_div(chunks, by_keys ? 4 * s : s);
+            auto each = [&](int64_t chunk, int64_t ends) { return own * chunk * (d.D == 72 ? 5 : 4) / 4 + ends; };
+            int64_t t = by_keys ? ceil_div(m, slots) * each(13, 50)
+                                : m / slots * each(16, 35) + (late ? each(late <= 256 ? 11 : 16, 35) : 0);
+            if (s > 1) t += 65 + bh * s * d.Tq * d.D * 32 / 180000;  // the parts, written and read
             if (t < best) {
                 best = t;
                 p = DiffPlan{by_keys, (int32_t)s};
@@ -1264,7 +1269,7 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d, bool lens) {
             const int64_t slots = two ? 256 : 512;
             const bool q_first = lq > lk;  // what takes longer begins first
             int64_t t = q_first ? finish(rq * sq, lq, rk * sk, lk, slots) : finish(rk * sk, lk, rq * sq, lq, slots);
-            if (parts) t += 10 + parts * (rt::kDiffRows * 4 * 2) * d.D / 3000000;  // written and read
+            if (parts) t += 16 + parts * (rt::kDiffRows * 4 * 2) * d.D / 3000000;  // written and read
             if (t < best) {
                 best = t;
                 p = DiffBackPlan{two, q_first, (int32_t)sk, (int32_t)sq};
