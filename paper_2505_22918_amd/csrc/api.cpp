@@ -1188,7 +1188,7 @@ DiffBytes diff_bytes(const rt_diff_dims& d, int32_t n_lam) {
 // estimate of the times.  Sharing keys starts four times as many workgroups, one to a CU, and reads the keys four times
 // as often: 8 heads of 2048 tokens 41 us against 59 of tiles of 128, 4 heads of 3000, 72 wide, 61 against 78 of tiles in
 // parts; but 35 heads of 700, 72 wide, 49 against 31, 18 heads of 4055 queries over 2391 keys 239 against 208.  Parts cost
-// their sums' way through memory: 8 heads of 2500 tokens 95 us in three, 73 whole, 10 heads of 7460 and fewer keys 350 and
+// their sums' way through memory: 8 heads of 2500 tokens 95 us in three, 73 whole, 6 heads of 7460 and fewer keys 350 and
 // 264; but 4 heads of 200 queries over 6000 keys 20 in eight, 33 in two.  The estimate's rates are those of 108 drawn calls
 // in each of 13 plans, for which its choice is 1.2 % above the best in the mean.
 struct DiffPlan {
@@ -1220,8 +1220,9 @@ DiffPlan diff_plan(const rt_diff_dims& d, bool lens) {
     }
     return p;
 }
-int64_t diff_workspace(const rt_diff_dims& d, const DiffPlan& p) {
-    const int64_t s = p.split;
+// The larger need of calls with and without numbers of keys, which is what every call is given.
+int64_t diff_workspace(const rt_diff_dims& d) {
+    const int64_t s = std::max(diff_plan(d, false).split, diff_plan(d, true).split);
     return std::max<int64_t>(16, s > 1 ? (int64_t)d.B * d.H * s * 2 * d.Tq * (2 * d.D + 3) * 4 : 0);
 }
 
@@ -1242,8 +1243,9 @@ int64_t finish(int64_t n1, int64_t l1, int64_t n2, int64_t l2, int64_t slots) {
 // estimate of when the last workgroup ends.  Eight waves to a tile, two to a SIMD where there is a tile to a CU: 16 heads
 // of 1024 tokens, 72 wide, 60 us against 73, one head of 4096 56 against 62; but 15 heads of 1500 tokens 100 against 84.
 // Parts, of either side's walks: 15 heads of 2734 queries over 1175 keys and fewer 137 -> 97 us, 32 heads of 4096 queries
-// over 226 keys and fewer 283 -> 103 (their dK and dV are 64 tiles of 128 chunks each), the other way round (200 queries
-// over 6000 keys) 104 -> 34.
+// over 226 keys and fewer 283 -> 95 (their dK and dV are 64 tiles of 128 chunks each), the other way round (200 queries
+// over 6000 keys) 104 -> 34; but 8 heads of 961 queries over 3723 keys, 72 wide, 119 against 103 whole.  The estimate's
+// rates are fitted to 273 drawn calls in up to 24 plans each, for which its choice is 1.6 % above the best in the mean.
 struct DiffBackPlan {
     int32_t two, q_first, split_k, split_q;
 };
@@ -1254,9 +1256,8 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d, bool lens) {
     // half microseconds: of a walk's chunks of 32 rows, two waves to a SIMD
     const int64_t wk = 4 * ceil_div(d.Tq, 32), wq = 3 * ceil_div(d.Tk, 32);
     const int64_t longest = std::max(wk, wq);
-    // where samples have numbers of keys of their own, tiles and parts are counted as if seven eighths had work (12 heads of
-    // 3000 tokens and fewer keys 195 us as if all had, 167 seven eighths or six; 24 heads of 1542 119 as if all, 119, 126)
-    const int64_t share = lens ? 7 : 8, rk = ceil_div(nk * share, 8), rq = ceil_div(nq * share, 8);
+    // where samples have numbers of keys of their own, tiles are counted as if seven eighths had work, parts as if five did
+    const int64_t share = lens && d.B > 1 ? 7 : 8, rk = ceil_div(nk * share, 8), rq = ceil_div(nq * share, 8);
     int64_t best = INT64_MAX;
     for (int two = 0; two < (nk + nq > 4096 ? 1 : 2); ++two) {
         for (int i = 1; i <= 32; ++i) {
@@ -1265,11 +1266,15 @@ DiffBackPlan diff_back_plan(const rt_diff_dims& d, bool lens) {
             // the parts in whole tiles of 128 x D; a gigabyte and a half of them at most
             const int64_t parts = (sk > 1 ? nk * sk * 4 : 0) + (sq > 1 ? nq * sq * 2 : 0);
             if (i > 1 && (part < 16 || parts > 40000)) break;
-            const int64_t lk = ceil_div(wk, sk * (two + 1)) + 20 + 6 * two, lq = ceil_div(wq, sq * (two + 1)) + 20 + 6 * two;
             const int64_t slots = two ? 256 : 512;
+            // of four waves' time for a walk, eight take two thirds, four alone on their CU seven eighths, a quarter more 72
+            // wide; its start and end, with the row values of short heads
+            const int64_t rate = (two ? 26 : (rk * sk + rq * sq <= 256 ? 34 : 40)) * (d.D == 72 ? 5 : 4);
+            const int64_t ends = (two ? 34 : 28) + (d.Tq <= rt::kDiffShort ? ceil_div(d.Tq, two ? 32 : 16) : 0);
+            const int64_t lk = ceil_div(wk, sk) * rate / 160 + ends, lq = ceil_div(wq, sq) * rate / 160 + ends;
             const bool q_first = lq > lk;  // what takes longer begins first
             int64_t t = q_first ? finish(rq * sq, lq, rk * sk, lk, slots) : finish(rk * sk, lk, rq * sq, lq, slots);
-            if (parts) t += 16 + parts * (rt::kDiffRows * 4 * 2) * d.D / 3000000;  // written and read
+            if (parts) t += t / 8 + 16 + parts * (lens ? 5 : 8) * rt::kDiffRows * d.D / 1300000;  // written and read
             if (t < best) {
                 best = t;
                 p = DiffBackPlan{two, q_first, (int32_t)sk, (int32_t)sq};
@@ -1287,8 +1292,12 @@ int64_t diff_part_k(const rt_diff_dims& d, int64_t split) {
 int64_t diff_part_q(const rt_diff_dims& d, int64_t split) {
     return (int64_t)d.B * d.H * ceil_div(d.Tq, rt::kDiffRows) * split * 2 * rt::kDiffRows * d.D;
 }
-int64_t diff_back_workspace(const rt_diff_dims& d, const DiffBackPlan& p) {
-    const int64_t parts = (p.split_k > 1 ? diff_part_k(d, p.split_k) : 0) + (p.split_q > 1 ? diff_part_q(d, p.split_q) : 0);
+int64_t diff_back_workspace(const rt_diff_dims& d) {
+    int64_t parts = 0;
+    for (bool lens : {false, true}) {
+        const DiffBackPlan p = diff_back_plan(d, lens);
+        parts = std::max(parts, (p.split_k > 1 ? diff_part_k(d, p.split_k) : 0) + (p.split_q > 1 ? diff_part_q(d, p.split_q) : 0));
+    }
     return std::max<int64_t>(16, (diff_vals(d) + diff_lam_part(d) + parts) * 4);
 }
 
@@ -1327,7 +1336,7 @@ rt_status diff_args(const void* q, const void* k, const void* v, const float* la
 rt_status rt_attn_diff_workspace(rt_diff_dims dims, int64_t* bytes) {
     if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
     RT_TRY(check_diff(dims));
-    *bytes = std::max(diff_workspace(dims, diff_plan(dims, false)), diff_workspace(dims, diff_plan(dims, true)));
+    *bytes = diff_workspace(dims);
     return ok();
 }
 
@@ -1347,7 +1356,7 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
         RT_TRY(check_stat(row_sum, "row_sum"));
     }
     const DiffPlan plan = diff_plan(dims, k_lens != nullptr);
-    const int64_t need = diff_workspace(dims, plan);
+    const int64_t need = plan.split > 1 ? diff_workspace(dims) : 0;
     a.split = plan.split;
     const void* ws = a.split > 1 ? workspace : nullptr;
     if (a.split > 1) {
@@ -1371,7 +1380,7 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
 rt_status rt_attn_diff_backward_workspace(rt_diff_dims dims, int64_t* bytes) {
     if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
     RT_TRY(check_diff(dims));
-    *bytes = std::max(diff_back_workspace(dims, diff_back_plan(dims, false)), diff_back_workspace(dims, diff_back_plan(dims, true)));
+    *bytes = diff_back_workspace(dims);
     return ok();
 }
 
@@ -1398,7 +1407,7 @@ rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, con
         RT_TRY(check_tensor(dv, "dv"));
     }
     const DiffBackPlan plan = diff_back_plan(dims, k_lens != nullptr);
-    const int64_t need = diff_back_workspace(dims, plan);
+    const int64_t need = diff_back_workspace(dims);
     if (rows && workspace_bytes < need)
         return fail(RT_ECAPACITY, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
     const DiffBytes n = diff_bytes(dims, n_lam);
