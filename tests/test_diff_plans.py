@@ -1,0 +1,32 @@
+"""Which plan a call of differential attention takes (CPU): the sizes of the GPU tests reach every kernel that is compiled,
+with a rule that goes by sizes alone and may be fitted anew."""
+
+import itertools
+
+import pytest
+
+import diff_plans
+import test_gpu_attn_diff as sizes
+import test_gpu_attn_diff_plans as plans
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    return diff_plans.build(str(tmp_path_factory.mktemp("diff_plans")))
+
+
+@pytest.mark.parametrize("case", plans.CASES, ids=lambda c: "-".join(str(x) for x in c[:5]))
+def test_sizes_take_the_plan_that_they_are_for(lib, case):
+    *dims, lens, kernel, parts, waves, walks = case
+    by_len = lens is not None and dims[0] > 1
+    for stats in (False, True):
+        assert diff_plans.forward(lib, *dims, lens is not None, stats) == (kernel, parts, by_len)
+    assert diff_plans.backward(lib, *dims, lens is not None) == (waves, walks, False, by_len)
+
+
+def test_every_plan_of_the_gradients_is_reached(lib):
+    """Each instance of diff_bwd, for both widths, and walks of either side and of both in parts."""
+    calls = [(*s, D, False) for s in sizes.SIZES for D in (64, 72)] + [(*c[:5], c[5] is not None) for c in plans.CASES]
+    bwd = {(c[4],) + diff_plans.backward(lib, *c)[:3] for c in calls}
+    walks = set(itertools.product((64, 72), (4, 8), ("", "k", "q", "kq"), (False,)))
+    assert bwd == walks | set(itertools.product((64, 72), (4, 8), ("",), (True,)))
