@@ -15,7 +15,7 @@ def lib(tmp_path_factory):
     return diff_plans.build(str(tmp_path_factory.mktemp("diff_plans")))
 
 
-@pytest.mark.parametrize("case", plans.CASES, ids=lambda c: "-".join(str(x) for x in c[:5]))
+@pytest.mark.parametrize("case", plans.CASES + [(*c[:5], None, *c[5:]) for c in plans.RAMPS], ids=lambda c: "-".join(str(x) for x in c[:5]))
 def test_sizes_take_the_plan_that_they_are_for(lib, case):
     *dims, lens, kernel, parts, waves, walks = case
     by_len = lens is not None and dims[0] > 1
@@ -24,9 +24,14 @@ def test_sizes_take_the_plan_that_they_are_for(lib, case):
     assert diff_plans.backward(lib, *dims, lens is not None) == (waves, walks, False, by_len)
 
 
-def test_every_plan_of_the_gradients_is_reached(lib):
-    """Each instance of diff_bwd, for both widths, and walks of either side and of both in parts."""
+def test_every_kernel_is_reached(lib):
+    """Each instance of diff_fwd, diff_few and diff_bwd, for both widths: test_sizes and test_plans call each size with and
+    without statistics."""
     calls = [(*s, D, False) for s in sizes.SIZES for D in (64, 72)] + [(*c[:5], c[5] is not None) for c in plans.CASES]
-    bwd = {(c[4],) + diff_plans.backward(lib, *c)[:3] for c in calls}
+    fwd, bwd = set(), set()
+    for c in calls:
+        fwd.add((c[4],) + diff_plans.forward(lib, *c)[:2])
+        bwd.add((c[4],) + diff_plans.backward(lib, *c)[:3])
+    assert fwd == set(itertools.product((64, 72), ("tile", "keys", "few"), (False, True)))
     walks = set(itertools.product((64, 72), (4, 8), ("", "k", "q", "kq"), (False,)))
     assert bwd == walks | set(itertools.product((64, 72), (4, 8), ("",), (True,)))

@@ -1,4 +1,4 @@
-"""Differential attention and its gradients by plans that a call can take, over walks of several stages,
+"""Differential attention and its gradients by each kernel and plan that a call can take, over walks of several stages,
 against the fp64 oracle.  test_diff_plans.py checks on the CPU that these sizes take the plans that they are here for."""
 
 import numpy as np
@@ -13,6 +13,17 @@ pytestmark = pytest.mark.gpu
 # B, H, Tq, Tk, D, numbers of keys or None; the forward kernel (tile: 128 queries to four waves, keys: the waves share 32
 # queries' keys) and whether it takes the keys in parts; waves to a tile of the gradients, and the walks in parts
 CASES = [
+    (1, 35, 700, 700, 64, None, "tile", False, 4, ""),
+    (1, 35, 700, 700, 72, None, "tile", False, 4, ""),
+    (3, 20, 200, 300, 64, (300, 7, 129), "tile", False, 4, ""),
+    (3, 20, 200, 300, 72, (40, 300, 129), "tile", False, 4, ""),
+    (1, 1, 124, 1405, 64, None, "tile", True, 8, "q"),
+    (2, 1, 50, 1407, 64, (300, 1407), "tile", True, 4, "q"),
+    (1, 2, 38, 1140, 72, (1005,), "tile", True, 4, "q"),
+    (2, 4, 1055, 3733, 64, None, "tile", True, 4, "q"),
+    (3, 3, 897, 2568, 72, None, "tile", True, 4, "q"),
+    (8, 2, 823, 2975, 64, (700, 2975, 0, 1, 2001, 2975, 64, 1299), "tile", True, 8, "q"),
+    (2, 2, 2747, 2747, 72, (2747, 1100), "tile", True, 4, "kq"),
     (1, 2, 1008, 1008, 64, None, "keys", False, 8, "kq"),
     (1, 2, 1071, 1071, 72, None, "keys", False, 8, "kq"),
     (1, 4, 1108, 346, 64, None, "keys", False, 8, "k"),
@@ -83,3 +94,22 @@ def test_plans(gpu, case):
         on = _lens(lens)
         assert all(torch.equal(x, y) for x, y in zip(out, rt.attn_diff(q, k, v, lam, k_lens=on)))
         assert all(torch.equal(x, y) for x, y in zip(got, rt.attn_diff_backward(q, k, v, *out, do, lam, k_lens=on)))
+
+
+# scores that rise by hundreds from tile to tile, fall again, and lie far below zero: the running max moves in the middle of
+# a walk, in tiles of 128 queries whole and in parts , and in gradients of four waves and of eight
+RAMPS = [(1, 60, 200, 400, 64, "tile", False, 4, ""), (1, 60, 200, 400, 72, "tile", False, 4, ""), (1, 1, 124, 1405, 64, "tile", True, 8, "q"),
+         (3, 3, 897, 2568, 72, "tile", True, 4, "q"), (1, 2, 1008, 1008, 64, "keys", False, 8, "kq"), (1, 2, 1071, 1071, 72, "keys", False, 8, "kq")]
+
+
+@pytest.mark.parametrize("B,H,Tq,Tk,D", [c[:5] for c in RAMPS])
+def test_running_max_moves_in_every_kernel(gpu, B, H, Tq, Tk, D):
+    import torch
+
+    print(f"[diff plans] ramp B={B} H={H} Tq={Tq} Tk={Tk} D={D}", flush=True)
+    q, k, v, do, lam = _inputs(B, H, Tq, Tk, D, 9)
+    ramp = torch.linspace(-40, 60, Tk, device="cuda")
+    ramp[Tk // 2:3 * Tk // 4] = -50
+    q[..., 0], k[..., 0] = 4.0, ramp.bfloat16()
+    k[:, 1::2, :, 0] = ramp.flip(0).bfloat16()
+    _check(B, H, Tq, Tk, D, None, q, k, v, do, lam)
