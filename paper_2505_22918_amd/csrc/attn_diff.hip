@@ -649,8 +649,9 @@ diff_fwd(DiffArgs a, int n_items) {
 // Up to 16 queries of a head, as diff_fwd's KEYS: map 1's in columns 0 .. 15 of the 32x32 products, map 2's in the others,
 // so that a chunk takes one softmax and V's products once (24 matrix products and 16 exponentials a lane, where two maps
 // apart would make 40 and 32).  Probabilities go into the products in two bf16 pieces, which leaves the error to O's own
-// rounding (8 x 15 tokens over up to 8192 keys 35.0 -> 36.2 us, 53.6 either way with keys and values cold).  Both maps' scores come out of one accumulator: the operand of a map's queries is zero in the other's columns, where
-// a key that is not finite in one map makes the other's statistics NaN (its output is NaN either way).
+// rounding (8 x 15 tokens over up to 8192 keys 35.0 -> 36.2 us, 53.6 either way with keys and values cold).  The maps'
+// scores come out of accumulators of their own, of which a lane takes its map's: one for both, with zeros for the other
+// map's queries, would give 0 times a key that is not finite in one map to the other (36.3 us for 36.7).
 template <int D, bool STATS, bool SPLIT>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void diff_few(DiffArgs a, int n_items) {
     constexpr int BS = 32, STEP = 4;
@@ -709,13 +710,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         ring.turn();
         ring.load(R::STAGE - st, (s + STEP) * BS);
         const int cv = st + R::WIDE;
-        f32x16 sc = {};
+        f32x16 both[2] = {};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sc = mma(rd.n_row(st + i * R::NT, k), q[i][k], sc);
-            if (TAIL) sc = mma(rd.n_row_tail(st + i * R::NT, R::ZERO), q_tail[i], sc);
+            for (int k = 0; k < 4; ++k) both[i] = mma(rd.n_row(st + i * R::NT, k), q[i][k], both[i]);
+            if (TAIL) both[i] = mma(rd.n_row_tail(st + i * R::NT, R::ZERO), q_tail[i], both[i]);
         }
+        f32x16 sc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) sc[x] = map ? both[1][x] : both[0][x];
         if ((s + 1) * BS > keys) {
             const int lim = keys - s * BS - 4 * rd.hi;
 #pragma unroll
