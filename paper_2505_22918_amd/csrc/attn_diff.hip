@@ -133,11 +133,8 @@ struct Reads {
         return SWZ ? tr_read(p + (w_tr ^ (64 * dt)), p + 8 * WB + (w_tr ^ (64 * dt) ^ 32))
                    : tr_read(p + w_tr + 64 * dt, p + 8 * WB + w_tr + 64 * dt);
     }
-    // narrow rows' last 8 elements for map i: in rows 8 i .. + 7 of the product, zeros in the others
-    __device__ __forceinline__ bf16x8 n_col_tail(int base, int i, int zero) const {
-        const bool mine = ((lane >> 1) & 1) == i;
-        return tr_read(lds + (mine ? base + n_t : zero), lds + (mine ? base + n_t + 8 * NB : zero));
-    }
+    // narrow rows' last 8 elements, in rows 0 .. 7 of the product and again in 8 .. 15
+    __device__ __forceinline__ bf16x8 n_col_tail(int base) const { return tr_read(lds + base + n_t, lds + base + n_t + 8 * NB); }
     __device__ __forceinline__ bf16x8 w_col_tail(int base) const { return tr_read(lds + base + w_t, lds + base + w_t + 8 * WB); }
 
     // rows row0 .. + 31 of x (zeros from row `end` on): lane holds row l32, elements 16 s + 8 hi ..
@@ -1238,12 +1235,18 @@ __device__ __forceinline__ void diff_walk(const DiffArgs& a, lds_u8* lds, int it
                         soft(i, sc, [](int) {});
 #pragma unroll
                         for (int k = 0; k < 4; ++k) grad(i, k);
-                        // (zeros meet the other map's NaN: a row that has one has it in both, through its delta)
-                        const bf16x8 c = rd.n_col_tail(cx + i * R::NT, i, R::ZERO);
+                        // Map i's rows of the product are lanes 32 i .. + 31; the others keep theirs.  (Zeros for the other map's
+                        // rows would need no choice, but make NaN of this map's NaN there: 9.00 ms for 8.87, 16 heads of 16384
+                        // tokens.  Accumulators for each map, with 4 registers spilled: 8.99, 88 heads of 4 queries 522 us for 505.)
+                        const bf16x8 c = rd.n_col_tail(cx + i * R::NT);
                         uint32_t z[8];
                         halves(ds[i], z);
-                        tacc[0] = mma16(c, op(z, 0), tacc[0]);
-                        tacc[1] = mma16(c, op(z, 1), tacc[1]);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const f32x4 t = mma16(c, op(z, h), tacc[h]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) tacc[h][e] = rd.hi == i ? t[e] : tacc[h][e];
+                        }
                         if (KV) __builtin_amdgcn_sched_barrier(0);  // else registers spill
                     }
                 }

@@ -1,4 +1,4 @@
-"""Values of one map that are not finite stay out of the other map's statistics and output."""
+"""Values of one map that are not finite stay out of the other map's statistics, output and gradients."""
 
 import numpy as np
 import pytest
@@ -44,3 +44,41 @@ def test_a_bad_query_stays_in_its_map(gpu, Tq, Tk, D):
     _within(o2[0], ref[1], tol[1], "o2")
     _within(top[1], ref[2][1], tol[2][1], "max")
     _within(total[1], ref[3][1], tol[3][1], "sum")
+
+
+# ---- gradients: those of the second map's queries and keys do not depend on the first (dS_2 = -lam P_2 (dA - dO . O_2)) ----
+
+# (in one launch, by four waves and eight, whole and in parts)
+GRAD_SIZES = [(1, 1, 40), (1, 9, 3000), (2, 17, 300), (1, 100, 70), (2, 200, 300), (1, 300, 40), (1, 129, 700), (2, 1040, 1040), (40, 300, 130)]
+
+
+def _second_map(q, k, v, do, lam, bad_q, bad_k):
+    """dq and dk of the last head's second map and its dlam with values of the first that are not finite, against those
+    without."""
+    n = [_np(x) for x in (q, k, v, do, lam)]
+    H, Tk, h = v.shape[1], v.shape[2], v.shape[1] - 1
+    maps = slice(2 * h, 2 * h + 2)
+    o = _np(rt.attn_diff(q, k, v, lam)[0])[0, h]
+    out = rt.attn_diff(bad_q, bad_k, v, lam)
+    dq, dk, _, dlam = (_np(x) for x in rt.attn_diff_backward(bad_q, bad_k, v, *out, do, lam))
+    (_, _, m, l), _ = oh.forward(n[0][0, maps], n[1][0, maps], n[2][0, h], n[4][h], Tk)
+    m[1], l[1] = (_np(x)[0, 2 * h + 1] for x in out[2:])
+    o2 = _np(out[1])[0, h]
+    assert np.isfinite(o2).all() and np.isfinite(l).all()
+    ref, tol = oh.backward(n[0][0, maps], n[1][0, maps], n[2][0, h], o, o2, m, l, n[3][0, h], n[4][h], Tk)
+    _within(dq[0, 2 * h + 1], ref[0][1], tol[0][1], "dq")
+    _within(dk[0, 2 * h + 1], ref[1][1], tol[1][1], "dk")
+    _within(dlam[h], ref[3], tol[3], "dlam")
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("D", [64, 72])
+@pytest.mark.parametrize("H,Tq,Tk", GRAD_SIZES)
+def test_gradients_of_the_second_map_without_the_first(gpu, H, Tq, Tk, D, bad):
+    print(f"[diff other map] gradients H={H} Tq={Tq} Tk={Tk} D={D} bad={bad}", flush=True)
+    q, k, v, do, lam = _inputs(1, H, Tq, Tk, D, Tq + Tk)
+    bad_k, bad_q = k.clone(), q.clone()
+    bad_k[0, 2 * H - 2, Tk // 3, D - 3] = bad
+    bad_q[0, 2 * H - 2, Tq // 2, 7] = bad
+    _second_map(q, k, v, do, lam, q, bad_k)
+    _second_map(q, k, v, do, lam, bad_q, k)
