@@ -398,10 +398,10 @@ rt_status rt_rope_backward(const void* dy, const int64_t dy_stride[3], const voi
  * o: device bf16 [B][H][Tq][2 D] (written).  o2, row_max, row_sum: written together, or all NULL:
  * O_2, bf16 as o, and fp32 [B][2 H][Tq] the largest score m (divided by sqrt(D)) of each map's row
  * and its sum of exp(score - m); without keys -inf and 0.  P is rounded to bf16 for the matrix
- * products, whose sums are fp32.  Equal calls give equal bits.  workspace: device, 16-byte
- * aligned, of the bytes that rt_attn_diff_workspace reports, overwritten (parts of the keys where
- * there are few rows; it may be NULL where 16 are reported).  Outputs and workspace must not
- * overlap each other or an input.
+ * products, whose sums are fp32, as scores are (of any size that fp32 holds).  Equal calls give
+ * equal bits.  workspace: device, 16-byte aligned, of the bytes that rt_attn_diff_workspace reports,
+ * overwritten (parts of the keys where there are few rows; it may be NULL where 16 are reported).
+ * Outputs and workspace must not overlap each other or an input.
  * D is 64 or 72; B H < 2^23, 4 T D <= 2^30 and B H T (in whole 64) < 2^28 for T = Tq and Tk. */
 typedef struct {
     int32_t B, H, Tq, Tk, D;
@@ -417,7 +417,9 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
  *   dQ_i = dS_i K_i / sqrt(D), dK_i = dS_i^T Q_i / sqrt(D);  dlam = -sum of delta_2 over the
  * rows of each head, or of all.  o, o2, row_max, row_sum: of rt_attn_diff for these inputs; d_o:
  * as o; dq, dk, dv: as q, k, v (written; rows past k_lens 0); d_lam: device fp32 [n_lam]
- * (written).  Sums are fp32, dlam's 64-bit, in a fixed order: equal calls give equal bits. */
+ * (written).  Sums are fp32, dlam's 64-bit, in a fixed order: equal calls give equal bits.  What
+ * fp32 statistics leave open of an exponent is up to 2^-21 of its row's largest |score|: with scores
+ * past 2^16 P is off by percents, past 2^21 the gradients mean nothing and need not be finite. */
 rt_status rt_attn_diff_backward_workspace(rt_diff_dims dims, int64_t* bytes);
 rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, const float* lam, int32_t n_lam,
                                 const int32_t* k_lens, const void* o, const void* o2, const float* row_max,

@@ -1327,6 +1327,7 @@ rt_status diff_args(const void* q, const void* k, const void* v, const float* la
     a.n_bh = d.B * d.H;
     a.scale_nat = (float)(1.0 / std::sqrt((double)d.D));
     a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)d.D));
+    a.move = rt::kDiffMove / a.scale_log2;
     *out = a;
     return RT_OK;
 }

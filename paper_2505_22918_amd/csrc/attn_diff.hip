@@ -320,18 +320,24 @@ __device__ __forceinline__ int item_of_k(const DiffArgs& a, int g, int n, int n_
 
 // ---- forward -------------------------------------------------------------------------------
 
+// A running max further out than this has a product with c2 whose rounding shows in an exponent (at 2^40 it makes 0 or
+// infinity of the largest probability): these are then formed by differences of scores, exact where they matter.  In every
+// chunk that would be an instruction more for each; the test takes 0 to 1.5 % (2 samples of 15 heads, 17776 tokens 6.56 ->
+// 6.59 ms, one head of 4096 35.8 -> 36.3 us).  diff_few, which waits for memory, always forms them so (27.3 -> 27.7 us, 15
+// tokens over 17776 keys).
+constexpr float kFar = 65536.0f;
+constexpr float kLowest = -3.402823466e38f;  // of a running max; finite: a chunk without keys gives p = 0, not NaN
+
 // the part of a tile's rows for which a sample has no keys: its statistics alone, by which diff_join leaves the sums out
 template <int D>
 __device__ __forceinline__ void empty_part(const DiffArgs& a, int bh, int part, int row0, int rows) {
     const int map = threadIdx.x & 1, row = row0 + (threadIdx.x >> 1);
     if ((int)threadIdx.x >= 2 * rows || row >= a.Tq) return;
     float* x = a.part + (size_t)a.n_bh * a.split * 2 * a.Tq * (2 * D) + ((((size_t)bh * a.split + part) * 2 + map) * a.Tq + row) * 3;
-    x[0] = -1e30f;
+    x[0] = kLowest;
     x[1] = 0.f;
     x[2] = -INFINITY;
 }
-
-constexpr float kMove = 24.0f;  // the running max moves when a probability against it passes 2^kMove
 
 // A workgroup of four waves takes 32 queries to a wave, which share a ring of keys and values; or (KEYS, where there are
 // few tiles) 32 queries in all, the waves every fourth 32 keys each from rings of their own, and joins their sums in LDS.
@@ -388,7 +394,7 @@ diff_fwd(DiffArgs a, int n_items) {
 #pragma unroll
         for (int d = 0; d < 4; ++d) acc[i][d] = f32x16{};
         tacc[i][0] = tacc[i][1] = f32x4{};
-        m_run[i] = -1e30f;  // finite: a chunk without keys gives p = 0, not NaN
+        m_run[i] = kLowest;
         m_top[i] = -INFINITY;
         l_run[i] = 0.f;
     }
@@ -417,30 +423,32 @@ diff_fwd(DiffArgs a, int n_items) {
                 };
                 uint32_t pk[2][8];
                 // Probabilities of a map against its running max, a matrix product of the other's between two pairs of
-                // them; should one pass 2^kMove, the max moves and they are formed again.
+                // them; should one pass 2^24, the max moves and they are formed again, as where it lies far out.
                 auto soft = [&](int i, const f32x16& sc, auto&& product) {
                     float top = -INFINITY;
-                    auto form = [&](auto&& between) {
+                    auto form = [&](auto far, auto&& between) {
                         const float mc = m_run[i] * c2;
+                        auto p = [&](float s) {
+                            return __builtin_amdgcn_exp2f(decltype(far)::value ? (s - m_run[i]) * c2 : __builtin_fmaf(s, c2, -mc));
+                        };
                         float sum[2] = {0.f, 0.f};
 #pragma unroll
                         for (int x = 0; x < 16; x += 2) {
-                            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -mc));
-                            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -mc));
+                            const float e0 = p(sc[x]), e1 = p(sc[x + 1]);
                             sum[(x >> 1) & 1] += e0 + e1;
                             pk[i][x / 2] = pack_bf16(e0, e1);
                             between(x);
                         }
                         return sum[0] + sum[1];
                     };
-                    float sum = form([&](int x) {
+                    float sum = form(std::integral_constant<bool, false>{}, [&](int x) {
                         top = fmaxf(fmaxf(top, sc[x]), sc[x + 1]);
                         __builtin_amdgcn_sched_barrier(0);
                         product(x / 2);
                         __builtin_amdgcn_sched_barrier(0);
                     });
                     if (STATS) m_top[i] = fmaxf(m_top[i], top);
-                    if (__builtin_amdgcn_ballot_w64((top - m_run[i]) * c2 > kMove)) {
+                    if (__builtin_amdgcn_ballot_w64(top - m_run[i] > a.move) | __builtin_amdgcn_ballot_w64(fabsf(m_run[i]) > kFar)) {
                         const float to = fmaxf(m_run[i], pair_max(top));
                         const float alpha = __builtin_amdgcn_exp2f((m_run[i] - to) * c2);
                         m_run[i] = to;
@@ -451,7 +459,7 @@ diff_fwd(DiffArgs a, int n_items) {
                             tacc[i][0] *= tail_bcast(alpha, 0);
                             tacc[i][1] *= tail_bcast(alpha, 1);
                         }
-                        sum = form([](int) {});
+                        sum = form(std::integral_constant<bool, true>{}, [](int) {});
                     }
                     l_run[i] += sum;
                 };
@@ -698,7 +706,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
     for (int d = 0; d < 4; ++d) acc[d] = f32x16{};
     tacc[0] = tacc[1] = f32x4{};
-    float m_run = -1e30f, m_top = -INFINITY, l_run = 0.f;
+    float m_run = kLowest, m_top = -INFINITY, l_run = 0.f;
     // a value of each column as the tails' accumulators hold them: query lane % 16 of map i
     auto tail_bcast = [&](float x, int i) { return __int_as_float(__builtin_amdgcn_ds_bpermute((16 * i + (rd.lane & 15)) << 2, __float_as_int(x))); };
     const float c2 = a.scale_log2;
@@ -728,7 +736,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int x = 3; x < 15; x += 2) top = fmaxf(fmaxf(top, sc[x]), sc[x + 1]);
         top = fmaxf(top, sc[15]);
         if (STATS) m_top = fmaxf(m_top, top);
-        if (__builtin_amdgcn_ballot_w64((top - m_run) * c2 > kMove)) {
+        if (__builtin_amdgcn_ballot_w64(top - m_run > a.move)) {
             const float to = fmaxf(m_run, pair_max(top));
             const float alpha = __builtin_amdgcn_exp2f((m_run - to) * c2);
             m_run = to;
@@ -740,13 +748,11 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 tacc[1] *= tail_bcast(alpha, 1);
             }
         }
-        const float mc = m_run * c2;
         float sum[2] = {0.f, 0.f};
         uint32_t pk[8], rest[8];
 #pragma unroll
         for (int x = 0; x < 16; x += 2) {
-            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x], c2, -mc));
-            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[x + 1], c2, -mc));
+            const float e0 = __builtin_amdgcn_exp2f((sc[x] - m_run) * c2), e1 = __builtin_amdgcn_exp2f((sc[x + 1] - m_run) * c2);
             sum[(x >> 1) & 1] += e0 + e1;
             pk[x / 2] = pack_bf16(e0, e1);
             rest[x / 2] = pack_bf16(e0 - lo_f(pk[x / 2]), e1 - hi_f(pk[x / 2]));

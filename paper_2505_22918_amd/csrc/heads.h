@@ -35,6 +35,7 @@ __attribute__((weak)) hipError_t launch_rope(const RopeArgs& a, hipStream_t stre
 constexpr int kDiffRows = 128;  // rows of a tile of four waves
 constexpr int kDiffShort = 128;  // most rows of queries whose values a workgroup forms
 constexpr int kDiffParts = 32;  // parts of a tile's keys, at most
+constexpr float kDiffMove = 24.0f;  // the running max moves where a probability against it would pass 2^24
 struct DiffArgs {
     const uint16_t* q;  // bf16 [B, 2 H, Tq, D]
     const uint16_t* k;  // bf16 [B, 2 H, Tk, D]
@@ -45,6 +46,7 @@ struct DiffArgs {
     int32_t by_len;  // the samples with most keys first (B up to 64)
     int32_t B, H, Tq, Tk, n_bh;
     float scale_nat, scale_log2;
+    float move;  // the running max moves where a score is this far above it
     // forward
     uint16_t* o;    // bf16 [B, H, Tq, 2 D]
     uint16_t* o2;   // or null, with the statistics
