@@ -1221,8 +1221,8 @@ DiffPlan diff_plan(const rt_diff_dims& d, bool lens) {
     return p;
 }
 // The larger need of calls with and without numbers of keys, which is what every call is given.
-int64_t diff_workspace(const rt_diff_dims& d) {
-    const int64_t s = std::max(diff_plan(d, false).split, diff_plan(d, true).split);
+int64_t diff_workspace(const rt_diff_dims& d, const DiffPlan& one, const DiffPlan& other) {
+    const int64_t s = std::max(one.split, other.split);
     return std::max<int64_t>(16, s > 1 ? (int64_t)d.B * d.H * s * 2 * d.Tq * (2 * d.D + 3) * 4 : 0);
 }
 
@@ -1292,13 +1292,18 @@ int64_t diff_part_k(const rt_diff_dims& d, int64_t split) {
 int64_t diff_part_q(const rt_diff_dims& d, int64_t split) {
     return (int64_t)d.B * d.H * ceil_div(d.Tq, rt::kDiffRows) * split * 2 * rt::kDiffRows * d.D;
 }
-int64_t diff_back_workspace(const rt_diff_dims& d) {
-    int64_t parts = 0;
-    for (bool lens : {false, true}) {
-        const DiffBackPlan p = diff_back_plan(d, lens);
-        parts = std::max(parts, (p.split_k > 1 ? diff_part_k(d, p.split_k) : 0) + (p.split_q > 1 ? diff_part_q(d, p.split_q) : 0));
+// The plans of calls with and without numbers of keys, made once a call (up to 4 us of the host's time), and the larger need.
+struct DiffBackPlans {
+    DiffBackPlan of[2];  // [whether there are numbers of keys]
+    int64_t workspace;
+};
+DiffBackPlans diff_back_plans(const rt_diff_dims& d) {
+    DiffBackPlans r{{diff_back_plan(d, false), diff_back_plan(d, true)}, 16};
+    for (const DiffBackPlan& p : r.of) {
+        const int64_t parts = (p.split_k > 1 ? diff_part_k(d, p.split_k) : 0) + (p.split_q > 1 ? diff_part_q(d, p.split_q) : 0);
+        r.workspace = std::max(r.workspace, (diff_vals(d) + diff_lam_part(d) + parts) * 4);
     }
-    return std::max<int64_t>(16, (diff_vals(d) + diff_lam_part(d) + parts) * 4);
+    return r;
 }
 
 // What both calls check and set alike.
@@ -1337,7 +1342,7 @@ rt_status diff_args(const void* q, const void* k, const void* v, const float* la
 rt_status rt_attn_diff_workspace(rt_diff_dims dims, int64_t* bytes) {
     if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
     RT_TRY(check_diff(dims));
-    *bytes = diff_workspace(dims);
+    *bytes = diff_workspace(dims, diff_plan(dims, false), diff_plan(dims, true));
     return ok();
 }
 
@@ -1357,7 +1362,7 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
         RT_TRY(check_stat(row_sum, "row_sum"));
     }
     const DiffPlan plan = diff_plan(dims, k_lens != nullptr);
-    const int64_t need = plan.split > 1 ? diff_workspace(dims) : 0;
+    const int64_t need = plan.split > 1 ? diff_workspace(dims, plan, diff_plan(dims, k_lens == nullptr)) : 0;
     a.split = plan.split;
     const void* ws = a.split > 1 ? workspace : nullptr;
     if (a.split > 1) {
@@ -1381,7 +1386,7 @@ rt_status rt_attn_diff(const void* q, const void* k, const void* v, const float*
 rt_status rt_attn_diff_backward_workspace(rt_diff_dims dims, int64_t* bytes) {
     if (!bytes) return fail(RT_EINVAL, "bytes is NULL");
     RT_TRY(check_diff(dims));
-    *bytes = diff_back_workspace(dims);
+    *bytes = diff_back_plans(dims).workspace;
     return ok();
 }
 
@@ -1407,8 +1412,9 @@ rt_status rt_attn_diff_backward(const void* q, const void* k, const void* v, con
         RT_TRY(check_tensor(dk, "dk"));
         RT_TRY(check_tensor(dv, "dv"));
     }
-    const DiffBackPlan plan = diff_back_plan(dims, k_lens != nullptr);
-    const int64_t need = diff_back_workspace(dims);
+    const DiffBackPlans plans = diff_back_plans(dims);
+    const DiffBackPlan& plan = plans.of[k_lens != nullptr];
+    const int64_t need = plans.workspace;
     if (rows && workspace_bytes < need)
         return fail(RT_ECAPACITY, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes, (long long)need);
     const DiffBytes n = diff_bytes(dims, n_lam);

@@ -14,7 +14,10 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 NOTES = r"""
 #include <hip/hip_runtime_api.h>
+#include <algorithm>
+#include <chrono>
 #include "heads.h"
+#include "rettention.h"
 namespace rt {
 int seen[8];
 int64_t blocks;
@@ -33,6 +36,28 @@ hipError_t launch_diff_backward(const DiffArgs& a, int, hipStream_t) {
 }  // namespace rt
 extern "C" const int* rt_seen() { return rt::seen; }
 extern "C" int64_t rt_blocks() { return rt::blocks; }
+template <class F>
+static double least(F&& f) {
+    double best = 1e30;
+    for (int i = 0; i < 400; ++i) {
+        const auto t = std::chrono::steady_clock::now();
+        for (int j = 0; j < 10; ++j) f();
+        best = std::min(best, std::chrono::duration<double, std::micro>(std::chrono::steady_clock::now() - t).count() / 10);
+    }
+    return best;
+}
+// microseconds of the host: a question for the workspace, and the call itself
+extern "C" void rt_times(rt_diff_dims d, int backward, double* us) {
+    auto at = [](int64_t i) { return (void*)((i + 1) << 40); };
+    auto f = [&](int64_t i) { return (float*)at(i); };
+    int64_t n;
+    us[0] = least([&] { backward ? rt_attn_diff_backward_workspace(d, &n) : rt_attn_diff_workspace(d, &n); });
+    us[1] = least([&] {
+        backward ? rt_attn_diff_backward(at(0), at(1), at(2), f(3), 1, nullptr, at(5), at(6), f(7), f(8), at(9), d, at(10), at(11),
+                                         at(12), f(13), at(14), (int64_t)1 << 40, nullptr)
+                 : rt_attn_diff(at(0), at(1), at(2), f(3), 1, nullptr, d, at(5), at(6), f(7), f(8), at(9), (int64_t)1 << 40, nullptr);
+    });
+}
 """
 
 
@@ -51,6 +76,7 @@ def build(folder):
         fn.restype, fn.argtypes = res_type, args
     lib.rt_seen.restype = ctypes.POINTER(ctypes.c_int)
     lib.rt_blocks.restype = ctypes.c_int64
+    lib.rt_times.restype, lib.rt_times.argtypes = None, [_lib.RtDiffDims, ctypes.c_int, ctypes.POINTER(ctypes.c_double)]
     return lib
 
 
