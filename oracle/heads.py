@@ -64,9 +64,12 @@ def _scores(q, k, d, keys, x_tol=False):
     return s, (d + 8) * HALF_F32 * (np.abs(q) @ np.abs(k[:keys]).T / np.sqrt(d) + np.abs(s).max(initial=0.0) + 1.0)
 
 
-def forward(q, k, v, lam, keys):
-    """q, k: two maps [T,d] each; v [Tk, 2d].  (o, o2, m, l) with m, l [2,T], and their tolerances in the same order."""
+def forward(q, k, v, lam, keys, pieces=1, waves=1):
+    """q, k: two maps [T,d] each; v [Tk, 2d].  (o, o2, m, l) with m, l [2,T], and their tolerances in the same order.
+    pieces: the numbers of bf16 that a probability is taken in, each the rounding of what those before it leave.  waves: that
+    share the keys 32 by 32, each with a sum of its own."""
     d, out, tol, ms, ls, mt, lt = q[0].shape[1], [], [], [], [], [], []
+    adds = keys if waves == 1 else keys // waves + 32 + waves
     for i in range(2):
         s, e_s = _scores(q[i], k[i], d, keys, True)
         m = s.max(1, initial=-np.inf)
@@ -75,7 +78,7 @@ def forward(q, k, v, lam, keys):
         A = e / np.where(l > 0, l, 1.0)[:, None]
         out.append(A @ v[:keys])
         # probabilities rounded to bf16 against the running max, their sum not; both off by the scores' errors
-        rel = HALF_BF16 + 2 * e_s + keys * HALF_F32
+        rel = HALF_BF16 ** pieces + 2 * e_s + pieces * adds * HALF_F32
         tol.append((A * rel) @ np.abs(v[:keys]))
         ms.append(m)
         ls.append(l)
