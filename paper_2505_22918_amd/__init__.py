@@ -930,8 +930,8 @@ def rope(x, positions, plan: RopePlan, out=None):
     """Rotary positions: each pair of the first plan.rotated elements of x's rows is turned by the angle of its token's
     position; the other elements are copied.
 
-    x: bf16, fp16 or fp32 [B,H,T,D] with any row strides (queries and keys of a packed projection [B,T,3,H,D] in one
-    call: qkv[:, :, :2].flatten(2, 3).transpose(1, 2)).  positions: int32, int64 or fp32 [T], or [B,T] for each
+    x: bf16, fp16 or fp32 [B,H,T,D] with any row strides (queries out of a packed projection [B,T,3,H,D]:
+    qkv[:, :, 0].transpose(1, 2)).  positions: int32, int64 or fp32 [T], or [B,T] for each
     sample's own, with a last dimension of coordinates where the plan has several axes; at position 0 rows stay as they
     are (times the plan's amplitude).  Returns a new contiguous tensor or `out`: any row strides, x itself to rotate
     in place."""
