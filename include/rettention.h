@@ -368,9 +368,10 @@ rt_status rt_layer_norm_backward(const void* dy, const int64_t dy_stride[3], con
  * freq: device, rotated / 2 radians a position; axis: device, the same number of values from 0 to
  * axes - 1, or NULL where axes is 1.  y may be x with x's strides (in place); else no element of
  * y may share memory with another, with x or with another input.  2 <= D <= 16384, T D < 2^32,
- * B H < 2^31 and B ceil(T n / 256) < 2^24 for n threads a token: D / v for RT_ROPE_INTERLEAVED with v > 1, else
- * rotated / 2 / v + (D - rotated) / v, where v is 8, 4 or 1: the most elements, 16 bytes at most,
- * that all rows of x and y start on and D, and for RT_ROPE_HALF rotated / 2, are whole numbers of. */
+ * B H < 2^31 and B ceil(T n / 256) < 2^24 for n threads a token: D / v for RT_ROPE_INTERLEAVED with
+ * v > 1, else rotated / 2 / v + (D - rotated) / v, where v is 8, 4 or 1: the most elements, 16 bytes
+ * at most, that all rows of x and y start on and D, and for RT_ROPE_HALF rotated / 2, are whole
+ * numbers of. */
 enum { RT_ROPE_INTERLEAVED = 0, RT_ROPE_HALF = 1 };
 enum { RT_POS_I32 = 0, RT_POS_I64 = 1, RT_POS_F32 = 2 };
 typedef struct {

@@ -1017,8 +1017,9 @@ def attn_diff(q, k, v, lam, k_lens=None, stats=True, out=None):
 def attn_diff_backward(q, k, v, o, o2, row_max, row_sum, d_o, lam, k_lens=None, out=None):
     """Gradients (dq, dk, dv, d_lam) of differential attention for the gradient d_o of its output: o, o2, row_max and
     row_sum are attn_diff's for these q, k, v, lam and k_lens.  d_lam is fp32 of lam's shape, summed over the rows of
-    each head, or of all; dk and dv are 0 past a sample's keys.  out: three tensors to write dq, dk, dv into instead
-    of new ones."""
+    each head, or of all; dk and dv are 0 past a sample's keys.  Probabilities come from the fp32 statistics: rows with
+    scores past 2^16 lose percents of theirs, past 2^21 all.  out: three tensors to write dq, dk, dv into instead of new
+    ones."""
     torch = _torch()
     lib = _lib.load()
     dims, shape, rows, _, need = _diff_inputs(q, k, v, lam, k_lens)

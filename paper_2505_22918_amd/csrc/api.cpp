@@ -1186,11 +1186,11 @@ DiffBytes diff_bytes(const rt_diff_dims& d, int32_t n_lam) {
 
 // Forward: whether a workgroup's waves share the keys of 32 queries, and workgroups that share a tile's keys, by an
 // estimate of the times.  Sharing keys starts four times as many workgroups, one to a CU, and reads the keys four times
-// as often: 8 heads of 2048 tokens 41 us against 59 of tiles of 128, 4 heads of 3000, 72 wide, 61 against 78 of tiles in
-// parts; but 35 heads of 700, 72 wide, 49 against 31, 18 heads of 4055 queries over 2391 keys 239 against 208.  Parts cost
-// their sums' way through memory: 8 heads of 2500 tokens 95 us in three, 73 whole, 6 heads of 7460 and fewer keys 350 and
-// 264; but 4 heads of 200 queries over 6000 keys 20 in eight, 33 in two.  The estimate's rates are those of 108 drawn calls
-// in each of 13 plans, for which its choice is 1.2 % above the best in the mean.
+// as often: 8 heads of 2048 tokens 43 us against 60 of tiles of 128, 4 heads of 3000, 72 wide, 65 against 81 of tiles in
+// parts; but 35 heads of 700, 72 wide, 50 against 32, 18 heads of 4055 queries over 2391 keys 244 against 205.  Parts cost
+// their sums' way through memory: 8 heads of 2500 tokens 96 us in three, 74 whole, 6 heads of 7460 and fewer keys 348 and
+// 258; but 4 heads of 200 queries over 6000 keys 21 in eight, 34 in two.  The estimate's rates are fitted to 108 drawn calls
+// in up to 13 plans each, for which its choice is 0.3 % above the best in the mean, 8 at most.
 struct DiffPlan {
     int32_t by_keys, split;
 };
@@ -1241,11 +1241,13 @@ int64_t finish(int64_t n1, int64_t l1, int64_t n2, int64_t l2, int64_t slots) {
 
 // Backward: whether eight waves take a tile, and workgroups that share the walk of a tile of keys, of queries, by an
 // estimate of when the last workgroup ends.  Eight waves to a tile, two to a SIMD where there is a tile to a CU: 16 heads
-// of 1024 tokens, 72 wide, 60 us against 73, one head of 4096 56 against 62; but 15 heads of 1500 tokens 100 against 84.
-// Parts, of either side's walks: 15 heads of 2734 queries over 1175 keys and fewer 137 -> 97 us, 32 heads of 4096 queries
-// over 226 keys and fewer 283 -> 95 (their dK and dV are 64 tiles of 128 chunks each), the other way round (200 queries
-// over 6000 keys) 104 -> 34; but 8 heads of 961 queries over 3723 keys, 72 wide, 119 against 103 whole.  The estimate's
-// rates are fitted to 273 drawn calls in up to 24 plans each, for which its choice is 1.6 % above the best in the mean.
+// of 1024 tokens, 72 wide, 56 us against 67, 15 heads of 2734 queries over 1175 keys and fewer 92 against 122; but 15 heads
+// of 1500 tokens 95 against 79.  Parts, of either side's walks: one head of 4096 tokens 55 us, by eight waves in four of dK
+// and dV and three of dQ, 122 whole; 32 heads of 4096 queries over 226 keys and fewer, 72 wide, 95 in six, 246 whole (their
+// dK and dV are 64 tiles of 128 chunks each); the other way round (4 heads of 200 queries over 6000 keys) 35 and 163; 8
+// heads of 961 queries over 3723 keys, 72 wide, 98 in two of dQ, 153 whole; but 8 heads of 2500 tokens 145 in two, 119
+// whole.  The estimate's rates are fitted to 273 drawn calls in up to 24 plans each, for which its choice is 1.4 % above
+// the best in the mean, 43 at most.
 struct DiffBackPlan {
     int32_t two, q_first, split_k, split_q;
 };

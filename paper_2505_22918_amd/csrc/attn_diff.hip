@@ -25,9 +25,9 @@
 // 17776 tokens 6.56 -> 10.0 ms, one head of 4096 35 -> 49 us).  diff_few, which waits for memory, makes it.
 //
 // Bound by the matrix cores and vector issue under the power limit, as plain attention is: 2 samples of 15 heads, 17776
-// tokens, D = 64 take 6.6 to 7.3 ms (1.00 to 1.11 PFLOP/s of 12 D; matrix cores busy 54 % at 1.64 to 1.71 GHz, 152 vector
+// tokens, D = 64 take 6.6 to 7.3 ms (1.00 to 1.11 PFLOP/s of 12 D; matrix cores busy 55 % at 1.64 to 1.73 GHz, 152 vector
 // instructions and 24 matrix products a chunk of 32 x 32), their gradients 15.9 to 17.8 ms (0.96 to 1.07 PFLOP/s
-// executed; 54 % at 1.70 to 1.79 GHz; waves wait 26 % of their time).  Two waves to a SIMD is what the registers
+// executed; 55 % at 1.70 to 1.80 GHz; waves wait 26 % of their time).  Two waves to a SIMD is what the registers
 // allow: a wave holds 32 x 2 D sums for both maps (128 registers) forward, 32 x 4 D backward.  So the walk of dK and dV
 // keeps its own values in LDS, and offsets packed; with spills of 90 registers it took twice the time.
 
